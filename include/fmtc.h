@@ -302,6 +302,111 @@ fmtc_status fmtc_decode_u8(const fmtc_basis8 *basis, const void *d_stream_in, si
                            int64_t N, int C, int H, int W, fmtc_layout layout, int bits, uint32_t *d_err_flag,
                            void *d_workspace, size_t ws_bytes, void *hip_stream);
 
+/* ---- a block of a network in 8-bit floating point ----
+ * What makes and reads the activations that the codec stores: rows (pixels of
+ * an NHWC tensor, or tokens) of channels, products with weights, and what lies
+ * between two products.  Matrices that enter a product are held as 8-bit codes
+ * with one scale per block of 128.  All calls are asynchronous, allocate
+ * nothing, need no alignment of bf16 / f16 / f32 arrays beyond their type, and
+ * take row strides in elements.  Sums, norms and statistics are held in f32.
+ * Zero rows are allowed (nothing is launched, or sums over rows are 0). */
+typedef enum fmtc_dtype { FMTC_F32 = 0, FMTC_BF16 = 1, FMTC_F16 = 2 } fmtc_dtype;
+typedef enum fmtc_f8_format { FMTC_E4M3 = 0, FMTC_E5M2 = 1 } fmtc_f8_format;   /* OCP 8-bit formats; E4M3 has no infinity */
+typedef enum fmtc_f8_scale { FMTC_SCALE_F32 = 0, FMTC_SCALE_E8M0 = 1 } fmtc_f8_scale; /* float, or 2^(byte - 127) */
+#define FMTC_F8_BLOCK 128
+
+/* A matrix [rows][depth] in 8-bit floating point: value = code * scale of its
+ * block, a block being block_rows x 128 (block_rows: 1 for activations and
+ * gradients, 128 for weights).  Codes: `ld` bytes from row to row, a multiple
+ * of 16 and at least depth rounded up to 128; the bytes from `depth` up to that
+ * are read and must be 0.  Scales: scale[k / 128][row / block_rows], `ld_scales`
+ * of them from one block of the depth to the next (a product walks the depth
+ * and wants the scales of many rows at a time).  d_codes 16-byte aligned. */
+typedef struct fmtc_f8 {
+    void *d_codes;
+    void *d_scales;
+    int64_t rows, depth;
+    int64_t ld, ld_scales;
+    int32_t format, scale, block_rows;
+} fmtc_f8;
+
+/* Quantizes d_x [rows][cols] into *by_rows ([rows][cols], for products over the
+ * columns) and/or *by_cols (the transpose [cols][rows], for products over the
+ * rows); either may be NULL.  Per block: a = largest finite magnitude; F32
+ * scales: s = max(a * (1 / L), 2^-126), L the largest code (448 or 57344); E8M0:
+ * the smallest power of two >= a / L, at least 2^-126; code = x * (1 / s) rounded
+ * to the nearest, ties to even (1 / L, 1 / s and both products rounded to f32).  NaN gives NaN; infinities give NaN in E4M3 and infinities
+ * in E5M2; they do not change the codes of their neighbours.  The zeros behind
+ * the depth are written too.  With block_rows = 128 both outputs hold the same
+ * codes and scales, transposed.  With both outputs format, scale and block_rows
+ * have to agree. */
+fmtc_status fmtc_f8_quantize(const void *d_x, fmtc_dtype type, int64_t rows, int64_t cols, int64_t ld_x,
+                             const fmtc_f8 *by_rows, const fmtc_f8 *by_cols, void *hip_stream);
+
+/* out[m][n] = sum_k a[m][k] b[n][k] (+ bias[n]), a: block_rows 1, either format;
+ * b: block_rows 1 or 128, E4M3; the same depth and kind of scale.  Sums are in
+ * f32, with one rounding to out_type at the end.  For BF16 and F16 outputs a
+ * block's products run on the 8-bit matrix instructions, which drop what of a
+ * product lies below 2^-13 of the largest of its group of 8 (about 2e-5 of a
+ * result's size, a tenth of an F16 rounding at most); for F32 outputs the codes
+ * are widened to f16 on the way, where every product is exact.  accumulate != 0 (out_type F32 only):
+ * added to what d_out holds.  d_bias: f32, may be NULL.  Workspace: 256-byte
+ * aligned, fmtc_f8_matmul_workspace_size(rows of a, rows of b, depth) bytes (may
+ * be 0: then NULL is fine).  Results do not depend on the run. */
+size_t fmtc_f8_matmul_workspace_size(int64_t M, int64_t N, int64_t K);
+fmtc_status fmtc_f8_matmul(const fmtc_f8 *a, const fmtc_f8 *b, const float *d_bias, void *d_out, fmtc_dtype out_type,
+                           int64_t ld_out, int accumulate, void *d_workspace, size_t ws_bytes, void *hip_stream);
+
+/* Gradients of y = x w^T + bias, x [P][K], w [O][K], from d_dy [P][O]:
+ * dx = dy w (d_dx [P][K], dx_type), dw = dy^T x (d_dw [O][K] f32), dbias = sum over
+ * the rows of dy (f32).  dy is quantized to `format` with `scale` scales, by rows
+ * for dx and by columns for dw; dbias uses dy as it is.  w_t: the weights'
+ * transpose ([K][O], block_rows 128, by_cols of fmtc_f8_quantize), x_t: x by
+ * columns ([K][P], block_rows 1); both E4M3 with `scale` scales.  d_dx (with
+ * w_t), d_dw (with x_t) and d_dbias may be NULL.  accumulate != 0: dw and dbias
+ * are added to what the arrays hold. */
+size_t fmtc_f8_matmul_backward_workspace_size(int64_t P, int64_t K, int64_t O);
+fmtc_status fmtc_f8_matmul_backward(const void *d_dy, fmtc_dtype dy_type, int64_t P, int64_t O, int64_t ld_dy,
+                                    const fmtc_f8 *w_t, const fmtc_f8 *x_t, fmtc_f8_format format, fmtc_f8_scale scale,
+                                    void *d_dx, fmtc_dtype dx_type, int64_t ld_dx, float *d_dw, int64_t ld_dw,
+                                    float *d_dbias, int accumulate, void *d_workspace, size_t ws_bytes,
+                                    void *hip_stream);
+
+/* What lies between two blocks, in one pass over the rows: with y the output of
+ * a block and h the stream that it read,
+ *     u  = w_post * y / rms(y)                rms(v) = sqrt(mean(v^2) + eps)
+ *     h' = skip * h + scale * gate * u
+ *     n  = w_pre * h' / rms(h')               (from h' before it is rounded)
+ * Rows of C channels, 1 <= C <= 16384.  d_w_post NULL: u = y.  d_gate NULL: 1;
+ * else [ceil(rows / rows_per_gate)][C], row p takes gate row p / rows_per_gate.
+ * d_y NULL: h' = skip * h (d_w_post and d_gate NULL too).  d_w_pre NULL: no n.
+ * y, h, h' and n are `type`; w_post, w_pre and gate f32 or `type`. */
+typedef struct fmtc_norm {
+    int64_t rows;
+    int32_t C, type, weight_type, reserved;
+    const void *d_y, *d_h;
+    int64_t ld_y, ld_h;
+    const void *d_w_post, *d_w_pre, *d_gate;
+    int64_t rows_per_gate;
+    float skip, scale, eps;
+} fmtc_norm;
+/* d_h_out (may be h itself, or NULL: not stored), d_n and n_codes (block_rows 1;
+ * the codes of fmtc_f8_quantize for n before it is rounded): any may be NULL,
+ * not all.  d_stats: f32 [2][rows], 1 / rms(y) (1 without w_post) and 1 / rms(h'),
+ * what the backward pass needs; may be NULL. */
+fmtc_status fmtc_block_norm(const fmtc_norm *args, void *d_h_out, int64_t ld_h_out, void *d_n, int64_t ld_n,
+                            const fmtc_f8 *n_codes, float *d_stats, void *hip_stream);
+/* The gradients, from dn (of n) and dh (of h', what reaches the stream from the
+ * later blocks); either may be NULL (0).  args: as in the forward call, but d_h is
+ * h' as it was stored; eps is not read.  Outputs, any NULL: d_dy, d_dh_in (of h; may
+ * be dh itself) in `type`; d_dw_post, d_dw_pre [C] and d_dgate (as d_gate) in f32.
+ * Sums over rows are in a fixed order. */
+size_t fmtc_block_norm_workspace_size(int64_t rows, int C, int64_t rows_per_gate);
+fmtc_status fmtc_block_norm_backward(const fmtc_norm *args, const float *d_stats, const void *d_dn, int64_t ld_dn,
+                                     const void *d_dh, int64_t ld_dh, void *d_dy, int64_t ld_dy, void *d_dh_in,
+                                     int64_t ld_dh_in, float *d_dw_post, float *d_dw_pre, float *d_dgate,
+                                     void *d_workspace, size_t ws_bytes, void *hip_stream);
+
 /* ---- instrumentation (not part of the method) ----
  * fmtc_profile_enable(n > 0) creates n HIP event pairs per kernel; from then on
  * every kernel launch of the library carries a pair attached to its own

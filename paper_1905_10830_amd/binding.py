@@ -11,6 +11,10 @@ import os
 NCHW, NHWC = 0, 1
 OK, EINVAL, EBUFSIZE, ECORRUPT, ENOMEM, EHIP = range(6)
 ERR_HEADER, ERR_TABLE, ERR_OFFSETS, ERR_CODE = 1, 2, 4, 8
+F32, BF16, F16 = range(3)
+E4M3, E5M2 = range(2)
+SCALE_F32, SCALE_E8M0 = range(2)
+F8_BLOCK = 128
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libfmtc.so")
@@ -26,11 +30,28 @@ EXPORTS = [
     "fmtc_fit_state_destroy", "fmtc_basis_truncate",
     "fmtc_basis8_create", "fmtc_basis8_export", "fmtc_basis8_destroy", "fmtc_quantize_u8", "fmtc_reconstruct_u8",
     "fmtc_encode_u8", "fmtc_decode_u8",
+    "fmtc_f8_quantize", "fmtc_f8_matmul_workspace_size", "fmtc_f8_matmul", "fmtc_f8_matmul_backward_workspace_size",
+    "fmtc_f8_matmul_backward", "fmtc_block_norm", "fmtc_block_norm_workspace_size", "fmtc_block_norm_backward",
     "fmtc_profile_enable", "fmtc_profile_kernels", "fmtc_profile_name", "fmtc_profile_read", "fmtc_profile_copy",
     "fmtc_test_option", "fmtc_test_projection",
 ]
 
 _lib = None
+
+
+class _F8(ctypes.Structure):
+    _fields_ = [("d_codes", ctypes.c_void_p), ("d_scales", ctypes.c_void_p), ("rows", ctypes.c_int64),
+                ("depth", ctypes.c_int64), ("ld", ctypes.c_int64), ("ld_scales", ctypes.c_int64),
+                ("format", ctypes.c_int32), ("scale", ctypes.c_int32), ("block_rows", ctypes.c_int32)]
+
+
+class _Norm(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("C", ctypes.c_int32), ("type", ctypes.c_int32),
+                ("weight_type", ctypes.c_int32), ("reserved", ctypes.c_int32), ("d_y", ctypes.c_void_p),
+                ("d_h", ctypes.c_void_p), ("ld_y", ctypes.c_int64), ("ld_h", ctypes.c_int64),
+                ("d_w_post", ctypes.c_void_p), ("d_w_pre", ctypes.c_void_p), ("d_gate", ctypes.c_void_p),
+                ("rows_per_gate", ctypes.c_int64), ("skip", ctypes.c_float), ("scale", ctypes.c_float),
+                ("eps", ctypes.c_float)]
 
 
 class FmtcError(RuntimeError):
@@ -96,6 +117,20 @@ def load_library():
     lib.fmtc_stream_info.argtypes = [vp, sz, ctypes.POINTER(i32), ctypes.POINTER(i32), ctypes.POINTER(i64),
                                      ctypes.POINTER(i32), ctypes.POINTER(i64), ctypes.POINTER(f32),
                                      ctypes.POINTER(ctypes.c_uint64), ctypes.POINTER(ctypes.c_uint64)]
+    f8 = ctypes.POINTER(_F8)
+    lib.fmtc_f8_quantize.argtypes = [vp, i32, i64, i64, i64, f8, f8, vp]
+    lib.fmtc_f8_matmul_workspace_size.argtypes = [i64, i64, i64]
+    lib.fmtc_f8_matmul_workspace_size.restype = sz
+    lib.fmtc_f8_matmul.argtypes = [f8, f8, vp, vp, i32, i64, i32, vp, sz, vp]
+    lib.fmtc_f8_matmul_backward_workspace_size.argtypes = [i64, i64, i64]
+    lib.fmtc_f8_matmul_backward_workspace_size.restype = sz
+    lib.fmtc_f8_matmul_backward.argtypes = [vp, i32, i64, i64, i64, f8, f8, i32, i32, vp, i32, i64, vp, i64, vp, i32, vp,
+                                            sz, vp]
+    lib.fmtc_block_norm.argtypes = [ctypes.POINTER(_Norm), vp, i64, vp, i64, f8, vp, vp]
+    lib.fmtc_block_norm_workspace_size.argtypes = [i64, i32, i64]
+    lib.fmtc_block_norm_workspace_size.restype = sz
+    lib.fmtc_block_norm_backward.argtypes = [ctypes.POINTER(_Norm), vp, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp,
+                                             sz, vp]
     lib.fmtc_last_error.restype = ctypes.c_char_p
     lib.fmtc_profile_enable.argtypes = [i32]
     lib.fmtc_profile_name.argtypes = [i32]
@@ -549,6 +584,239 @@ def stream_info(header_bytes):
                                            ctypes.byref(pbits), ctypes.byref(sbytes)))
     return dict(bits=bits.value, C=C.value, P=P.value, px_per_chunk=ppc.value, n_chunks=nch.value,
                 delta=dlt.value, payload_bits=pbits.value, stream_bytes=sbytes.value)
+
+
+# ---- a block of a network in 8-bit floating point ----
+
+def _dtype(t):
+    import torch
+
+    try:
+        return {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}[t]
+    except KeyError:
+        raise ValueError(f"expected float32, bfloat16 or float16, got {t}") from None
+
+
+def _rows(t, what, cols=None, rows=None, dtype=None):
+    """A device matrix whose rows are contiguous -> (pointer, type, row stride)."""
+    import torch
+
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 2):
+        raise ValueError(f"{what}: expected a 2-d device tensor")
+    r, c = t.shape
+    if (cols is not None and c != cols) or (rows is not None and r != rows):
+        raise ValueError(f"{what}: expected {rows} x {cols} values, got {r} x {c}")
+    step_r, step_c = t.stride()
+    if c > 1 and step_c != 1:
+        raise ValueError(f"{what}: the values of a row have to be adjacent")
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{what}: expected {dtype}, got {t.dtype}")
+    return t.data_ptr(), _dtype(t.dtype), step_r if r > 1 else c
+
+
+def _vector(t, what, n, dtype=None):
+    """A contiguous device vector of n values -> pointer (None: None)."""
+    import torch
+
+    if t is None:
+        return None
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.is_contiguous() and t.numel() == n) or \
+            (dtype is not None and t.dtype != dtype):
+        raise ValueError(f"{what}: expected {n} contiguous device values" + (f" of {dtype}" if dtype else ""))
+    return t.data_ptr()
+
+
+def _workspace(workspace, size, device):
+    import torch
+
+    if size and workspace is None:
+        workspace = torch.empty(size, dtype=torch.uint8, device=device)
+    if workspace is None:
+        return None, None, 0
+    return workspace, _dev(workspace, torch.uint8), workspace.numel()
+
+
+class F8:
+    """A matrix [rows, depth] in 8-bit floating point with a scale per block (fmtc_f8): codes, a tensor [rows, ld] of
+    torch.float8_e4m3fn or torch.float8_e5m2 (ld: depth rounded up to 128 or more, zeros behind the depth), and scales
+    [ceil(depth / 128), ceil(rows / block_rows)] of torch.float32 or torch.float8_e8m0fnu."""
+
+    __slots__ = ("codes", "scales", "rows", "depth", "block_rows", "_c")
+
+    def __init__(self, codes, scales, depth, block_rows=1):
+        import torch
+
+        formats = {torch.float8_e4m3fn: E4M3, torch.float8_e5m2: E5M2}
+        kinds = {torch.float32: SCALE_F32, torch.float8_e8m0fnu: SCALE_E8M0}
+        if codes.dim() != 2 or scales.dim() != 2 or codes.dtype not in formats or scales.dtype not in kinds or \
+                not (codes.is_cuda and scales.is_cuda):
+            raise ValueError("F8: expected 2-d device tensors, codes in an 8-bit format, scales f32 or e8m0")
+        self.codes, self.scales, self.depth, self.block_rows = codes, scales, int(depth), int(block_rows)
+        self.rows, width = codes.shape
+        blocks = -(-self.depth // F8_BLOCK)
+        if self.depth < 1 or self.block_rows not in (1, F8_BLOCK) or width < blocks * F8_BLOCK or \
+                scales.shape[0] != blocks or scales.shape[1] != -(-self.rows // self.block_rows):
+            raise ValueError(f"F8: codes {tuple(codes.shape)} and scales {tuple(scales.shape)} do not hold {self.rows} x "
+                             f"{depth} values in blocks of {block_rows} x {F8_BLOCK}")
+        if codes.stride(1) != 1 or (scales.shape[1] > 1 and scales.stride(1) != 1):
+            raise ValueError("F8: the codes of a row and the scales of a block of the depth have to be adjacent")
+        self._c = _F8(codes.data_ptr(), scales.data_ptr(), self.rows, self.depth, codes.stride(0) if self.rows > 1 else width,
+                      scales.stride(0) if blocks > 1 else scales.shape[1], formats[codes.dtype], kinds[scales.dtype],
+                      self.block_rows)
+
+
+def f8_empty(rows, depth, fmt=E4M3, scales=SCALE_F32, block_rows=1, device="cuda"):
+    """An F8 to be written by f8_quantize or block_norm."""
+    import torch
+
+    blocks = -(-depth // F8_BLOCK)
+    return F8(torch.empty((rows, blocks * F8_BLOCK), dtype=torch.float8_e5m2 if fmt == E5M2 else torch.float8_e4m3fn, device=device),
+              torch.empty((blocks, -(-rows // block_rows)), dtype=torch.float8_e8m0fnu if scales == SCALE_E8M0 else torch.float32,
+                          device=device), depth, block_rows)
+
+
+def _f8(q):
+    return None if q is None else ctypes.byref(q._c)
+
+
+def f8_quantize(x, by_rows=True, by_cols=False, fmt=E4M3, scales=SCALE_F32, block_rows=1):
+    """Asynchronous.  x: device matrix [rows, cols].  -> (F8 [rows, cols] or None, F8 [cols, rows] or None); by_rows and
+    by_cols say which are wanted, or are the F8 to be written."""
+    ptr, kind, ld = _rows(x, "x")
+    rows, cols = x.shape
+    if by_rows is True:
+        by_rows = f8_empty(rows, cols, fmt, scales, block_rows, x.device)
+    if by_cols is True:
+        by_cols = f8_empty(cols, rows, fmt, scales, block_rows, x.device) if rows else None
+    by_rows, by_cols = by_rows or None, by_cols or None
+    _check(load_library().fmtc_f8_quantize(ptr, kind, rows, cols, ld, _f8(by_rows), _f8(by_cols), _stream()))
+    return by_rows, by_cols
+
+
+def f8_matmul_workspace_size(M, N, K):
+    return load_library().fmtc_f8_matmul_workspace_size(M, N, K)
+
+
+def f8_matmul(a, b, bias=None, out=None, dtype=None, accumulate=False, workspace=None):
+    """Asynchronous.  a: F8 [M, K], b: F8 [N, K] -> a b^T + bias [M, N] in `dtype` (bf16 unless given, or out's)."""
+    import torch
+
+    M, N = a.rows, b.rows
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate needs the output that is added to")
+        out = torch.empty((M, N), dtype=dtype or torch.bfloat16, device=a.codes.device)
+    ptr, kind, ld = _rows(out, "out", N, M, dtype)
+    lib = load_library()
+    workspace, ws, size = _workspace(workspace, lib.fmtc_f8_matmul_workspace_size(M, N, a.depth), out.device)
+    _check(lib.fmtc_f8_matmul(_f8(a), _f8(b), _vector(bias, "bias", N, torch.float32), ptr, kind, ld, int(accumulate), ws, size,
+                              _stream()))
+    return out
+
+
+def f8_matmul_backward_workspace_size(P, K, O):
+    return load_library().fmtc_f8_matmul_backward_workspace_size(P, K, O)
+
+
+def f8_matmul_backward(dy, w_t, x_t, fmt=E4M3, scales=SCALE_F32, bias=False, dx=None, dw=None, dbias=None, accumulate=False,
+                       workspace=None):
+    """Asynchronous.  Gradients of y = x w^T + bias: dy [P, O]; w_t: the weights as F8 [K, O] in 128 x 128 blocks (None: no
+    dx); x_t: x by columns as F8 [K, P] (None: no dw).  -> (dx [P, K] in dy's type, dw [O, K] f32, dbias [O] f32), None
+    where not wanted (dbias: wanted with bias=True or where given).  accumulate: dw and dbias are added to."""
+    import torch
+
+    ptr, kind, ld = _rows(dy, "dy")
+    P, O = dy.shape
+    if accumulate and ((x_t is not None and dw is None) or (bias and dbias is None)):
+        raise ValueError("accumulate needs the outputs that are added to")
+    if w_t is not None and dx is None:
+        dx = torch.empty((P, w_t.rows), dtype=dy.dtype, device=dy.device)
+    if x_t is not None and dw is None:
+        dw = torch.empty((O, x_t.rows), dtype=torch.float32, device=dy.device)
+    if bias and dbias is None:
+        dbias = torch.empty(O, dtype=torch.float32, device=dy.device)
+    if (dx is not None and w_t is None) or (dw is not None and x_t is None):
+        raise ValueError("dx needs w_t, dw needs x_t")
+    dx_ptr, dx_kind, dx_ld = _rows(dx, "dx", w_t.rows, P) if dx is not None else (None, F32, 0)
+    dw_ptr, _, dw_ld = _rows(dw, "dw", x_t.rows, O, torch.float32) if dw is not None else (None, F32, 0)
+    K = w_t.rows if w_t is not None else x_t.rows if x_t is not None else 1
+    lib = load_library()
+    workspace, ws, size = _workspace(workspace, lib.fmtc_f8_matmul_backward_workspace_size(P, K, O), dy.device)
+    _check(lib.fmtc_f8_matmul_backward(ptr, kind, P, O, ld, _f8(w_t), _f8(x_t), fmt, scales, dx_ptr, dx_kind, dx_ld, dw_ptr, dw_ld,
+                                       _vector(dbias, "dbias", O, torch.float32), int(accumulate), ws, size, _stream()))
+    return dx, dw, dbias
+
+
+def _norm_args(y, h, w_post, w_pre, gate, rows_per_gate, skip, scale, eps):
+    P, C = h.shape
+    a = _Norm(rows=P, C=C, skip=skip, scale=scale, eps=eps)
+    a.d_h, a.type, a.ld_h = _rows(h, "h")
+    if y is not None:
+        a.d_y, _, a.ld_y = _rows(y, "y", C, P, h.dtype)
+    kinds = {t.dtype for t in (w_post, w_pre, gate) if t is not None}
+    if len(kinds) > 1:
+        raise ValueError("w_post, w_pre and gate have different types")
+    a.weight_type = _dtype(kinds.pop()) if kinds else F32
+    a.d_w_post, a.d_w_pre = _vector(w_post, "w_post", C), _vector(w_pre, "w_pre", C)
+    if gate is not None:
+        a.rows_per_gate = int(rows_per_gate) or max(P, 1)
+        a.d_gate = _vector(gate, "gate", -(-P // a.rows_per_gate) * C if P and a.rows_per_gate > 0 else gate.numel())
+    return a
+
+
+def block_norm(y, h, w_post, w_pre, gate=None, rows_per_gate=0, skip=1.0, scale=1.0, eps=1e-6, h_out=None, n_out=None,
+               stats=None):
+    """Asynchronous.  u = w_post y / rms(y); h' = skip h + scale gate u; n = w_pre h' / rms(h').  y (or None), h: [P, C];
+    gate: [ceil(P / rows_per_gate), C] (rows_per_gate 0: one row for all).  h_out: the tensor to write h' to (None: a new
+    one, False: not stored); n_out: a tensor or an F8 to write n to (None: a new tensor).  stats: the f32 tensor [2, P]
+    that the backward pass needs, or True for a new one.  -> (h', n, stats), None where there is none."""
+    import torch
+
+    a = _norm_args(y, h, w_post, w_pre, gate, rows_per_gate, skip, scale, eps)
+    P, C = h.shape
+    if h_out is None:
+        h_out = torch.empty((P, C), dtype=h.dtype, device=h.device)
+    elif h_out is False:
+        h_out = None
+    if n_out is None and w_pre is not None:
+        n_out = torch.empty((P, C), dtype=h.dtype, device=h.device)
+    if stats is True:
+        stats = torch.empty((2, P), dtype=torch.float32, device=h.device)
+    h_ptr, _, h_ld = _rows(h_out, "h_out", C, P, h.dtype) if h_out is not None else (None, 0, 0)
+    n_codes = n_out if isinstance(n_out, F8) else None
+    n_ptr, _, n_ld = _rows(n_out, "n_out", C, P, h.dtype) if n_out is not None and n_codes is None else (None, 0, 0)
+    _check(load_library().fmtc_block_norm(ctypes.byref(a), h_ptr, h_ld, n_ptr, n_ld, _f8(n_codes),
+                                          _vector(stats, "stats", 2 * P, torch.float32), _stream()))
+    return h_out, n_out, stats
+
+
+def block_norm_workspace_size(P, C, rows_per_gate=0):
+    return load_library().fmtc_block_norm_workspace_size(P, C, rows_per_gate)
+
+
+def block_norm_backward(dn, dh, y, h_out, stats, w_post, w_pre, gate=None, rows_per_gate=0, skip=1.0, scale=1.0, dy=None,
+                        dh_in=None, workspace=None):
+    """Asynchronous.  dn, dh: gradients of n and of h' (either may be None); h_out: h' as block_norm stored it, stats as it
+    left them.  dy, dh_in: tensors to write to (None: new ones).  -> (dy, dh_in, dw_post, dw_pre, dgate), the last three in
+    f32, None where there is no such input."""
+    import torch
+
+    a = _norm_args(y, h_out, w_post, w_pre, gate, rows_per_gate, skip, scale, 0.0)
+    P, C = h_out.shape
+    new = lambda like: torch.empty(like.shape, dtype=torch.float32, device=h_out.device) if like is not None else None  # noqa: E731
+    dw_post, dw_pre, dgate = new(w_post), new(w_pre), new(gate)
+    if dy is None and y is not None:
+        dy = torch.empty((P, C), dtype=h_out.dtype, device=h_out.device)
+    if dh_in is None:
+        dh_in = torch.empty((P, C), dtype=h_out.dtype, device=h_out.device)
+    of = lambda t, what: _rows(t, what, C, P, h_out.dtype) if t is not None else (None, 0, 0)  # noqa: E731
+    (dn_p, _, dn_ld), (dh_p, _, dh_ld), (dy_p, _, dy_ld), (di_p, _, di_ld) = of(dn, "dn"), of(dh, "dh"), of(dy, "dy"), of(dh_in, "dh_in")
+    ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    lib = load_library()
+    workspace, ws, size = _workspace(workspace, lib.fmtc_block_norm_workspace_size(P, C, a.rows_per_gate), h_out.device)
+    _check(lib.fmtc_block_norm_backward(ctypes.byref(a), _vector(stats, "stats", 2 * P, torch.float32), dn_p, dn_ld, dh_p, dh_ld,
+                                        dy_p, dy_ld, di_p, di_ld, ptr(dw_post), ptr(dw_pre), ptr(dgate), ws, size, _stream()))
+    return dy, dh_in, dw_post, dw_pre, dgate
 
 
 TEST_STATIC_TWO_KERNELS, TEST_DECODE_ONE_ROW, TEST_SHORT_WAITS = 0, 1, 2

@@ -8,6 +8,7 @@
 #include <new>
 #include <vector>
 
+#include "fmtc_block.h"
 #include "fmtc_internal.h"
 #include "fmtc_pack_device.h"
 
@@ -425,6 +426,14 @@ fmtc_status upload_basis8(fmtc_basis8* b) {
 }
 
 }  // namespace
+
+fmtc_status fmtc::set_error(fmtc_status st, const char* fmt, ...) {
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(g_err, sizeof g_err, fmt, ap);
+    va_end(ap);
+    return st;
+}
 
 extern "C" {
 

@@ -135,7 +135,8 @@ int test_option(int which);  // current value (0 unless a test set it)
 // ---- optional per-kernel timing (fmtc_profile_* in fmtc.h) ----
 // When enabled, a launch carries a pair of events that the runtime attaches to the kernel's own dispatch, so
 // the elapsed time is the kernel's start-to-end time on the GPU (no bracket of separate marker commands).
-enum KernelId { K_PROJECT = 0, K_HISTOGRAM, K_TABLE, K_PACK, K_DECODE, K_COPY, K_QUANTIZE_U8, K_RECONSTRUCT_U8, K_COUNT };
+enum KernelId { K_PROJECT = 0, K_HISTOGRAM, K_TABLE, K_PACK, K_DECODE, K_COPY, K_QUANTIZE_U8, K_RECONSTRUCT_U8,
+                K_F8_QUANTIZE, K_F8_MATMUL, K_BLOCK_NORM, K_BLOCK_NORM_BACKWARD, K_COUNT };
 bool prof_next(int id, hipEvent_t* start, hipEvent_t* stop);
 
 template <class T>
