@@ -4,7 +4,10 @@
 // first operand and a's its second: a lane then holds four consecutive columns n of one row m of the result, so that sa is
 // one number per lane and the results leave in vectors.  Power-of-two scales are operands of the instruction itself; f32
 // scales multiply the block's product, which one fma adds to the running f32 sum.
+#include <type_traits>
+
 #include "fmtc_block.h"
+#include "fmtc_device.h"
 
 namespace fmtc {
 
@@ -53,11 +56,17 @@ __device__ __forceinline__ v8h widen8(int lo, int hi) {
     }
     return v8h{r[0][0], r[0][1], r[1][0], r[1][1], r[2][0], r[2][1], r[3][0], r[3][1]};
 }
+struct Wide { v8h v[4]; };
 template <int FORMAT>
-__device__ __forceinline__ v4f mfma_block_wide(v8i b, v8i a, v4f c) {
+__device__ __forceinline__ Wide widen(v8i q) {
+    Wide w;
 #pragma unroll
-    for (int j = 0; j < 4; j++)
-        c = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen8<FMTC_E4M3>(b[2 * j], b[2 * j + 1]), widen8<FORMAT>(a[2 * j], a[2 * j + 1]), c, 0, 0, 0);
+    for (int j = 0; j < 4; j++) w.v[j] = widen8<FORMAT>(q[2 * j], q[2 * j + 1]);
+    return w;
+}
+__device__ __forceinline__ v4f mfma_block_wide(const Wide& b, const Wide& a, v4f c) {
+#pragma unroll
+    for (int j = 0; j < 4; j++) c = __builtin_amdgcn_mfma_f32_16x16x32_f16(b.v[j], a.v[j], c, 0, 0, 0);
     return c;
 }
 
@@ -142,7 +151,7 @@ __global__ __launch_bounds__(64 * kRowsWaves) void k_f8_matmul_rows(Product p, u
             for (int i = 0; i < MT; i++) {
                 const float sa = scale_value(p.sa, kind, kb * p.ld_sa + m_at[i]);
                 const v8i a = load_operand(a_row[i] + kb * kF8Block, g);
-                const v4f zero = {}, d = WAY == kScaled ? mfma_block<FORMAT>(b, a, zero) : mfma_block_wide<FORMAT>(b, a, zero);
+                const v4f zero = {}, d = WAY == kScaled ? mfma_block<FORMAT>(b, a, zero) : mfma_block_wide(widen<FMTC_E4M3>(b), widen<FORMAT>(a), zero);
 #pragma unroll
                 for (int r = 0; r < 4; r++) acc[i][r] = fmaf(d[r], sa * sb[r], acc[i][r]);
             }
@@ -162,6 +171,200 @@ __global__ __launch_bounds__(64 * kRowsWaves) void k_f8_matmul_rows(Product p, u
         for (int w = 1; w < kRowsWaves; w++) v += sums[w][i][lane];
         const int64_t m = (mt * MT + i) * 16 + i16, n4 = nt * 16 + g * 4;
         if (m < p.M && n4 < p.N) store_out(p.out, p.out_type, p.ld_out, m, n4, p.N, v, p.bias, p.accumulate);
+    }
+}
+
+// Many rows: a tile of BM x BN results per workgroup, operands through LDS, one block of the depth (128 bytes of a row) a
+// step, two steps' operands in LDS.  A wavefront has MT x 4 tiles of 16 x 16: b's four tiles of a step stay in registers,
+// a's come one after the other, each read while the one before it is multiplied.  The one barrier of a step stands before
+// its last tile of a, when everything that is still needed of the step is in registers: behind it the next step's operands
+// are read and those of the step after it set out into the place that came free, all under the last tile's products.
+//
+// Rows of 128 bytes in LDS, the 16-byte pieces of a row exchanged by a key of the row, so that 16 lanes that read the same
+// piece of 16 rows touch every bank once.  The results leave through LDS too, 64 columns of a row at a time.
+template <int WM_, int WN_, int MT_>
+struct Tile {
+    static constexpr int WM = WM_, WN = WN_, MT = MT_, NT = 4;
+    static constexpr int kThreads = 64 * WM * WN, BM = WM * MT * 16, BN = WN * NT * 16;
+    static constexpr int kStage = (BM + BN) * kF8Block, kScales = 4 * (BM + BN);
+    static constexpr int kLoads = (BM + BN) / 8 / (WM * WN);  // loads of 8 rows a wavefront, a's and b's in one range
+    static constexpr int kPitch = 68, kOutRows = 64;         // results in LDS: a wavefront's 64 rows x 64 columns at a time
+    static constexpr int kLoop = 2 * (kStage + kScales), kOut = WM * WN * kOutRows * kPitch * 4;
+    static constexpr int kLds = kLoop > kOut ? kLoop : kOut;
+    static_assert((BM + BN) % (8 * WM * WN) == 0 && BM % 64 == 0 && MT % 4 == 0);
+    static_assert(BM + BN <= kThreads);  // a thread moves at most one scale
+};
+__device__ __forceinline__ int row_key(int row) { return (row >> 1) & 7; }
+
+// 16 bytes a lane from base + off straight into LDS, lane l to lds_base + 16 l (the caller counts its loads in flight)
+__device__ __forceinline__ void load_to_lds16(const uint8_t* base, uint32_t off, uint32_t lds_base) {
+    uint32_t keep;
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b32 m0, %0"
+                 : "=&s"(keep) : "v"(off), "s"(base), "s"(lds_base) : "memory");
+}
+
+template <int FORMAT, int WAY, int B_ROWS, class S>
+__global__ __launch_bounds__(S::kThreads) void k_f8_matmul_tiles(Product p, uint32_t tiles_m, uint32_t tiles_n) {
+    extern __shared__ __attribute__((aligned(128))) uint8_t lds[];
+    constexpr int MT = S::MT, NT = S::NT;
+    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), g = lane >> 4, i16 = lane & 15;
+    const int wm = wave % S::WM, wn = wave / S::WM;
+
+    // Workgroups go to the 8 XCDs in turn: each XCD gets a range of tiles, and within it four rows of tiles at a time, so
+    // that the tiles that run on it together share operands in its cache.
+    const uint32_t total = tiles_m * tiles_n, each = total / 8, more = total % 8, xcd = blockIdx.x % 8;
+    const uint32_t id = xcd * each + (xcd < more ? xcd : more) + blockIdx.x / 8;
+    const uint32_t span = 4 * tiles_n, first = id / span * 4, in = id % span, deep = tiles_m - first < 4 ? tiles_m - first : 4;
+    const int64_t m0 = (int64_t)(first + in % deep) * S::BM, n0 = (int64_t)(in / deep) * S::BN;
+    const int rows_a = p.M - m0 < S::BM ? (int)(p.M - m0) : S::BM, rows_b = p.N - n0 < S::BN ? (int)(p.N - n0) : S::BN;
+
+    // what this lane moves: 16 bytes of kLoads rows (rows that do not exist: the last one, whose results are not stored)
+    const uint8_t *from_a = p.a + m0 * p.ld_a, *from_b = p.b + n0 * p.ld_b;
+    uint32_t off[S::kLoads];
+#pragma unroll
+    for (int i = 0; i < S::kLoads; i++) {
+        const int row = (wave * S::kLoads + i) * 8 + (lane >> 3);
+        const bool of_a = row < S::BM;
+        const int r = of_a ? (row < rows_a ? row : rows_a - 1) : (row - S::BM < rows_b ? row - S::BM : rows_b - 1);
+        off[i] = (uint32_t)r * (uint32_t)(of_a ? p.ld_a : p.ld_b) + 16 * ((lane & 7) ^ row_key(row));
+    }
+    const uint32_t lds_at = (uint32_t)(uintptr_t)(lds_void_t*)lds;
+    auto fetch = [&](int64_t kb) {
+        const uint32_t to = lds_at + (uint32_t)(kb & 1) * S::kStage + wave * S::kLoads * 1024;
+#pragma unroll
+        for (int i = 0; i < S::kLoads; i++)
+            load_to_lds16(((wave * S::kLoads + i) * 8 < S::BM ? from_a : from_b) + kb * kF8Block, off[i], to + i * 1024);
+    };
+    // scales: a thread has that of a row of a or of b, as a float or an exponent
+    uint32_t* const scales = reinterpret_cast<uint32_t*>(lds + 2 * S::kStage);
+    const bool scale_of_a = wave * 64 < S::BM, has_scale = wave * 64 < S::BM + S::BN;
+    const void* const from_s = scale_of_a ? p.sa : p.sb;
+    const int64_t first_s = scale_of_a ? m0 : n0 / B_ROWS, step_s = scale_of_a ? p.ld_sa : p.ld_sb;
+    uint32_t off_s, mine = 0;
+    if (scale_of_a) off_s = t < rows_a ? t : rows_a - 1;
+    else off_s = (t - S::BM < rows_b ? t - S::BM : rows_b - 1) / B_ROWS;
+    auto fetch_scale = [&](int64_t kb) {
+        if (!has_scale) return;
+        const int64_t at = first_s + kb * step_s + off_s;
+        if constexpr (WAY == kExponents) mine = static_cast<const uint8_t*>(from_s)[at];
+        else mine = __float_as_uint(scale_value(from_s, WAY == kScaled ? (int)FMTC_SCALE_F32 : p.scale, at));
+    };
+    auto put_scale = [&](int64_t kb) {
+        if (has_scale) scales[(kb & 1) * (S::BM + S::BN) + t] = mine;
+    };
+
+    const int row_a = wm * MT * 16 + i16, row_b = S::BM + wn * 64 + i16, key = row_key(i16);  // (the key of row + 16 i, too)
+    auto piece = [&](int64_t kb, int row) {
+        const uint8_t* at = lds + (kb & 1) * S::kStage + row * kF8Block;
+        const v4i lo = *reinterpret_cast<const v4i*>(at + 16 * (g ^ key)), hi = *reinterpret_cast<const v4i*>(at + 16 * ((4 + g) ^ key));
+        return v8i{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    };
+
+    v4f acc[MT][NT] = {};
+    fetch(0);
+    fetch_scale(0);
+    wait_loads<0>();
+    put_scale(0);
+    __syncthreads();
+    if (p.blocks > 1) {
+        fetch_scale(1);
+        fetch(1);
+    }
+    // b's tiles as the way takes them; the products of a tile of a, added to the sums while the next one is multiplied
+    using Held = typename std::conditional<WAY == kWide, Wide, v8i>::type;
+    auto hold = [&](v8i raw) {
+        if constexpr (WAY == kWide) return widen<FMTC_E4M3>(raw);
+        else return raw;
+    };
+    Held b[NT];
+    v8i a = piece(0, row_a);
+#pragma unroll
+    for (int j = 0; j < NT; j++) b[j] = hold(piece(0, row_b + 16 * j));
+    v4f d[NT] = {};
+    float f[NT][4] = {};
+
+    for (int64_t kb = 0; kb < p.blocks; kb++) {
+        const uint32_t* s = scales + (kb & 1) * (S::BM + S::BN);
+        uint32_t sb[NT][4];
+        if constexpr (WAY == kExponents) {
+#pragma unroll
+            for (int j = 0; j < NT; j++) sb[j][0] = s[row_b + 16 * j];
+        } else if constexpr (B_ROWS == 1) {
+#pragma unroll
+            for (int j = 0; j < NT; j++)
+#pragma unroll
+                for (int r = 0; r < 4; r++) sb[j][r] = s[S::BM + wn * 64 + 16 * j + 4 * g + r];
+        } else {
+            sb[0][0] = s[S::BM + wn * 64];
+        }
+#pragma unroll
+        for (int i = 0; i < MT; i++) {
+            const uint32_t sa = s[row_a + 16 * i];
+            if (i == MT - 1) {
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the last tile of a is in registers
+                wait_loads<0>();                                    // the next step's operands (this wavefront's) are in LDS
+                if (kb + 1 < p.blocks) put_scale(kb + 1);
+                __syncthreads();
+                if (kb + 2 < p.blocks) {
+                    fetch_scale(kb + 2);
+                    fetch(kb + 2);
+                }
+            }
+            // (past the last step: what LDS holds, not used)
+            const v8i next = i == MT - 1 ? piece(kb + 1, row_a) : piece(kb, row_a + 16 * (i + 1));
+            if constexpr (WAY == kExponents) {
+#pragma unroll
+                for (int j = 0; j < NT; j++) {
+                    acc[i][j] = mfma_block_scaled<FORMAT>(b[j], a, acc[i][j], (int)sb[j][0], (int)sa);
+                    if (i == MT - 1) b[j] = piece(kb + 1, row_b + 16 * j);
+                }
+            } else {
+                v4f* const before = acc[i ? i - 1 : MT - 1];
+                const auto held = [&] { if constexpr (WAY == kWide) return widen<FORMAT>(a); else return a; }();
+#pragma unroll
+                for (int j = 0; j < NT; j++) {
+                    v4f now;
+                    if constexpr (WAY == kWide) now = mfma_block_wide(b[j], held, v4f{0.f, 0.f, 0.f, 0.f});
+                    else now = mfma_block<FORMAT>(b[j], held, v4f{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+                    for (int r = 0; r < 4; r++) {
+                        before[j][r] = fmaf(d[j][r], f[B_ROWS == 1 ? j : 0][B_ROWS == 1 ? r : 0], before[j][r]);
+                        if constexpr (B_ROWS == 1) f[j][r] = __uint_as_float(sa) * __uint_as_float(sb[j][r]);
+                    }
+                    asm volatile("" : "+v"(before[j]));  // here, and not all of a step's at its end
+                    d[j] = now;
+                    if (i == MT - 1) b[j] = hold(piece(kb + 1, row_b + 16 * j));
+                }
+                if constexpr (B_ROWS != 1) f[0][0] = __uint_as_float(sa) * __uint_as_float(sb[0][0]);
+            }
+            a = next;
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+    if constexpr (WAY != kExponents) {
+#pragma unroll
+        for (int j = 0; j < NT; j++)
+#pragma unroll
+            for (int r = 0; r < 4; r++) acc[MT - 1][j][r] = fmaf(d[j][r], f[B_ROWS == 1 ? j : 0][B_ROWS == 1 ? r : 0], acc[MT - 1][j][r]);
+    }
+    // 4 tiles of a at a time: 64 rows of 64 columns in the wavefront's own part of LDS, then whole rows to memory
+    __syncthreads();
+    float* const out = reinterpret_cast<float*>(lds) + wave * S::kOutRows * S::kPitch;
+    const int64_t n = n0 + wn * 64 + 4 * i16;
+#pragma unroll
+    for (int i0 = 0; i0 < MT; i0 += 4) {
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+#pragma unroll
+            for (int j = 0; j < NT; j++) *reinterpret_cast<v4f*>(out + (16 * i + i16) * S::kPitch + 16 * j + 4 * g) = acc[i0 + i][j];
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll 4
+        for (int r = g; r < 64; r += 4) {
+            const int64_t m = m0 + wm * MT * 16 + i0 * 16 + r;
+            const v4f v = *reinterpret_cast<const v4f*>(out + r * S::kPitch + 4 * i16);
+            if (m < p.M && n < p.N) store_out(p.out, p.out_type, p.ld_out, m, n, p.N, v, p.bias, p.accumulate);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
 }
 
@@ -185,6 +388,14 @@ hipError_t launch_f8_matmul(const fmtc_f8& a, const fmtc_f8& b, const float* d_b
         return with_way(way, [&](auto wy) {
             return with_bit(b.block_rows == 1, [&](auto one) {
                 constexpr int F = decltype(fm)::value, W = decltype(wy)::value, B = decltype(one)::value ? 1 : kF8Block;
+                auto tiles = [&](auto tile) {
+                    using S = decltype(tile);
+                    const int64_t tm = (p.M + S::BM - 1) / S::BM, tn = (p.N + S::BN - 1) / S::BN;
+                    auto kernel = k_f8_matmul_tiles<F, W, B, S>;
+                    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds);
+                    return e != hipSuccess ? e : launch(K_F8_MATMUL, kernel, dim3((unsigned)(tm * tn)), dim3(S::kThreads), S::kLds, s, p, (uint32_t)tm, (uint32_t)tn);
+                };
+                if (p.M > 256 && p.N > 256 && p.ld_a < (1 << 23) && p.ld_b < (1 << 23)) return tiles(Tile<2, 4, W == kWide ? 4 : 8>{});
                 if (p.M <= 16)
                     return launch(K_F8_MATMUL, k_f8_matmul_rows<F, W, B, 1>, dim3((unsigned)n_tiles), dim3(64 * kRowsWaves), 0, s, p,
                                   (uint32_t)n_tiles);
