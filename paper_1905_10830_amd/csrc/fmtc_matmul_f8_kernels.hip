@@ -186,21 +186,19 @@ template <int WM_, int WN_, int MT_>
 struct Tile {
     static constexpr int WM = WM_, WN = WN_, MT = MT_, NT = 4;
     static constexpr int kThreads = 64 * WM * WN, BM = WM * MT * 16, BN = WN * NT * 16;
-    static constexpr int kStage = (BM + BN) * kF8Block, kScales = 4 * (BM + BN);
+    static constexpr int kStage = (BM + BN) * kF8Block, kScales = 4 * kThreads;
     static constexpr int kLoads = (BM + BN) / 8 / (WM * WN);  // loads of 8 rows a wavefront, a's and b's in one range
     static constexpr int kPitch = 68, kOutRows = 64;         // results in LDS: a wavefront's 64 rows x 64 columns at a time
     static constexpr int kLoop = 2 * (kStage + kScales), kOut = WM * WN * kOutRows * kPitch * 4;
     static constexpr int kLds = kLoop > kOut ? kLoop : kOut;
     static_assert((BM + BN) % (8 * WM * WN) == 0 && BM % 64 == 0 && MT % 4 == 0);
-    static_assert(BM + BN <= kThreads);  // a thread moves at most one scale
+    static_assert(BM + BN <= kThreads);  // a thread moves one scale
 };
 __device__ __forceinline__ int row_key(int row) { return (row >> 1) & 7; }
 
 // 16 bytes a lane from base + off straight into LDS, lane l to lds_base + 16 l (the caller counts its loads in flight)
 __device__ __forceinline__ void load_to_lds16(const uint8_t* base, uint32_t off, uint32_t lds_base) {
-    uint32_t keep;
-    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b32 m0, %0"
-                 : "=&s"(keep) : "v"(off), "s"(base), "s"(lds_base) : "memory");
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(base), "s"(lds_base) : "memory", "m0");
 }
 
 template <int FORMAT, int WAY, int B_ROWS, class S>
@@ -229,29 +227,27 @@ __global__ __launch_bounds__(S::kThreads) void k_f8_matmul_tiles(Product p, uint
         off[i] = (uint32_t)r * (uint32_t)(of_a ? p.ld_a : p.ld_b) + 16 * ((lane & 7) ^ row_key(row));
     }
     const uint32_t lds_at = (uint32_t)(uintptr_t)(lds_void_t*)lds;
-    auto fetch = [&](int64_t kb) {
-        const uint32_t to = lds_at + (uint32_t)(kb & 1) * S::kStage + wave * S::kLoads * 1024;
+    // a quarter of a step's loads (all at once, the queue of loads is full and the wavefront stands still)
+    auto fetch = [&](int64_t kb, uint32_t stage, int quarter) {
+        const uint32_t to = lds_at + stage * S::kStage + wave * S::kLoads * 1024;
 #pragma unroll
-        for (int i = 0; i < S::kLoads; i++)
+        for (int i = quarter * S::kLoads / 4; i < (quarter + 1) * S::kLoads / 4; i++)
             load_to_lds16(((wave * S::kLoads + i) * 8 < S::BM ? from_a : from_b) + kb * kF8Block, off[i], to + i * 1024);
     };
     // scales: a thread has that of a row of a or of b, as a float or an exponent
     uint32_t* const scales = reinterpret_cast<uint32_t*>(lds + 2 * S::kStage);
-    const bool scale_of_a = wave * 64 < S::BM, has_scale = wave * 64 < S::BM + S::BN;
+    const bool scale_of_a = wave * 64 < S::BM;
     const void* const from_s = scale_of_a ? p.sa : p.sb;
     const int64_t first_s = scale_of_a ? m0 : n0 / B_ROWS, step_s = scale_of_a ? p.ld_sa : p.ld_sb;
     uint32_t off_s, mine = 0;
     if (scale_of_a) off_s = t < rows_a ? t : rows_a - 1;
     else off_s = (t - S::BM < rows_b ? t - S::BM : rows_b - 1) / B_ROWS;
     auto fetch_scale = [&](int64_t kb) {
-        if (!has_scale) return;
         const int64_t at = first_s + kb * step_s + off_s;
         if constexpr (WAY == kExponents) mine = static_cast<const uint8_t*>(from_s)[at];
         else mine = __float_as_uint(scale_value(from_s, WAY == kScaled ? (int)FMTC_SCALE_F32 : p.scale, at));
     };
-    auto put_scale = [&](int64_t kb) {
-        if (has_scale) scales[(kb & 1) * (S::BM + S::BN) + t] = mine;
-    };
+    auto put_scale = [&](int64_t kb) { scales[(kb & 1) * S::kThreads + t] = mine; };
 
     const int row_a = wm * MT * 16 + i16, row_b = S::BM + wn * 64 + i16, key = row_key(i16);  // (the key of row + 16 i, too)
     auto piece = [&](int64_t kb, int row) {
@@ -261,15 +257,17 @@ __global__ __launch_bounds__(S::kThreads) void k_f8_matmul_tiles(Product p, uint
     };
 
     v4f acc[MT][NT] = {};
-    fetch(0);
+    // (past the last block: that one again, into the place that is free; not used, and no branch in the loop)
+    const int64_t last = p.blocks - 1;
+#pragma unroll
+    for (int q = 0; q < 4; q++) fetch(0, 0, q);
     fetch_scale(0);
     wait_loads<0>();
     put_scale(0);
     __syncthreads();
-    if (p.blocks > 1) {
-        fetch_scale(1);
-        fetch(1);
-    }
+    fetch_scale(last < 1 ? last : 1);
+    fetch(last < 1 ? last : 1, 1, 0);
+    fetch(last < 1 ? last : 1, 1, 1);
     // b's tiles as the way takes them; the products of a tile of a, added to the sums while the next one is multiplied
     using Held = typename std::conditional<WAY == kWide, Wide, v8i>::type;
     auto hold = [&](v8i raw) {
@@ -277,50 +275,55 @@ __global__ __launch_bounds__(S::kThreads) void k_f8_matmul_tiles(Product p, uint
         else return raw;
     };
     Held b[NT];
-    v8i a = piece(0, row_a);
+    v8i a[3];  // tiles i, i + 1 and i + 2: a tile's read has two tiles' products to arrive under
+    uint32_t sa[3], sb[NT][4];
+    auto read_a = [&](int to, int64_t kb, int i) {
+        a[to] = piece(kb, row_a + 16 * i);
+        sa[to] = scales[(kb & 1) * S::kThreads + row_a + 16 * i];
+    };
+    auto read_b = [&](int64_t kb, int j) {
+        b[j] = hold(piece(kb, row_b + 16 * j));
+        const uint32_t* s = scales + (kb & 1) * S::kThreads;
+        if constexpr (WAY == kExponents) {
+            sb[j][0] = s[row_b + 16 * j];
+        } else if constexpr (B_ROWS == 1) {
+            const uint4 v = *reinterpret_cast<const uint4*>(s + S::BM + wn * 64 + 16 * j + 4 * g);
+            sb[j][0] = v.x, sb[j][1] = v.y, sb[j][2] = v.z, sb[j][3] = v.w;
+        } else if (j == 0) {
+            sb[0][0] = s[S::BM + wn * 64];
+        }
+    };
+    read_a(0, 0, 0);
+    read_a(1, 0, 1);
 #pragma unroll
-    for (int j = 0; j < NT; j++) b[j] = hold(piece(0, row_b + 16 * j));
+    for (int j = 0; j < NT; j++) read_b(0, j);
     v4f d[NT] = {};
     float f[NT][4] = {};
 
     for (int64_t kb = 0; kb < p.blocks; kb++) {
-        const uint32_t* s = scales + (kb & 1) * (S::BM + S::BN);
-        uint32_t sb[NT][4];
-        if constexpr (WAY == kExponents) {
-#pragma unroll
-            for (int j = 0; j < NT; j++) sb[j][0] = s[row_b + 16 * j];
-        } else if constexpr (B_ROWS == 1) {
-#pragma unroll
-            for (int j = 0; j < NT; j++)
-#pragma unroll
-                for (int r = 0; r < 4; r++) sb[j][r] = s[S::BM + wn * 64 + 16 * j + 4 * g + r];
-        } else {
-            sb[0][0] = s[S::BM + wn * 64];
-        }
 #pragma unroll
         for (int i = 0; i < MT; i++) {
-            const uint32_t sa = s[row_a + 16 * i];
-            if (i == MT - 1) {
-                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the last tile of a is in registers
+            if (i == MT - 2) {
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the last tiles of a are in registers
                 wait_loads<0>();                                    // the next step's operands (this wavefront's) are in LDS
-                if (kb + 1 < p.blocks) put_scale(kb + 1);
+                put_scale(kb + 1);
                 __syncthreads();
-                if (kb + 2 < p.blocks) {
-                    fetch_scale(kb + 2);
-                    fetch(kb + 2);
-                }
+                fetch_scale(kb + 2 < last ? kb + 2 : last);
             }
+            if (i >= MT - 2) fetch(kb + 2 < last ? kb + 2 : last, (uint32_t)kb & 1, i - (MT - 2));
+            if (i < 2) fetch(kb + 1 < last ? kb + 1 : last, (uint32_t)(kb + 1) & 1, i + 2);
             // (past the last step: what LDS holds, not used)
-            const v8i next = i == MT - 1 ? piece(kb + 1, row_a) : piece(kb, row_a + 16 * (i + 1));
+            if (i < MT - 2) read_a(2, kb, i + 2);
+            else read_a(2, kb + 1, i + 2 - MT);
             if constexpr (WAY == kExponents) {
 #pragma unroll
                 for (int j = 0; j < NT; j++) {
-                    acc[i][j] = mfma_block_scaled<FORMAT>(b[j], a, acc[i][j], (int)sb[j][0], (int)sa);
-                    if (i == MT - 1) b[j] = piece(kb + 1, row_b + 16 * j);
+                    acc[i][j] = mfma_block_scaled<FORMAT>(b[j], a[0], acc[i][j], (int)sb[j][0], (int)sa[0]);
+                    if (i == MT - 1) read_b(kb + 1, j);
                 }
             } else {
                 v4f* const before = acc[i ? i - 1 : MT - 1];
-                const auto held = [&] { if constexpr (WAY == kWide) return widen<FORMAT>(a); else return a; }();
+                const auto held = [&] { if constexpr (WAY == kWide) return widen<FORMAT>(a[0]); else return a[0]; }();
 #pragma unroll
                 for (int j = 0; j < NT; j++) {
                     v4f now;
@@ -329,15 +332,24 @@ __global__ __launch_bounds__(S::kThreads) void k_f8_matmul_tiles(Product p, uint
 #pragma unroll
                     for (int r = 0; r < 4; r++) {
                         before[j][r] = fmaf(d[j][r], f[B_ROWS == 1 ? j : 0][B_ROWS == 1 ? r : 0], before[j][r]);
-                        if constexpr (B_ROWS == 1) f[j][r] = __uint_as_float(sa) * __uint_as_float(sb[j][r]);
+                        if constexpr (B_ROWS == 1) f[j][r] = __uint_as_float(sa[0]) * __uint_as_float(sb[j][r]);
                     }
-                    asm volatile("" : "+v"(before[j]));  // here, and not all of a step's at its end
                     d[j] = now;
-                    if (i == MT - 1) b[j] = hold(piece(kb + 1, row_b + 16 * j));
                 }
-                if constexpr (B_ROWS != 1) f[0][0] = __uint_as_float(sa) * __uint_as_float(sb[0][0]);
+                if constexpr (B_ROWS != 1) f[0][0] = __uint_as_float(sa[0]) * __uint_as_float(sb[0][0]);
+                if (i == MT - 1)
+#pragma unroll
+                    for (int j = 0; j < NT; j++) read_b(kb + 1, j);
             }
-            a = next;
+            a[0] = a[1], a[1] = a[2], sa[0] = sa[1], sa[1] = sa[2];
+            if constexpr (WAY == kScaled) {
+#pragma unroll
+                for (int j = 0; j < NT; j++) {  // the sums of the tile before it between this one's products
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
+                }
+            }
             __builtin_amdgcn_sched_barrier(0);
         }
     }
@@ -348,6 +360,7 @@ __global__ __launch_bounds__(S::kThreads) void k_f8_matmul_tiles(Product p, uint
             for (int r = 0; r < 4; r++) acc[MT - 1][j][r] = fmaf(d[j][r], f[B_ROWS == 1 ? j : 0][B_ROWS == 1 ? r : 0], acc[MT - 1][j][r]);
     }
     // 4 tiles of a at a time: 64 rows of 64 columns in the wavefront's own part of LDS, then whole rows to memory
+    wait_loads<0>();
     __syncthreads();
     float* const out = reinterpret_cast<float*>(lds) + wave * S::kOutRows * S::kPitch;
     const int64_t n = n0 + wn * 64 + 4 * i16;
