@@ -198,7 +198,9 @@ __device__ __forceinline__ int row_key(int row) { return (row >> 1) & 7; }
 
 // 16 bytes a lane from base + off straight into LDS, lane l to lds_base + 16 l (the caller counts its loads in flight)
 __device__ __forceinline__ void load_to_lds16(const uint8_t* base, uint32_t off, uint32_t lds_base) {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(base), "s"(lds_base) : "memory", "m0");
+    uint32_t keep;
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b32 m0, %0"
+                 : "=&s"(keep) : "v"(off), "s"(base), "s"(lds_base) : "memory");
 }
 
 template <int FORMAT, int WAY, int B_ROWS, class S>
@@ -227,7 +229,9 @@ __global__ __launch_bounds__(S::kThreads) void k_f8_matmul_tiles(Product p, uint
         off[i] = (uint32_t)r * (uint32_t)(of_a ? p.ld_a : p.ld_b) + 16 * ((lane & 7) ^ row_key(row));
     }
     const uint32_t lds_at = (uint32_t)(uintptr_t)(lds_void_t*)lds;
-    // a quarter of a step's loads (all at once, the queue of loads is full and the wavefront stands still)
+    // A quarter of a step's loads: all at once, the queue of loads is full and the wavefront stands still.  (f16: the products
+    // take twice as long and come less dense, the loads are best out of the way: 1112 us in quarters, 1038 us, 8192^3.)
+    constexpr bool kQuarters = WAY != kWide;
     auto fetch = [&](int64_t kb, uint32_t stage, int quarter) {
         const uint32_t to = lds_at + stage * S::kStage + wave * S::kLoads * 1024;
 #pragma unroll
@@ -266,8 +270,8 @@ __global__ __launch_bounds__(S::kThreads) void k_f8_matmul_tiles(Product p, uint
     put_scale(0);
     __syncthreads();
     fetch_scale(last < 1 ? last : 1);
-    fetch(last < 1 ? last : 1, 1, 0);
-    fetch(last < 1 ? last : 1, 1, 1);
+#pragma unroll
+    for (int q = 0; q < (kQuarters ? 2 : 4); q++) fetch(last < 1 ? last : 1, 1, q);
     // b's tiles as the way takes them; the products of a tile of a, added to the sums while the next one is multiplied
     using Held = typename std::conditional<WAY == kWide, Wide, v8i>::type;
     auto hold = [&](v8i raw) {
@@ -310,8 +314,11 @@ __global__ __launch_bounds__(S::kThreads) void k_f8_matmul_tiles(Product p, uint
                 __syncthreads();
                 fetch_scale(kb + 2 < last ? kb + 2 : last);
             }
-            if (i >= MT - 2) fetch(kb + 2 < last ? kb + 2 : last, (uint32_t)kb & 1, i - (MT - 2));
-            if (i < 2) fetch(kb + 1 < last ? kb + 1 : last, (uint32_t)(kb + 1) & 1, i + 2);
+            if (i == MT - 2 || (kQuarters && i == MT - 1)) {
+#pragma unroll
+                for (int q = i - (MT - 2); q < (kQuarters ? i - (MT - 2) + 1 : 4); q++) fetch(kb + 2 < last ? kb + 2 : last, (uint32_t)kb & 1, q);
+            }
+            if (kQuarters && i < 2) fetch(kb + 1 < last ? kb + 1 : last, (uint32_t)(kb + 1) & 1, i + 2);
             // (past the last step: what LDS holds, not used)
             if (i < MT - 2) read_a(2, kb, i + 2);
             else read_a(2, kb + 1, i + 2 - MT);
@@ -334,6 +341,7 @@ __global__ __launch_bounds__(S::kThreads) void k_f8_matmul_tiles(Product p, uint
                         before[j][r] = fmaf(d[j][r], f[B_ROWS == 1 ? j : 0][B_ROWS == 1 ? r : 0], before[j][r]);
                         if constexpr (B_ROWS == 1) f[j][r] = __uint_as_float(sa[0]) * __uint_as_float(sb[j][r]);
                     }
+                    if constexpr (WAY == kWide) asm volatile("" : "+v"(before[j]));  // (else the scheduler gathers the sums)
                     d[j] = now;
                 }
                 if constexpr (B_ROWS != 1) f[0][0] = __uint_as_float(sa[0]) * __uint_as_float(sb[0][0]);
