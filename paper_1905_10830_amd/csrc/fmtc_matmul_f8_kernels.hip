@@ -116,6 +116,8 @@ struct Product {
     const float* bias;
     void* out;
     int out_type, accumulate, scale;
+    int64_t split_blocks;  // tiles: blocks of the depth that a workgroup takes; the sums of split z go to out + z * split_out
+    int64_t split_out;     // floats
 };
 
 // Few rows: 16 MT rows x 16 columns per workgroup, operands straight from memory to registers; the workgroup's wavefronts
@@ -212,14 +214,16 @@ __global__ __launch_bounds__(S::kThreads) void k_f8_matmul_tiles(Product p, uint
 
     // Workgroups go to the 8 XCDs in turn: each XCD gets a range of tiles, and within it four rows of tiles at a time, so
     // that the tiles that run on it together share operands in its cache.
-    const uint32_t total = tiles_m * tiles_n, each = total / 8, more = total % 8, xcd = blockIdx.x % 8;
-    const uint32_t id = xcd * each + (xcd < more ? xcd : more) + blockIdx.x / 8;
+    const uint32_t total = gridDim.x, each = total / 8, more = total % 8, xcd = blockIdx.x % 8;
+    const uint32_t place = xcd * each + (xcd < more ? xcd : more) + blockIdx.x / 8;
+    const uint32_t z = place / (tiles_m * tiles_n), id = place - z * (tiles_m * tiles_n);
     const uint32_t span = 4 * tiles_n, first = id / span * 4, in = id % span, deep = tiles_m - first < 4 ? tiles_m - first : 4;
     const int64_t m0 = (int64_t)(first + in % deep) * S::BM, n0 = (int64_t)(in / deep) * S::BN;
     const int rows_a = p.M - m0 < S::BM ? (int)(p.M - m0) : S::BM, rows_b = p.N - n0 < S::BN ? (int)(p.N - n0) : S::BN;
 
     // what this lane moves: 16 bytes of kLoads rows (rows that do not exist: the last one, whose results are not stored)
-    const uint8_t *from_a = p.a + m0 * p.ld_a, *from_b = p.b + n0 * p.ld_b;
+    const int64_t kb0 = z * p.split_blocks, blocks = p.blocks - kb0 < p.split_blocks ? p.blocks - kb0 : p.split_blocks;
+    const uint8_t *from_a = p.a + m0 * p.ld_a + kb0 * kF8Block, *from_b = p.b + n0 * p.ld_b + kb0 * kF8Block;
     uint32_t off[S::kLoads];
 #pragma unroll
     for (int i = 0; i < S::kLoads; i++) {
@@ -242,7 +246,7 @@ __global__ __launch_bounds__(S::kThreads) void k_f8_matmul_tiles(Product p, uint
     uint32_t* const scales = reinterpret_cast<uint32_t*>(lds + 2 * S::kStage);
     const bool scale_of_a = wave * 64 < S::BM;
     const void* const from_s = scale_of_a ? p.sa : p.sb;
-    const int64_t first_s = scale_of_a ? m0 : n0 / B_ROWS, step_s = scale_of_a ? p.ld_sa : p.ld_sb;
+    const int64_t step_s = scale_of_a ? p.ld_sa : p.ld_sb, first_s = (scale_of_a ? m0 : n0 / B_ROWS) + kb0 * step_s;
     uint32_t off_s, mine = 0;
     if (scale_of_a) off_s = t < rows_a ? t : rows_a - 1;
     else off_s = (t - S::BM < rows_b ? t - S::BM : rows_b - 1) / B_ROWS;
@@ -262,7 +266,7 @@ __global__ __launch_bounds__(S::kThreads) void k_f8_matmul_tiles(Product p, uint
 
     v4f acc[MT][NT] = {};
     // (past the last block: that one again, into the place that is free; not used, and no branch in the loop)
-    const int64_t last = p.blocks - 1;
+    const int64_t last = blocks - 1;
 #pragma unroll
     for (int q = 0; q < 4; q++) fetch(0, 0, q);
     fetch_scale(0);
@@ -304,7 +308,7 @@ __global__ __launch_bounds__(S::kThreads) void k_f8_matmul_tiles(Product p, uint
     v4f d[NT] = {};
     float f[NT][4] = {};
 
-    for (int64_t kb = 0; kb < p.blocks; kb++) {
+    for (int64_t kb = 0; kb < blocks; kb++) {
 #pragma unroll
         for (int i = 0; i < MT; i++) {
             if (i == MT - 2) {
@@ -372,6 +376,7 @@ __global__ __launch_bounds__(S::kThreads) void k_f8_matmul_tiles(Product p, uint
     __syncthreads();
     float* const out = reinterpret_cast<float*>(lds) + wave * S::kOutRows * S::kPitch;
     const int64_t n = n0 + wn * 64 + 4 * i16;
+    void* const to = p.split_out ? static_cast<float*>(p.out) + z * p.split_out : p.out;
 #pragma unroll
     for (int i0 = 0; i0 < MT; i0 += 4) {
 #pragma unroll
@@ -383,10 +388,19 @@ __global__ __launch_bounds__(S::kThreads) void k_f8_matmul_tiles(Product p, uint
         for (int r = g; r < 64; r += 4) {
             const int64_t m = m0 + wm * MT * 16 + i0 * 16 + r;
             const v4f v = *reinterpret_cast<const v4f*>(out + r * S::kPitch + 4 * i16);
-            if (m < p.M && n < p.N) store_out(p.out, p.out_type, p.ld_out, m, n, p.N, v, p.bias, p.accumulate);
+            if (m < p.M && n < p.N) store_out(to, p.out_type, p.ld_out, m, n, p.N, v, p.bias, p.accumulate);
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
+}
+
+// out = sum over the splits in order, and what store_out does: four columns of a row a thread
+__global__ __launch_bounds__(256) void k_f8_join(Product p, const float* __restrict__ part, int64_t ld, int splits, uint32_t quads) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, m = i / quads, n = (i - m * quads) * 4;
+    if (m >= p.M) return;
+    v4f v = *reinterpret_cast<const v4f*>(part + m * ld + n);
+    for (int z = 1; z < splits; z++) v += *reinterpret_cast<const v4f*>(part + z * p.split_out + m * ld + n);
+    store_out(p.out, p.out_type, p.ld_out, m, n, p.N, v, p.bias, p.accumulate);
 }
 
 template <class F>
@@ -396,16 +410,76 @@ hipError_t with_way(int way, F&& f) {
 
 }  // namespace
 
-size_t matmul_f8_workspace(int64_t, int64_t, int64_t) { return 0; }
+namespace {
+
+// Which kernel, and in how many parts of the depth: the least of the times that a product of these sizes is expected to
+// take, in us, from what each kernel takes to start and end and for a block of the depth, alone on a compute unit and with
+// all of them busy.  The numbers are fits to measured times over 17 to 4096 rows, 512 to 8192 columns and a depth of 512 to
+// 8192 (with f32 scales): 128 x 4096 x 4096 rows 22.7, tiles of 128 30.4, in 4 parts 21.6; 1024 x 1024 x 4096 40.7, 30.6, 25.9
+// in 4 parts; 4096 x 1024 x 1024 45.2, 14.3, tiles of 256 21.6; 4096^3 -, 87.8, 63.9; 512 x 8192 x 8192 -, 66.6, 85.1, and
+// 52.9 in 4 parts of tiles of 256.  Up to 16 rows the wavefronts of the first kernel waste nothing: always that one.
+struct Plan { int kernel, splits; int64_t split_blocks; };
+enum { kRows = 0, kTiles128 = 1, kTiles256 = 2 };
+constexpr double kCus = 256;
+
+Plan make_plan(int64_t M, int64_t N, int64_t K, bool wide) {
+    const int64_t blocks = (K + kF8Block - 1) / kF8Block;
+    Plan best{kRows, 1, blocks};
+    if (M <= 16) return best;
+    const double row_groups = (double)((M + 63) / 64) * ((N + 15) / 16);
+    double least = 2.5 + 2.3 * ((blocks + kRowsWaves - 1) / kRowsWaves) * fmax(1.0, row_groups / kCus);
+    for (int kernel = kTiles128; kernel <= (M > 128 && N > 128 ? kTiles256 : kTiles128); kernel++)
+        for (int64_t want = 1; want <= 16 && want <= blocks; want *= 2) {
+            const int64_t bm = kernel == kTiles256 && !wide ? 256 : 128, bn = kernel == kTiles256 ? 256 : 128;
+            const int64_t per = (blocks + want - 1) / want, splits = (blocks + per - 1) / per;
+            const double groups = (double)((M + bm - 1) / bm) * ((N + bn - 1) / bn) * splits;
+            const double busy = fmin(1.0, groups / kCus), rounds = ceil(groups / kCus);
+            double start, step;
+            if (kernel == kTiles128) start = wide ? 8.0 : 6.5, step = wide ? 1.22 : 0.74 + 0.16 * busy;
+            else start = wide ? 9.0 : 11.0, step = wide ? 1.68 + 0.35 * busy : 1.14 + 0.5 * busy;
+            double t = start + step * per * rounds;
+            if (splits > 1) t += 4.0 + 1e-6 * splits * M * N;  // the parts' sums written and read, 8 bytes at 8 TB/s
+            if (t < least) {
+                least = t;
+                best = {kernel, (int)splits, per};
+            }
+        }
+    return best;
+}
+
+int64_t split_ld(int64_t N) { return (N + 3) / 4 * 4; }
+
+}  // namespace
+
+size_t matmul_f8_workspace(int64_t M, int64_t N, int64_t K) {
+    size_t most = 0;
+    for (int wide = 0; wide < 2; wide++) {
+        const Plan plan = make_plan(M, N, K, wide);
+        const size_t bytes = plan.splits > 1 ? align_up(sizeof(float) * (size_t)plan.splits * M * split_ld(N), 256) : 0;
+        if (bytes > most) most = bytes;
+    }
+    return most;
+}
 
 hipError_t launch_f8_matmul(const fmtc_f8& a, const fmtc_f8& b, const float* d_bias, void* d_out, int out_type,
-                            int64_t ld_out, int accumulate, void*, hipStream_t s) {
+                            int64_t ld_out, int accumulate, void* d_ws, hipStream_t s) {
     Product p{static_cast<const uint8_t*>(a.d_codes), static_cast<const uint8_t*>(b.d_codes), a.d_scales, b.d_scales,
               a.rows, b.rows, (a.depth + kF8Block - 1) / kF8Block, a.ld, b.ld, a.ld_scales, b.ld_scales, ld_out,
-              d_bias, d_out, out_type, accumulate, a.scale};
-    const int64_t n_tiles = (p.N + 15) / 16;
+              d_bias, d_out, out_type, accumulate, a.scale, 0, 0};
     const int way = out_type == FMTC_F32 ? kWide : a.scale == FMTC_SCALE_E8M0 ? kExponents : kScaled;
-    return with_bit(a.format, [&](auto fm) {
+    Plan plan = make_plan(p.M, p.N, a.depth, way == kWide);
+    if (p.ld_a >= (1 << 23) || p.ld_b >= (1 << 23)) plan = {kRows, 1, p.blocks};  // (a tile's offsets are 32 bits)
+    p.split_blocks = plan.split_blocks;
+    Product inner = p;
+    if (plan.splits > 1) {
+        inner.out = d_ws;
+        inner.ld_out = split_ld(p.N);
+        inner.split_out = p.split_out = p.M * inner.ld_out;
+        inner.out_type = FMTC_F32;
+        inner.bias = nullptr;
+        inner.accumulate = 0;
+    }
+    hipError_t e = with_bit(a.format, [&](auto fm) {
         return with_way(way, [&](auto wy) {
             return with_bit(b.block_rows == 1, [&](auto one) {
                 constexpr int F = decltype(fm)::value, W = decltype(wy)::value, B = decltype(one)::value ? 1 : kF8Block;
@@ -414,9 +488,11 @@ hipError_t launch_f8_matmul(const fmtc_f8& a, const fmtc_f8& b, const float* d_b
                     const int64_t tm = (p.M + S::BM - 1) / S::BM, tn = (p.N + S::BN - 1) / S::BN;
                     auto kernel = k_f8_matmul_tiles<F, W, B, S>;
                     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds);
-                    return e != hipSuccess ? e : launch(K_F8_MATMUL, kernel, dim3((unsigned)(tm * tn)), dim3(S::kThreads), S::kLds, s, p, (uint32_t)tm, (uint32_t)tn);
+                    return e != hipSuccess ? e : launch(K_F8_MATMUL, kernel, dim3((unsigned)(tm * tn * plan.splits)), dim3(S::kThreads), S::kLds, s, inner, (uint32_t)tm, (uint32_t)tn);
                 };
-                if (p.M > 256 && p.N > 256 && p.ld_a < (1 << 23) && p.ld_b < (1 << 23)) return tiles(Tile<2, 4, W == kWide ? 4 : 8>{});
+                if (plan.kernel == kTiles256) return tiles(Tile<2, 4, W == kWide ? 4 : 8>{});
+                if (plan.kernel == kTiles128) return tiles(Tile<2, 2, 4>{});
+                const int64_t n_tiles = (p.N + 15) / 16;
                 if (p.M <= 16)
                     return launch(K_F8_MATMUL, k_f8_matmul_rows<F, W, B, 1>, dim3((unsigned)n_tiles), dim3(64 * kRowsWaves), 0, s, p,
                                   (uint32_t)n_tiles);
@@ -425,6 +501,10 @@ hipError_t launch_f8_matmul(const fmtc_f8& a, const fmtc_f8& b, const float* d_b
             });
         });
     });
+    if (e != hipSuccess || plan.splits == 1) return e;
+    const int64_t quads = (p.N + 3) / 4;
+    return launch(K_F8_MATMUL, k_f8_join, dim3((unsigned)((p.M * quads + 255) / 256)), dim3(256), 0, s, p, static_cast<const float*>(d_ws),
+                  inner.ld_out, plan.splits, (uint32_t)quads);
 }
 
 }  // namespace fmtc
