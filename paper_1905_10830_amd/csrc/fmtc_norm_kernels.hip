@@ -7,30 +7,70 @@
 //              the rows that share a gate row
 // Memory bound: 3 arrays read and 1 or 2 written (forward), 4 read and 2 written (backward), each once.  TPR lanes hold a
 // row in registers, VPT groups of 8 consecutive values each; group g of a lane starts at column 8 (g TPR + lane), so that
-// 16 lanes hold a block of 128.
+// 16 lanes hold a block of 128.  A workgroup walks several rows: the weights stay in registers, and the next row's loads are
+// on their way while a row is worked on.
 #include "fmtc_block.h"
 
 namespace fmtc {
 
 namespace {
 
-template <int TPR>
-struct RowSum {  // f32 sum over the TPR lanes of a row, in a fixed order
-    static constexpr int kSlots = TPR > 64 ? TPR / 64 : 1;
-    __device__ static float run(float v, float (*slot)[kSlots]) {
-        v = row16_sum(v);
-        if constexpr (TPR >= 64) {
-            v += __shfl_xor(v, 16, 64);
-            v += __shfl_xor(v, 32, 64);
+// f32 sums over the TPR lanes of a row, in a fixed order, through one of two slots in turn: a wavefront that writes a slot
+// again has passed the other one's barrier, before which every wavefront had read this one.
+template <int TPR, int N>
+struct RowSums {
+    static constexpr int kWaves = TPR > 64 ? TPR / 64 : 1;
+    struct Slot { float v[N][kWaves]; };
+    __device__ static void run(float (&v)[N], Slot* slots, int& turn) {
+        Slot& slot = slots[turn];
+        turn ^= 1;
+#pragma unroll
+        for (int k = 0; k < N; k++) {
+            v[k] = row16_sum(v[k]);
+            if constexpr (TPR >= 64) {
+                v[k] += __shfl_xor(v[k], 16, 64);
+                v[k] += __shfl_xor(v[k], 32, 64);
+            }
         }
         if constexpr (TPR > 64) {
-            if ((threadIdx.x & 63) == 0) (*slot)[threadIdx.x >> 6] = v;
-            __syncthreads();
-            v = 0.f;
+            const int wave = threadIdx.x % TPR >> 6;
+            if ((threadIdx.x & 63) == 0)
 #pragma unroll
-            for (int i = 0; i < kSlots; i++) v += (*slot)[i];
+                for (int k = 0; k < N; k++) slot.v[k][wave] = v[k];
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < N; k++) {  // 16 lanes read the wavefronts' sums and add them up as above
+                const int i = threadIdx.x & 15;
+                v[k] = row16_sum(kWaves == 16 || i < kWaves ? slot.v[k][i % kWaves] : 0.f);
+            }
         }
-        return v;
+    }
+};
+
+// 8 values as they lie in memory, of which the first n exist, in whole registers
+template <class T>
+struct Raw {
+    static constexpr int kWords = 2 * sizeof(T), kPer = 4 / sizeof(T);
+    uint32_t w[kWords];
+    __device__ __forceinline__ void load(const T* p, int n) {
+        if (n >= 8) {
+            __builtin_memcpy(w, p, sizeof w);
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < kWords; i++) {
+            w[i] = 0;
+#pragma unroll
+            for (int j = 0; j < kPer; j++)
+                if (i * kPer + j < n) {
+                    if constexpr (kPer == 2) w[i] |= (uint32_t)__builtin_bit_cast(uint16_t, p[i * kPer + j]) << (16 * j);
+                    else w[i] = __builtin_bit_cast(uint32_t, p[i]);
+                }
+        }
+    }
+    __device__ __forceinline__ float operator[](int i) const {
+        if constexpr (kPer == 1) return __uint_as_float(w[i]);
+        else return to_f32(__builtin_bit_cast(T, (uint16_t)(w[i >> 1] >> (16 * (i & 1)))));
     }
 };
 
@@ -55,6 +95,13 @@ struct NormOut {
     float* stats;
 };
 
+// which of a workgroup's rows a thread belongs to: one for all of a wavefront from 64 lanes on, so that addresses are scalar
+template <int TPR>
+__device__ __forceinline__ int row_in_group() {
+    const int r = threadIdx.x / TPR;
+    return TPR >= 64 ? __builtin_amdgcn_readfirstlane(r) : r;
+}
+
 constexpr int norm_threads(int TPR) { return TPR < 256 ? 256 : TPR; }
 
 template <int FORMAT, int SCALE>
@@ -73,21 +120,46 @@ __device__ __forceinline__ void store_codes(const fmtc_f8& q, int64_t row, int c
 
 template <class T, class W, int TPR, int VPT>
 __global__ __launch_bounds__(norm_threads(TPR)) void k_block_norm(fmtc_norm p, NormOut out) {
-    __shared__ float slots[2][RowSum<TPR>::kSlots];
     constexpr int kRows = norm_threads(TPR) / TPR;
+    using Sum = RowSums<TPR, 1>;
+    __shared__ typename Sum::Slot slots[kRows][2];
     const int lane = threadIdx.x % TPR, C = p.C;
+    const int mine = row_in_group<TPR>();
+    typename Sum::Slot* const slot = slots[mine];
+    int turn = 0;
     const float rC = 1.f / (float)C;
     float w_pre[VPT][8], gate[VPT][8];
     int64_t gate_row = -1;
     if (p.d_w_pre) load_params<W, TPR, VPT>(p.d_w_pre, 0, C, lane, w_pre);
-    for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR; row < p.rows; row += (int64_t)gridDim.x * kRows) {
-        float h[VPT][8], y[VPT][8];
+    Raw<T> next_h[VPT], next_y[VPT];
+    auto fetch = [&](int64_t row) {
 #pragma unroll
         for (int g = 0; g < VPT; g++) {
             const int c = 8 * (g * TPR + lane);
-            load8(at<T>(p.d_h, row * p.ld_h + c), C - c, h[g]);
-            if (p.d_y) load8(at<T>(p.d_y, row * p.ld_y + c), C - c, y[g]);
+            next_h[g].load(at<T>(p.d_h, row * p.ld_h + c), C - c);
+            if (p.d_y) next_y[g].load(at<T>(p.d_y, row * p.ld_y + c), C - c);
         }
+    };
+    // (the rows of a workgroup walk together: in a pass past the end a row's lanes work on the last row and store nothing)
+    const int64_t step = (int64_t)gridDim.x * kRows;
+    int64_t first = (int64_t)blockIdx.x * kRows;
+    auto row_of = [&](int64_t f) {
+        const int64_t row = f + mine;
+        return row < p.rows ? row : p.rows - 1;
+    };
+    fetch(row_of(first));
+    for (; first < p.rows; first += step) {
+        const int64_t row = row_of(first);
+        const bool live = first + mine < p.rows;
+        float h[VPT][8], y[VPT][8];
+#pragma unroll
+        for (int g = 0; g < VPT; g++)
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                h[g][i] = next_h[g][i];
+                y[g][i] = p.d_y ? next_y[g][i] : 0.f;
+            }
+        if (first + step < p.rows) fetch(row_of(first + step));
         float r_y = 1.f;
         if (p.d_y) {
             const int64_t want = p.d_gate ? row / p.rows_per_gate : 0;
@@ -103,12 +175,13 @@ __global__ __launch_bounds__(norm_threads(TPR)) void k_block_norm(fmtc_norm p, N
                         gate[g][i] = p.scale * (p.d_gate ? gate[g][i] : 1.f) * (p.d_w_post ? w[g][i] : 1.f);
             }
             if (p.d_w_post) {
-                float sum = 0.f;
+                float sum[1] = {0.f};
 #pragma unroll
                 for (int g = 0; g < VPT; g++)
 #pragma unroll
-                    for (int i = 0; i < 8; i++) sum = fmaf(y[g][i], y[g][i], sum);
-                r_y = 1.f / sqrtf(RowSum<TPR>::run(sum, &slots[0]) * rC + p.eps);
+                    for (int i = 0; i < 8; i++) sum[0] = fmaf(y[g][i], y[g][i], sum[0]);
+                Sum::run(sum, slot, turn);
+                r_y = 1.f / sqrtf(sum[0] * rC + p.eps);
             }
 #pragma unroll
             for (int g = 0; g < VPT; g++)
@@ -120,7 +193,7 @@ __global__ __launch_bounds__(norm_threads(TPR)) void k_block_norm(fmtc_norm p, N
 #pragma unroll
                 for (int i = 0; i < 8; i++) h[g][i] *= p.skip;
         }
-        if (out.h)
+        if (out.h && live)
 #pragma unroll
             for (int g = 0; g < VPT; g++) {
                 const int c = 8 * (g * TPR + lane);
@@ -128,17 +201,19 @@ __global__ __launch_bounds__(norm_threads(TPR)) void k_block_norm(fmtc_norm p, N
             }
         float r_h = 1.f;
         if (p.d_w_pre) {
-            float sum = 0.f;
+            float sum[1] = {0.f};
 #pragma unroll
             for (int g = 0; g < VPT; g++)
 #pragma unroll
-                for (int i = 0; i < 8; i++) sum = fmaf(h[g][i], h[g][i], sum);
-            r_h = 1.f / sqrtf(RowSum<TPR>::run(sum, &slots[1]) * rC + p.eps);
+                for (int i = 0; i < 8; i++) sum[0] = fmaf(h[g][i], h[g][i], sum[0]);
+            Sum::run(sum, slot, turn);
+            r_h = 1.f / sqrtf(sum[0] * rC + p.eps);
 #pragma unroll
             for (int g = 0; g < VPT; g++) {
                 const int c = 8 * (g * TPR + lane);
 #pragma unroll
                 for (int i = 0; i < 8; i++) h[g][i] = h[g][i] * r_h * w_pre[g][i];
+                if (!live) continue;
                 if (out.n) store8(at<T>(out.n, row * out.ld_n + c), C - c, h[g]);
                 if (out.codes.d_codes) {
                     if (out.codes.format == FMTC_E4M3) {
@@ -151,7 +226,7 @@ __global__ __launch_bounds__(norm_threads(TPR)) void k_block_norm(fmtc_norm p, N
                 }
             }
         }
-        if (out.stats && lane == 0) {
+        if (out.stats && live && lane == 0) {
             out.stats[row] = r_y;
             out.stats[p.rows + row] = r_h;
         }
@@ -159,9 +234,10 @@ __global__ __launch_bounds__(norm_threads(TPR)) void k_block_norm(fmtc_norm p, N
 }
 
 // ---- backward ----
-// Rows are cut into strips; TPR lanes walk a strip and keep the sums over its rows in registers.  Where a gate row serves at
-// least a strip's number of rows, its rows are cut into `per_gate` strips of their own and the strips' sums are added up
-// by k_strip_sums; where it serves fewer, a strip holds whole gate rows and writes their gradients itself.
+// Rows are cut into strips; TPR lanes walk a strip and keep the sums over its rows in registers, and a workgroup adds up
+// those of its strips.  Where a gate row serves more rows than a strip has, its rows are cut into `per_gate` strips of their
+// own, whose sums for the gate are added up afterwards; where it serves fewer, a strip holds whole gate rows and writes
+// their gradients itself.
 struct Strips {
     int64_t count, rows;   // strips; rows of each (the last of a gate row may have fewer)
     int64_t per_gate;      // strips of a gate row, 0: a strip holds whole gate rows (or there is no gate)
@@ -169,13 +245,17 @@ struct Strips {
 };
 __host__ __device__ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// Lanes of a row by its width, one group of 8 values each up to 8192: a row in as few lanes as hold it, whole wavefronts from
+// 129 values on.
+constexpr int lanes_of(int C) { return C <= 128 ? 16 : C <= 512 ? 64 : C <= 1024 ? 128 : C <= 2048 ? 256 : C <= 4096 ? 512 : 1024; }
+
 Strips make_strips(int64_t rows, int C, int64_t rows_per_gate) {
-    // 1024 strips of wide rows, more of narrow ones (which have fewer lanes each): enough to fill the device, while the
-    // strips' sums stay a small part of the traffic
-    const int64_t want = C > 512 ? 1024 : C > 128 ? 4096 : 8192;
-    Strips s{};
+    // as many strips as 256 compute units walk at a time with 16 wavefronts each, of at least 4 rows: the strips' sums stay a
+    // small part of the traffic
+    const int64_t want = 256 * 1024 / lanes_of(C);
     int64_t each = ceil_div(rows, want);
     if (each < 4) each = 4;
+    Strips s{};
     if (rows_per_gate <= 0) {
         s.rows = each;
         s.count = ceil_div(rows, each);
@@ -199,179 +279,229 @@ struct NormGrads {
     const void *dn, *dh;
     void *dy, *dh_in;
     int64_t ld_dn, ld_dh, ld_dy, ld_dh_in;
-    float *part_post, *part_pre, *part_gate;  // [strips][C] each (gate: where a gate row has several strips)
+    float *part_post, *part_pre;  // [workgroups][C]
+    float* part_gate;             // [strips][C], where a gate row has several strips
     float* dgate;
     Strips strips;
 };
 
 template <class T, class W, int TPR, int VPT>
-__global__ __launch_bounds__(norm_threads(TPR)) void k_block_norm_backward(fmtc_norm p, NormGrads q) {
-    __shared__ float slots[2][RowSum<TPR>::kSlots];
-    constexpr int kRows = norm_threads(TPR) / TPR;
+__global__ __launch_bounds__(norm_threads(TPR), 4) void k_block_norm_backward(fmtc_norm p, NormGrads q) {
+    constexpr int kThreads = norm_threads(TPR), kRows = kThreads / TPR;
+    constexpr bool kHold = VPT == 1;  // the weights stay in registers; else they come from the cache for every row
+    using Sum = RowSums<TPR, 3>;
+    __shared__ typename Sum::Slot slots[kRows][2];
+    __shared__ float joined[kRows > 1 ? kThreads * 8 : 1];
     const int lane = threadIdx.x % TPR, C = p.C;
+    const int mine = row_in_group<TPR>();
+    typename Sum::Slot* const slot = slots[mine];
+    int turn = 0;
     const float rC = 1.f / (float)C;
-    const int64_t strip = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR;
-    if (strip >= q.strips.count) return;  // (all lanes of a row)
-    int64_t row, end;
+    const int64_t strip = (int64_t)blockIdx.x * kRows + mine;
+    int64_t first, end;
     if (q.strips.per_gate) {
-        const int64_t g = strip / q.strips.per_gate, j = strip - g * q.strips.per_gate;
-        const int64_t last = (g + 1) * p.rows_per_gate;
-        row = g * p.rows_per_gate + j * q.strips.rows;
-        end = row + q.strips.rows < last ? row + q.strips.rows : last;
+        const int64_t g = strip / q.strips.per_gate, j = strip - g * q.strips.per_gate, last = (g + 1) * p.rows_per_gate;
+        first = g * p.rows_per_gate + j * q.strips.rows;
+        end = first + q.strips.rows < last ? first + q.strips.rows : last;
     } else {
-        row = strip * q.strips.rows;
-        end = row + q.strips.rows;
+        first = strip * q.strips.rows;
+        end = first + q.strips.rows;
     }
     if (end > p.rows) end = p.rows;
-    if (row >= end && q.dgate && q.strips.per_gate > 1)  // the last gate row has fewer rows than the others
-#pragma unroll
-        for (int g = 0; g < VPT; g++) {
-            const int c = 8 * (g * TPR + lane);
-            const float none[8] = {};
-            store8(q.part_gate + strip * C + c, C - c, none);
-        }
+    if (strip >= q.strips.count) end = first;  // (nothing; the workgroup's strips walk together)
 
-    float d_post[VPT][8] = {}, d_pre[VPT][8] = {}, z[VPT][8] = {}, w_post[VPT][8], w_pre[VPT][8], gate[VPT][8];
-    if (p.d_w_pre) load_params<W, TPR, VPT>(p.d_w_pre, 0, C, lane, w_pre);
-    if (p.d_w_post) load_params<W, TPR, VPT>(p.d_w_post, 0, C, lane, w_post);
-    else
+    float d_post[VPT][8] = {}, d_pre[VPT][8] = {}, z[VPT][8] = {}, w_pre[VPT][8], gain[VPT][8];
+    int64_t gate_row = 0;
+    auto load_gain = [&] {  // scale gate w_post
 #pragma unroll
         for (int g = 0; g < VPT; g++)
 #pragma unroll
-            for (int i = 0; i < 8; i++) w_post[g][i] = 1.f;
-#pragma unroll
-    for (int g = 0; g < VPT; g++)
-#pragma unroll
-        for (int i = 0; i < 8; i++) gate[g][i] = 1.f;
-    int64_t gate_row = -1;
-    for (; row < end; row++) {
+            for (int i = 0; i < 8; i++) gain[g][i] = p.scale;
+        float v[VPT][8];
         if (p.d_gate) {
-            const int64_t want = row / p.rows_per_gate;
-            if (want != gate_row) {
-                gate_row = want;
-                load_params<W, TPR, VPT>(p.d_gate, want, C, lane, gate);
-            }
+            load_params<W, TPR, VPT>(p.d_gate, gate_row, C, lane, v);
+#pragma unroll
+            for (int g = 0; g < VPT; g++)
+#pragma unroll
+                for (int i = 0; i < 8; i++) gain[g][i] *= v[g][i];
         }
-        const float r_y = p.d_y && p.d_w_post ? q.stats[row] : 1.f, r_h = q.stats[p.rows + row];
-        float t[VPT][8], hn[VPT][8], dn[VPT][8], y[VPT][8];
-        float sum = 0.f;
+        if (p.d_w_post) {
+            load_params<W, TPR, VPT>(p.d_w_post, 0, C, lane, v);
+#pragma unroll
+            for (int g = 0; g < VPT; g++)
+#pragma unroll
+                for (int i = 0; i < 8; i++) gain[g][i] *= v[g][i];
+        }
+    };
+    // what the rows that share a gate row added up in z: the gate's gradient, and their part of w_post's
+    auto flush = [&](float* to) {
 #pragma unroll
         for (int g = 0; g < VPT; g++) {
             const int c = 8 * (g * TPR + lane);
-            if (q.dh) load8(at<T>(q.dh, row * q.ld_dh + c), C - c, t[g]);
-            else
+            float gate[8], w_post[8];
 #pragma unroll
-                for (int i = 0; i < 8; i++) t[g][i] = 0.f;
-            if (p.d_y) load8(at<T>(p.d_y, row * p.ld_y + c), C - c, y[g]);
+            for (int i = 0; i < 8; i++) gate[i] = w_post[i] = 1.f;
+            if (p.d_gate) load8(at<W>(p.d_gate, gate_row * C + c), C - c, gate);
+            if (p.d_w_post) load8(at<W>(p.d_w_post, c), C - c, w_post);
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                d_post[g][i] = fmaf(gate[i], z[g][i], d_post[g][i]);
+                w_post[i] *= z[g][i];
+                z[g][i] = 0.f;
+            }
+            if (to) store8(to + c, C - c, w_post);
+        }
+    };
+    Raw<T> next_t[VPT], next_h[VPT], next_n[VPT], next_y[VPT];
+    float next_r_y = 1.f, next_r_h = 1.f;
+    auto fetch = [&](int64_t row) {
+#pragma unroll
+        for (int g = 0; g < VPT; g++) {
+            const int c = 8 * (g * TPR + lane);
+            if (q.dh) next_t[g].load(at<T>(q.dh, row * q.ld_dh + c), C - c);
             if (q.dn) {
-                load8(at<T>(p.d_h, row * p.ld_h + c), C - c, hn[g]);
-                load8(at<T>(q.dn, row * q.ld_dn + c), C - c, dn[g]);
+                next_h[g].load(at<T>(p.d_h, row * p.ld_h + c), C - c);
+                next_n[g].load(at<T>(q.dn, row * q.ld_dn + c), C - c);
             }
+            if (p.d_y) next_y[g].load(at<T>(p.d_y, row * p.ld_y + c), C - c);
         }
-        if (q.dn) {
-#pragma unroll
-            for (int g = 0; g < VPT; g++)
-#pragma unroll
-                for (int i = 0; i < 8; i++) {
-                    hn[g][i] *= r_h;
-                    d_pre[g][i] = fmaf(dn[g][i], hn[g][i], d_pre[g][i]);
-                    dn[g][i] *= w_pre[g][i];
-                    sum = fmaf(dn[g][i], hn[g][i], sum);
-                }
-            const float mean = RowSum<TPR>::run(sum, &slots[0]) * rC;
-#pragma unroll
-            for (int g = 0; g < VPT; g++)
-#pragma unroll
-                for (int i = 0; i < 8; i++) t[g][i] = fmaf(r_h, fmaf(-mean, hn[g][i], dn[g][i]), t[g][i]);
+        if (p.d_w_post) next_r_y = q.stats[row];
+        next_r_h = q.stats[p.rows + row];
+    };
+    if (first < end) fetch(first);
+    if (p.d_gate && first < end) gate_row = first / p.rows_per_gate;
+    if constexpr (kHold) {
+        if (p.d_w_pre) load_params<W, TPR, VPT>(p.d_w_pre, 0, C, lane, w_pre);
+        load_gain();
+    }
+    for (int64_t k = 0; k < q.strips.rows; k++) {
+        const int64_t row = first + k;
+        const bool live = row < end;
+        if (p.d_gate && live && row / p.rows_per_gate != gate_row) {
+            gate_row = row / p.rows_per_gate;
+            if constexpr (kHold) load_gain();
         }
-        if (q.dh_in) {
-#pragma unroll
-            for (int g = 0; g < VPT; g++) {
-                const int c = 8 * (g * TPR + lane);
-                float v[8];
-#pragma unroll
-                for (int i = 0; i < 8; i++) v[i] = p.skip * t[g][i];
-                store8(at<T>(q.dh_in, row * q.ld_dh_in + c), C - c, v);
-            }
+        if constexpr (!kHold) {
+            if (p.d_w_pre) load_params<W, TPR, VPT>(p.d_w_pre, 0, C, lane, w_pre);
+            load_gain();
         }
-        if (!p.d_y) continue;
-        sum = 0.f;
+        const float r_y = next_r_y, r_h = next_r_h;
+        float t[VPT][8], hn[VPT][8], y[VPT][8];  // (dh + r_h a, to become the whole gradient; h' and y normalised)
+        float sum[3] = {0.f, 0.f, 0.f};          // <a, hn>, <scale gate w_post yn, t>, <scale gate w_post yn, hn>
 #pragma unroll
         for (int g = 0; g < VPT; g++)
 #pragma unroll
             for (int i = 0; i < 8; i++) {
-                y[g][i] *= r_y;
-                const float st = p.scale * t[g][i];
-                z[g][i] = fmaf(st, y[g][i], z[g][i]);
-                t[g][i] = st * gate[g][i] * w_post[g][i];
-                sum = fmaf(t[g][i], y[g][i], sum);
-            }
-        if (p.d_w_post) {
-            const float mean = RowSum<TPR>::run(sum, &slots[1]) * rC;
-#pragma unroll
-            for (int g = 0; g < VPT; g++)
-#pragma unroll
-                for (int i = 0; i < 8; i++) t[g][i] = r_y * fmaf(-mean, y[g][i], t[g][i]);
-        }
-        if (q.dy)
-#pragma unroll
-            for (int g = 0; g < VPT; g++) {
-                const int c = 8 * (g * TPR + lane);
-                store8(at<T>(q.dy, row * q.ld_dy + c), C - c, t[g]);
-            }
-        if (row + 1 == end || (p.d_gate && !q.strips.per_gate && (row + 1) % p.rows_per_gate == 0)) {
-            float* to = q.dgate ? (q.strips.per_gate > 1 ? q.part_gate + strip * C : q.dgate + gate_row * C) : nullptr;
-#pragma unroll
-            for (int g = 0; g < VPT; g++) {
-                const int c = 8 * (g * TPR + lane);
-                float v[8];
-#pragma unroll
-                for (int i = 0; i < 8; i++) {
-                    d_post[g][i] = fmaf(gate[g][i], z[g][i], d_post[g][i]);
-                    v[i] = w_post[g][i] * z[g][i];
-                    z[g][i] = 0.f;
+                t[g][i] = q.dh && live ? next_t[g][i] : 0.f;
+                hn[g][i] = 0.f;
+                if (q.dn && live) {
+                    hn[g][i] = next_h[g][i] * r_h;
+                    const float dn = next_n[g][i], a = dn * w_pre[g][i];
+                    d_pre[g][i] = fmaf(dn, hn[g][i], d_pre[g][i]);
+                    sum[0] = fmaf(a, hn[g][i], sum[0]);
+                    t[g][i] = fmaf(r_h, a, t[g][i]);
                 }
-                if (to) store8(to + c, C - c, v);
+                y[g][i] = 0.f;
+                if (p.d_y && live) {
+                    y[g][i] = next_y[g][i] * r_y;
+                    const float c = gain[g][i] * y[g][i];
+                    sum[1] = fmaf(c, t[g][i], sum[1]);
+                    sum[2] = fmaf(c, hn[g][i], sum[2]);
+                }
+            }
+        if (row + 1 < end) fetch(row + 1);
+        Sum::run(sum, slot, turn);
+        const float mean_h = r_h * sum[0] * rC, mean_y = p.d_w_post ? (sum[1] - mean_h * sum[2]) * rC : 0.f;
+        if (!live) continue;
+#pragma unroll
+        for (int g = 0; g < VPT; g++) {
+            const int c = 8 * (g * TPR + lane);
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                t[g][i] = fmaf(-mean_h, hn[g][i], t[g][i]);
+                v[i] = p.skip * t[g][i];
+            }
+            if (q.dh_in) store8(at<T>(q.dh_in, row * q.ld_dh_in + c), C - c, v);
+            if (!p.d_y) continue;
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                z[g][i] = fmaf(p.scale * t[g][i], y[g][i], z[g][i]);
+                v[i] = r_y * fmaf(-mean_y, y[g][i], t[g][i] * gain[g][i]);
+            }
+            if (q.dy) store8(at<T>(q.dy, row * q.ld_dy + c), C - c, v);
+        }
+        if (p.d_gate && !q.strips.per_gate && ((row + 1) % p.rows_per_gate == 0 || row + 1 == end))
+            flush(q.dgate ? q.dgate + gate_row * C : nullptr);
+    }
+    if (q.strips.per_gate || !p.d_gate) {
+        float* to = nullptr;
+        if (q.dgate && q.strips.per_gate && strip < q.strips.count) {
+            if (q.strips.per_gate > 1) to = q.part_gate + strip * C;  // (a strip without rows: zeros)
+            else to = q.dgate + strip * C;
+        }
+        flush(to);
+    }
+    auto join = [&](float (&v)[VPT][8], float* part) {
+        if (!part) return;
+        float* const to = part + (int64_t)blockIdx.x * C;
+        if constexpr (kRows == 1) {
+#pragma unroll
+            for (int g = 0; g < VPT; g++) {
+                const int c = 8 * (g * TPR + lane);
+                store8(to + c, C - c, v[g]);
+            }
+        } else {
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < 8; i++) joined[threadIdx.x * 8 + i] = v[0][i];
+            __syncthreads();
+            for (int c = threadIdx.x; c < C; c += kThreads) {
+                float sum = joined[c];
+#pragma unroll
+                for (int r = 1; r < kRows; r++) sum += joined[r * TPR * 8 + c];
+                to[c] = sum;
             }
         }
-    }
-#pragma unroll
-    for (int g = 0; g < VPT; g++) {
-        const int c = 8 * (g * TPR + lane);
-        if (q.part_post) store8(q.part_post + strip * C + c, C - c, d_post[g]);
-        if (q.part_pre) store8(q.part_pre + strip * C + c, C - c, d_pre[g]);
-    }
+    };
+    join(d_post, q.part_post);
+    join(d_pre, q.part_pre);
 }
 
-// out[j][c] = sum over i < n of part[j n + i][c], j = blockIdx.y: 32 columns a workgroup, 8 slices of the rows, added up in
-// order
-__global__ __launch_bounds__(256) void k_strip_sums(const float* __restrict__ part, int64_t n, int C, float* __restrict__ out) {
-    __shared__ float slice[8][32];
-    const int col = threadIdx.x & 31, k = threadIdx.x >> 5, c = blockIdx.x * 32 + col;
-    const float* from = part + (int64_t)blockIdx.y * n * C;
+// Sums over the strips' parts, in order: blockIdx.y 0 and 1 the weights' (n parts), from 2 on the gate rows' (n_gate parts
+// each).  32 columns a workgroup, 32 slices of the parts.
+__global__ __launch_bounds__(1024) void k_strip_sums(const float* __restrict__ part_post, const float* __restrict__ part_pre, int64_t n,
+                                                     const float* __restrict__ part_gate, int64_t n_gate, int C,
+                                                     float* __restrict__ d_post, float* __restrict__ d_pre,
+                                                     float* __restrict__ d_gate) {
+    __shared__ float slice[32][33];
+    const int col = threadIdx.x & 31, k = threadIdx.x >> 5, c = blockIdx.x * 32 + col, which = blockIdx.y;
+    const float* from = which == 0 ? part_post : which == 1 ? part_pre : part_gate + (int64_t)(which - 2) * n_gate * C;
+    float* to = which == 0 ? d_post : which == 1 ? d_pre : d_gate + (int64_t)(which - 2) * C;
+    if (!to) return;
+    const int64_t count = which < 2 ? n : n_gate;
     float sum = 0.f;
     if (c < C)
-        for (int64_t i = k; i < n; i += 8) sum += from[i * C + c];
+#pragma unroll 4
+        for (int64_t i = k; i < count; i += 32) sum += from[i * C + c];
     slice[k][col] = sum;
     __syncthreads();
-    if (k == 0 && c < C) {
-#pragma unroll
-        for (int i = 1; i < 8; i++) sum += slice[i][col];
-        out[(int64_t)blockIdx.y * C + c] = sum;
-    }
+    sum = slice[col][k];  // (transposed: a wavefront's half has one column's slices)
+    sum = row16_sum(sum);
+    sum += __shfl_xor(sum, 16, 64);
+    if (col == 0 && blockIdx.x * 32 + k < C) to[blockIdx.x * 32 + k] = sum;
 }
 
-// TPR and VPT by the width alone: a row in as few lanes as hold it with at most 16 values each, whole wavefronts from 256
-// values on
 template <class F>
 hipError_t with_width(int C, F&& f) {
-    if (C <= 128) return f(Int<16>{}, Int<1>{});
-    if (C <= 512) return f(Int<64>{}, Int<1>{});
-    if (C <= 1024) return f(Int<64>{}, Int<2>{});
-    if (C <= 2048) return f(Int<256>{}, Int<1>{});
-    if (C <= 4096) return f(Int<256>{}, Int<2>{});
-    if (C <= 8192) return f(Int<512>{}, Int<2>{});
-    return f(Int<1024>{}, Int<2>{});
+    switch (lanes_of(C)) {
+        case 16: return f(Int<16>{}, Int<1>{});
+        case 64: return f(Int<64>{}, Int<1>{});
+        case 128: return f(Int<128>{}, Int<1>{});
+        case 256: return f(Int<256>{}, Int<1>{});
+        case 512: return f(Int<512>{}, Int<1>{});
+        default: return C <= 8192 ? f(Int<1024>{}, Int<1>{}) : f(Int<1024>{}, Int<2>{});
+    }
 }
 template <class F>
 hipError_t with_types(int type, int weight_type, F&& f) {
@@ -391,7 +521,8 @@ hipError_t launch_block_norm(const fmtc_norm& a, void* d_h_out, int64_t ld_h_out
             constexpr int TPR = decltype(lanes)::value, VPT = decltype(groups)::value;
             constexpr int rows = norm_threads(TPR) / TPR;
             int64_t grid = ceil_div(a.rows, rows);
-            if (grid > 2048) grid = 2048;
+            const int64_t most = 256 * 2048 / norm_threads(TPR);  // what walks at a time: 32 wavefronts a compute unit
+            if (grid > most) grid = most;
             return launch(K_BLOCK_NORM, k_block_norm<typename decltype(ty)::type, typename decltype(wt)::type, TPR, VPT>,
                           dim3((unsigned)grid), dim3(norm_threads(TPR)), 0, s, a, out);
         });
@@ -400,7 +531,8 @@ hipError_t launch_block_norm(const fmtc_norm& a, void* d_h_out, int64_t ld_h_out
 
 size_t block_norm_workspace(int64_t rows, int C, int64_t rows_per_gate) {
     const Strips st = make_strips(rows, C, rows_per_gate);
-    return align_up(sizeof(float) * (size_t)st.count * C, 256) * (st.per_gate > 1 ? 3 : 2);
+    const int64_t groups = ceil_div(st.count, norm_threads(lanes_of(C)) / lanes_of(C));
+    return 2 * align_up(sizeof(float) * (size_t)groups * C, 256) + (st.per_gate > 1 ? align_up(sizeof(float) * (size_t)st.count * C, 256) : 0);
 }
 
 hipError_t launch_block_norm_backward(const fmtc_norm& a, const float* d_stats, const void* d_dn, int64_t ld_dn,
@@ -408,26 +540,23 @@ hipError_t launch_block_norm_backward(const fmtc_norm& a, const float* d_stats, 
                                       int64_t ld_dh_in, float* d_dw_post, float* d_dw_pre, float* d_dgate,
                                       void* d_ws, hipStream_t s) {
     const Strips st = make_strips(a.rows, a.C, a.d_gate ? a.rows_per_gate : 0);
-    const size_t each = align_up(sizeof(float) * (size_t)st.count * a.C, 256);
-    float* part[3] = {static_cast<float*>(d_ws), reinterpret_cast<float*>(static_cast<char*>(d_ws) + each),
-                      reinterpret_cast<float*>(static_cast<char*>(d_ws) + 2 * each)};
+    const int64_t groups = ceil_div(st.count, norm_threads(lanes_of(a.C)) / lanes_of(a.C));
+    const size_t each = align_up(sizeof(float) * (size_t)groups * a.C, 256);
+    char* ws = static_cast<char*>(d_ws);
+    float *post = reinterpret_cast<float*>(ws), *pre = reinterpret_cast<float*>(ws + each), *gate = reinterpret_cast<float*>(ws + 2 * each);
     NormGrads q{d_stats, d_dn, d_dh, d_dy, d_dh_in, ld_dn, ld_dh, ld_dy, ld_dh_in,
-                d_dw_post ? part[0] : nullptr, d_dw_pre ? part[1] : nullptr, part[2], d_dgate, st};
+                d_dw_post ? post : nullptr, d_dw_pre ? pre : nullptr, gate, d_dgate, st};
     hipError_t e = with_types(a.type, a.weight_type, [&](auto ty, auto wt) {
-        return with_width(a.C, [&](auto lanes, auto groups) {
-            constexpr int TPR = decltype(lanes)::value, VPT = decltype(groups)::value;
+        return with_width(a.C, [&](auto lanes, auto per) {
+            constexpr int TPR = decltype(lanes)::value, VPT = decltype(per)::value;
             return launch(K_BLOCK_NORM_BACKWARD, k_block_norm_backward<typename decltype(ty)::type, typename decltype(wt)::type, TPR, VPT>,
-                          dim3((unsigned)ceil_div(st.count, norm_threads(TPR) / TPR)), dim3(norm_threads(TPR)), 0, s, a, q);
+                          dim3((unsigned)groups), dim3(norm_threads(TPR)), 0, s, a, q);
         });
     });
-    auto sums = [&](const float* from, int64_t n, int64_t groups, float* to) {
-        return launch(K_BLOCK_NORM_BACKWARD, k_strip_sums, dim3((unsigned)ceil_div(a.C, 32), (unsigned)groups), dim3(256), 0, s, from, n,
-                      (int)a.C, to);
-    };
-    if (e == hipSuccess && d_dw_post) e = sums(part[0], st.count, 1, d_dw_post);
-    if (e == hipSuccess && d_dw_pre) e = sums(part[1], st.count, 1, d_dw_pre);
-    if (e == hipSuccess && d_dgate && st.per_gate > 1) e = sums(part[2], st.per_gate, st.gates, d_dgate);
-    return e;
+    const bool join_gate = d_dgate && st.per_gate > 1;
+    if (e != hipSuccess || (!d_dw_post && !d_dw_pre && !join_gate)) return e;
+    return launch(K_BLOCK_NORM_BACKWARD, k_strip_sums, dim3((unsigned)ceil_div(a.C, 32), (unsigned)(join_gate ? 2 + st.gates : 2)), dim3(1024), 0, s,
+                  post, pre, groups, gate, st.per_gate, (int)a.C, d_dw_post, d_dw_pre, join_gate ? d_dgate : nullptr);
 }
 
 }  // namespace fmtc
