@@ -152,7 +152,10 @@ def _check(status):
 def _stream():
     import torch
 
-    return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+    try:  # the same stream as below, without the object around it (3 us of a call that launches one kernel)
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    except AttributeError:
+        return torch.cuda.current_stream().cuda_stream
 
 
 def _dims(x, layout):
@@ -588,51 +591,67 @@ def stream_info(header_bytes):
 
 # ---- a block of a network in 8-bit floating point ----
 
-def _dtype(t):
+_KINDS = {}    # torch type -> F32, BF16, F16; filled with torch's first use
+_FORMATS = {}  # torch type -> E4M3, E5M2
+_SCALES = {}   # torch type -> SCALE_F32, SCALE_E8M0
+
+
+def _types():
     import torch
 
+    _KINDS.update({torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16})
+    _FORMATS.update({torch.float8_e4m3fn: E4M3, torch.float8_e5m2: E5M2})
+    _SCALES.update({torch.float32: SCALE_F32, torch.float8_e8m0fnu: SCALE_E8M0})
+
+
+def _dtype(t):
+    if not _KINDS:
+        _types()
     try:
-        return {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}[t]
+        return _KINDS[t]
     except KeyError:
         raise ValueError(f"expected float32, bfloat16 or float16, got {t}") from None
 
 
 def _rows(t, what, cols=None, rows=None, dtype=None):
     """A device matrix whose rows are contiguous -> (pointer, type, row stride)."""
-    import torch
-
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 2):
+    try:
+        (r, c), (step_r, step_c), ok = t.shape, t.stride(), t.is_cuda
+    except (AttributeError, ValueError):
+        ok = False
+    if not ok:
         raise ValueError(f"{what}: expected a 2-d device tensor")
-    r, c = t.shape
     if (cols is not None and c != cols) or (rows is not None and r != rows):
         raise ValueError(f"{what}: expected {rows} x {cols} values, got {r} x {c}")
-    step_r, step_c = t.stride()
     if c > 1 and step_c != 1:
         raise ValueError(f"{what}: the values of a row have to be adjacent")
-    if dtype is not None and t.dtype != dtype:
-        raise ValueError(f"{what}: expected {dtype}, got {t.dtype}")
-    return t.data_ptr(), _dtype(t.dtype), step_r if r > 1 else c
+    kind = t.dtype
+    if dtype is not None and kind != dtype:
+        raise ValueError(f"{what}: expected {dtype}, got {kind}")
+    return t.data_ptr(), _dtype(kind), step_r if r > 1 else c
 
 
 def _vector(t, what, n, dtype=None):
     """A contiguous device vector of n values -> pointer (None: None)."""
-    import torch
-
     if t is None:
         return None
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.is_contiguous() and t.numel() == n) or \
-            (dtype is not None and t.dtype != dtype):
-        raise ValueError(f"{what}: expected {n} contiguous device values" + (f" of {dtype}" if dtype else ""))
-    return t.data_ptr()
+    try:
+        if t.is_cuda and t.is_contiguous() and t.numel() == n and (dtype is None or t.dtype == dtype):
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    raise ValueError(f"{what}: expected {n} contiguous device values" + (f" of {dtype}" if dtype else ""))
 
 
 def _workspace(workspace, size, device):
+    """-> (the tensor, its address, its bytes); a new one of `size` bytes if there is none"""
     import torch
 
-    if size and workspace is None:
-        workspace = torch.empty(size, dtype=torch.uint8, device=device)
     if workspace is None:
-        return None, None, 0
+        if not size:
+            return None, None, 0
+        workspace = torch.empty(size, dtype=torch.uint8, device=device)
+        return workspace, workspace.data_ptr(), size
     return workspace, _dev(workspace, torch.uint8), workspace.numel()
 
 
@@ -644,35 +663,44 @@ class F8:
     __slots__ = ("codes", "scales", "rows", "depth", "block_rows", "_c")
 
     def __init__(self, codes, scales, depth, block_rows=1):
-        import torch
-
-        formats = {torch.float8_e4m3fn: E4M3, torch.float8_e5m2: E5M2}
-        kinds = {torch.float32: SCALE_F32, torch.float8_e8m0fnu: SCALE_E8M0}
-        if codes.dim() != 2 or scales.dim() != 2 or codes.dtype not in formats or scales.dtype not in kinds or \
-                not (codes.is_cuda and scales.is_cuda):
+        if not _FORMATS:
+            _types()
+        try:
+            (rows, width), (n_blocks, n_rows) = codes.shape, scales.shape
+            fmt, kind = _FORMATS[codes.dtype], _SCALES[scales.dtype]
+            (ld, step), (ld_scales, step_scales) = codes.stride(), scales.stride()
+            ok = codes.is_cuda and scales.is_cuda
+        except (AttributeError, KeyError, ValueError):
+            ok = False
+        if not ok:
             raise ValueError("F8: expected 2-d device tensors, codes in an 8-bit format, scales f32 or e8m0")
-        self.codes, self.scales, self.depth, self.block_rows = codes, scales, int(depth), int(block_rows)
-        self.rows, width = codes.shape
-        blocks = -(-self.depth // F8_BLOCK)
-        if self.depth < 1 or self.block_rows not in (1, F8_BLOCK) or width < blocks * F8_BLOCK or \
-                scales.shape[0] != blocks or scales.shape[1] != -(-self.rows // self.block_rows):
-            raise ValueError(f"F8: codes {tuple(codes.shape)} and scales {tuple(scales.shape)} do not hold {self.rows} x "
-                             f"{depth} values in blocks of {block_rows} x {F8_BLOCK}")
-        if codes.stride(1) != 1 or (scales.shape[1] > 1 and scales.stride(1) != 1):
+        blocks = -(-depth // F8_BLOCK)
+        if depth < 1 or block_rows not in (1, F8_BLOCK) or width < blocks * F8_BLOCK or n_blocks != blocks or \
+                n_rows != -(-rows // block_rows):
+            raise ValueError(f"F8: codes {tuple(codes.shape)} and scales {tuple(scales.shape)} do not hold {rows} x {depth} "
+                             f"values in blocks of {block_rows} x {F8_BLOCK}")
+        if step != 1 or (n_rows > 1 and step_scales != 1):
             raise ValueError("F8: the codes of a row and the scales of a block of the depth have to be adjacent")
-        self._c = _F8(codes.data_ptr(), scales.data_ptr(), self.rows, self.depth, codes.stride(0) if self.rows > 1 else width,
-                      scales.stride(0) if blocks > 1 else scales.shape[1], formats[codes.dtype], kinds[scales.dtype],
-                      self.block_rows)
+        self._set(codes, scales, rows, depth, block_rows, ld if rows > 1 else width, ld_scales if blocks > 1 else n_rows, fmt, kind)
+
+    def _set(self, codes, scales, rows, depth, block_rows, ld, ld_scales, fmt, kind):
+        self.codes, self.scales, self.rows, self.depth, self.block_rows = codes, scales, rows, depth, block_rows
+        self._c = _F8(codes.data_ptr(), scales.data_ptr(), rows, depth, ld, ld_scales, fmt, kind, block_rows)
+        return self
 
 
 def f8_empty(rows, depth, fmt=E4M3, scales=SCALE_F32, block_rows=1, device="cuda"):
     """An F8 to be written by f8_quantize or block_norm."""
     import torch
 
+    if rows < 0 or depth < 1 or block_rows not in (1, F8_BLOCK):
+        raise ValueError(f"f8_empty: {rows} x {depth} values in blocks of {block_rows} rows")
     blocks = -(-depth // F8_BLOCK)
-    return F8(torch.empty((rows, blocks * F8_BLOCK), dtype=torch.float8_e5m2 if fmt == E5M2 else torch.float8_e4m3fn, device=device),
-              torch.empty((blocks, -(-rows // block_rows)), dtype=torch.float8_e8m0fnu if scales == SCALE_E8M0 else torch.float32,
-                          device=device), depth, block_rows)
+    ld, ld_scales = blocks * F8_BLOCK, -(-rows // block_rows)
+    return F8.__new__(F8)._set(
+        torch.empty((rows, ld), dtype=torch.float8_e5m2 if fmt == E5M2 else torch.float8_e4m3fn, device=device),
+        torch.empty((blocks, ld_scales), dtype=torch.float8_e8m0fnu if scales == SCALE_E8M0 else torch.float32, device=device),
+        rows, depth, block_rows, ld, ld_scales, fmt, scales)
 
 
 def _f8(q):
@@ -749,19 +777,18 @@ def f8_matmul_backward(dy, w_t, x_t, fmt=E4M3, scales=SCALE_F32, bias=False, dx=
 
 def _norm_args(y, h, w_post, w_pre, gate, rows_per_gate, skip, scale, eps):
     P, C = h.shape
-    a = _Norm(rows=P, C=C, skip=skip, scale=scale, eps=eps)
-    a.d_h, a.type, a.ld_h = _rows(h, "h")
-    if y is not None:
-        a.d_y, _, a.ld_y = _rows(y, "y", C, P, h.dtype)
-    kinds = {t.dtype for t in (w_post, w_pre, gate) if t is not None}
-    if len(kinds) > 1:
+    h_ptr, kind, ld_h = _rows(h, "h")
+    y_ptr, _, ld_y = _rows(y, "y", C, P, h.dtype) if y is not None else (None, 0, 0)
+    like = w_pre if w_pre is not None else w_post if w_post is not None else gate
+    if like is not None and any(t is not None and t.dtype != like.dtype for t in (w_post, w_pre, gate)):
         raise ValueError("w_post, w_pre and gate have different types")
-    a.weight_type = _dtype(kinds.pop()) if kinds else F32
-    a.d_w_post, a.d_w_pre = _vector(w_post, "w_post", C), _vector(w_pre, "w_pre", C)
-    if gate is not None:
-        a.rows_per_gate = int(rows_per_gate) or max(P, 1)
-        a.d_gate = _vector(gate, "gate", -(-P // a.rows_per_gate) * C if P and a.rows_per_gate > 0 else gate.numel())
-    return a
+    if gate is None:
+        rows_per_gate, gate_ptr = 0, None
+    else:
+        rows_per_gate = int(rows_per_gate) or max(P, 1)
+        gate_ptr = _vector(gate, "gate", -(-P // rows_per_gate) * C if P and rows_per_gate > 0 else gate.numel())
+    return _Norm(P, C, kind, F32 if like is None else _dtype(like.dtype), 0, y_ptr, h_ptr, ld_y, ld_h, _vector(w_post, "w_post", C),
+                 _vector(w_pre, "w_pre", C), gate_ptr, rows_per_gate, skip, scale, eps)
 
 
 def block_norm(y, h, w_post, w_pre, gate=None, rows_per_gate=0, skip=1.0, scale=1.0, eps=1e-6, h_out=None, n_out=None,
