@@ -643,6 +643,13 @@ def _vector(t, what, n, dtype=None):
     raise ValueError(f"{what}: expected {n} contiguous device values" + (f" of {dtype}" if dtype else ""))
 
 
+def _matrix(rows, cols, dtype, device):
+    """A new tensor [rows, cols] (the cheapest of torch's ways to make one)."""
+    import torch
+
+    return torch.empty_strided((rows, cols), (cols, 1), dtype=dtype, device=device)
+
+
 def _workspace(workspace, size, device):
     """-> (the tensor, its address, its bytes); a new one of `size` bytes if there is none"""
     import torch
@@ -698,8 +705,8 @@ def f8_empty(rows, depth, fmt=E4M3, scales=SCALE_F32, block_rows=1, device="cuda
     blocks = -(-depth // F8_BLOCK)
     ld, ld_scales = blocks * F8_BLOCK, -(-rows // block_rows)
     return F8.__new__(F8)._set(
-        torch.empty((rows, ld), dtype=torch.float8_e5m2 if fmt == E5M2 else torch.float8_e4m3fn, device=device),
-        torch.empty((blocks, ld_scales), dtype=torch.float8_e8m0fnu if scales == SCALE_E8M0 else torch.float32, device=device),
+        _matrix(rows, ld, torch.float8_e5m2 if fmt == E5M2 else torch.float8_e4m3fn, device),
+        _matrix(blocks, ld_scales, torch.float8_e8m0fnu if scales == SCALE_E8M0 else torch.float32, device),
         rows, depth, block_rows, ld, ld_scales, fmt, scales)
 
 
@@ -733,7 +740,7 @@ def f8_matmul(a, b, bias=None, out=None, dtype=None, accumulate=False, workspace
     if out is None:
         if accumulate:
             raise ValueError("accumulate needs the output that is added to")
-        out = torch.empty((M, N), dtype=dtype or torch.bfloat16, device=a.codes.device)
+        out = _matrix(M, N, dtype or torch.bfloat16, a.codes.device)
     ptr, kind, ld = _rows(out, "out", N, M, dtype)
     lib = load_library()
     workspace, ws, size = _workspace(workspace, lib.fmtc_f8_matmul_workspace_size(M, N, a.depth), out.device)
@@ -758,9 +765,9 @@ def f8_matmul_backward(dy, w_t, x_t, fmt=E4M3, scales=SCALE_F32, bias=False, dx=
     if accumulate and ((x_t is not None and dw is None) or (bias and dbias is None)):
         raise ValueError("accumulate needs the outputs that are added to")
     if w_t is not None and dx is None:
-        dx = torch.empty((P, w_t.rows), dtype=dy.dtype, device=dy.device)
+        dx = _matrix(P, w_t.rows, dy.dtype, dy.device)
     if x_t is not None and dw is None:
-        dw = torch.empty((O, x_t.rows), dtype=torch.float32, device=dy.device)
+        dw = _matrix(O, x_t.rows, torch.float32, dy.device)
     if bias and dbias is None:
         dbias = torch.empty(O, dtype=torch.float32, device=dy.device)
     if (dx is not None and w_t is None) or (dw is not None and x_t is None):
@@ -802,13 +809,13 @@ def block_norm(y, h, w_post, w_pre, gate=None, rows_per_gate=0, skip=1.0, scale=
     a = _norm_args(y, h, w_post, w_pre, gate, rows_per_gate, skip, scale, eps)
     P, C = h.shape
     if h_out is None:
-        h_out = torch.empty((P, C), dtype=h.dtype, device=h.device)
+        h_out = _matrix(P, C, h.dtype, h.device)
     elif h_out is False:
         h_out = None
     if n_out is None and w_pre is not None:
-        n_out = torch.empty((P, C), dtype=h.dtype, device=h.device)
+        n_out = _matrix(P, C, h.dtype, h.device)
     if stats is True:
-        stats = torch.empty((2, P), dtype=torch.float32, device=h.device)
+        stats = _matrix(2, P, torch.float32, h.device)
     h_ptr, _, h_ld = _rows(h_out, "h_out", C, P, h.dtype) if h_out is not None else (None, 0, 0)
     n_codes = n_out if isinstance(n_out, F8) else None
     n_ptr, _, n_ld = _rows(n_out, "n_out", C, P, h.dtype) if n_out is not None and n_codes is None else (None, 0, 0)
@@ -830,12 +837,12 @@ def block_norm_backward(dn, dh, y, h_out, stats, w_post, w_pre, gate=None, rows_
 
     a = _norm_args(y, h_out, w_post, w_pre, gate, rows_per_gate, skip, scale, 0.0)
     P, C = h_out.shape
-    new = lambda like: torch.empty(like.shape, dtype=torch.float32, device=h_out.device) if like is not None else None  # noqa: E731
+    new = lambda like: torch.empty_like(like, dtype=torch.float32) if like is not None else None  # noqa: E731
     dw_post, dw_pre, dgate = new(w_post), new(w_pre), new(gate)
     if dy is None and y is not None:
-        dy = torch.empty((P, C), dtype=h_out.dtype, device=h_out.device)
+        dy = _matrix(P, C, h_out.dtype, h_out.device)
     if dh_in is None:
-        dh_in = torch.empty((P, C), dtype=h_out.dtype, device=h_out.device)
+        dh_in = _matrix(P, C, h_out.dtype, h_out.device)
     of = lambda t, what: _rows(t, what, C, P, h_out.dtype) if t is not None else (None, 0, 0)  # noqa: E731
     (dn_p, _, dn_ld), (dh_p, _, dh_ld), (dy_p, _, dy_ld), (di_p, _, di_ld) = of(dn, "dn"), of(dh, "dh"), of(dy, "dy"), of(dh_in, "dh_in")
     ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
