@@ -70,8 +70,11 @@ __device__ __forceinline__ v4f mfma_block_wide(const Wide& b, const Wide& a, v4f
     return c;
 }
 
-// How a product is computed: f32 scales and the 8-bit instruction, power-of-two scales as its operands, or f16
-enum Way { kScaled = 0, kExponents = 1, kWide = 2 };
+// How a product is computed: f32 scales and the 8-bit instruction, power-of-two scales as its operands, or in f16 with either
+// kind of scale
+enum Way { kScaled = 0, kExponents = 1, kWide = 2, kWideExponents = 3 };
+constexpr bool is_wide(int way) { return way >= kWide; }
+constexpr int scale_kind(int way) { return way == kScaled || way == kWide ? FMTC_SCALE_F32 : FMTC_SCALE_E8M0; }
 
 // out[m][n .. n + 3] = v (+ bias) (+ what is there)
 __device__ __forceinline__ void store_out(void* out, int type, int64_t ld, int64_t m, int64_t n, int64_t N, v4f v,
@@ -102,11 +105,20 @@ __device__ __forceinline__ void store_out(void* out, int type, int64_t ld, int64
     }
 }
 
-// a scale as a float
-__device__ __forceinline__ float scale_value(const void* scales, int kind, int64_t at) {
-    if (kind == FMTC_SCALE_F32) return static_cast<const float*>(scales)[at];
-    const uint32_t e = static_cast<const uint8_t*>(scales)[at];  // 0: 2^-127, 255: not a number
-    return __uint_as_float(e == 0 ? 0x00400000u : e == 255 ? 0x7fc00000u : e << 23);
+// a scale as it is held, and as a float
+template <int KIND>
+__device__ __forceinline__ uint32_t load_scale(const void* scales, int64_t at) {
+    if constexpr (KIND == FMTC_SCALE_F32) return static_cast<const uint32_t*>(scales)[at];
+    else return static_cast<const uint8_t*>(scales)[at];
+}
+template <int KIND>
+__device__ __forceinline__ uint32_t scale_bits(uint32_t held) {
+    if constexpr (KIND == FMTC_SCALE_F32) return held;
+    else return held == 0 ? 0x00400000u : held == 255 ? 0x7fc00000u : held << 23;  // 2^-127 and not a number
+}
+template <int KIND>
+__device__ __forceinline__ float scale_value(const void* scales, int64_t at) {
+    return __uint_as_float(scale_bits<KIND>(load_scale<KIND>(scales, at)));
 }
 
 struct Product {
@@ -115,7 +127,7 @@ struct Product {
     int64_t M, N, blocks, ld_a, ld_b, ld_sa, ld_sb, ld_out;
     const float* bias;
     void* out;
-    int out_type, accumulate, scale;
+    int out_type, accumulate;
     int64_t split_blocks;  // tiles: blocks of the depth that a workgroup takes; the sums of split z go to out + z * split_out
     int64_t split_out;     // floats
 };
@@ -142,16 +154,15 @@ __global__ __launch_bounds__(64 * kRowsWaves) void k_f8_matmul_rows(Product p, u
     for (int64_t kb = wave; kb < p.blocks; kb += kRowsWaves) {
         const v8i b = load_operand(b_row + kb * kF8Block, g);
         if constexpr (WAY != kExponents) {
-            const int kind = WAY == kScaled ? (int)FMTC_SCALE_F32 : p.scale;
             float sb[4];
 #pragma unroll
             for (int r = 0; r < 4; r++) {
                 const int64_t nr = nt * 16 + g * 4 + r;
-                sb[r] = scale_value(p.sb, kind, kb * p.ld_sb + (nr < p.N ? nr : p.N - 1) / B_ROWS);
+                sb[r] = scale_value<scale_kind(WAY)>(p.sb, kb * p.ld_sb + (nr < p.N ? nr : p.N - 1) / B_ROWS);
             }
 #pragma unroll
             for (int i = 0; i < MT; i++) {
-                const float sa = scale_value(p.sa, kind, kb * p.ld_sa + m_at[i]);
+                const float sa = scale_value<scale_kind(WAY)>(p.sa, kb * p.ld_sa + m_at[i]);
                 const v8i a = load_operand(a_row[i] + kb * kF8Block, g);
                 const v4f zero = {}, d = WAY == kScaled ? mfma_block<FORMAT>(b, a, zero) : mfma_block_wide(widen<FMTC_E4M3>(b), widen<FORMAT>(a), zero);
 #pragma unroll
@@ -206,7 +217,7 @@ __device__ __forceinline__ void load_to_lds16(const uint8_t* base, uint32_t off,
 }
 
 template <int FORMAT, int WAY, int B_ROWS, class S>
-__global__ __launch_bounds__(S::kThreads) void k_f8_matmul_tiles(Product p, uint32_t tiles_m, uint32_t tiles_n) {
+__global__ __launch_bounds__(S::kThreads, 2) void k_f8_matmul_tiles(Product p, uint32_t tiles_m, uint32_t tiles_n) {
     extern __shared__ __attribute__((aligned(128))) uint8_t lds[];
     constexpr int MT = S::MT, NT = S::NT;
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), g = lane >> 4, i16 = lane & 15;
@@ -235,7 +246,7 @@ __global__ __launch_bounds__(S::kThreads) void k_f8_matmul_tiles(Product p, uint
     const uint32_t lds_at = (uint32_t)(uintptr_t)(lds_void_t*)lds;
     // A quarter of a step's loads: all at once, the queue of loads is full and the wavefront stands still.  (f16: the products
     // take twice as long and come less dense, the loads are best out of the way: 1112 us in quarters, 1038 us, 8192^3.)
-    constexpr bool kQuarters = WAY != kWide;
+    constexpr bool kQuarters = !is_wide(WAY);
     auto fetch = [&](int64_t kb, uint32_t stage, int quarter) {
         const uint32_t to = lds_at + stage * S::kStage + wave * S::kLoads * 1024;
 #pragma unroll
@@ -252,10 +263,9 @@ __global__ __launch_bounds__(S::kThreads) void k_f8_matmul_tiles(Product p, uint
     else off_s = (t - S::BM < rows_b ? t - S::BM : rows_b - 1) / B_ROWS;
     auto fetch_scale = [&](int64_t kb) {
         const int64_t at = first_s + kb * step_s + off_s;
-        if constexpr (WAY == kExponents) mine = static_cast<const uint8_t*>(from_s)[at];
-        else mine = __float_as_uint(scale_value(from_s, WAY == kScaled ? (int)FMTC_SCALE_F32 : p.scale, at));
+        mine = load_scale<scale_kind(WAY)>(from_s, at);  // (made a float where it is put: the load has a step's time)
     };
-    auto put_scale = [&](int64_t kb) { scales[(kb & 1) * S::kThreads + t] = mine; };
+    auto put_scale = [&](int64_t kb) { scales[(kb & 1) * S::kThreads + t] = WAY == kExponents ? mine : scale_bits<scale_kind(WAY)>(mine); };
 
     const int row_a = wm * MT * 16 + i16, row_b = S::BM + wn * 64 + i16, key = row_key(i16);  // (the key of row + 16 i, too)
     auto piece = [&](int64_t kb, int row) {
@@ -277,9 +287,9 @@ __global__ __launch_bounds__(S::kThreads) void k_f8_matmul_tiles(Product p, uint
 #pragma unroll
     for (int q = 0; q < (kQuarters ? 2 : 4); q++) fetch(last < 1 ? last : 1, 1, q);
     // b's tiles as the way takes them; the products of a tile of a, added to the sums while the next one is multiplied
-    using Held = typename std::conditional<WAY == kWide, Wide, v8i>::type;
+    using Held = typename std::conditional<is_wide(WAY), Wide, v8i>::type;
     auto hold = [&](v8i raw) {
-        if constexpr (WAY == kWide) return widen<FMTC_E4M3>(raw);
+        if constexpr (is_wide(WAY)) return widen<FMTC_E4M3>(raw);
         else return raw;
     };
     Held b[NT];
@@ -334,18 +344,18 @@ __global__ __launch_bounds__(S::kThreads) void k_f8_matmul_tiles(Product p, uint
                 }
             } else {
                 v4f* const before = acc[i ? i - 1 : MT - 1];
-                const auto held = [&] { if constexpr (WAY == kWide) return widen<FORMAT>(a[0]); else return a[0]; }();
+                const auto held = [&] { if constexpr (is_wide(WAY)) return widen<FORMAT>(a[0]); else return a[0]; }();
 #pragma unroll
                 for (int j = 0; j < NT; j++) {
                     v4f now;
-                    if constexpr (WAY == kWide) now = mfma_block_wide(b[j], held, v4f{0.f, 0.f, 0.f, 0.f});
+                    if constexpr (is_wide(WAY)) now = mfma_block_wide(b[j], held, v4f{0.f, 0.f, 0.f, 0.f});
                     else now = mfma_block<FORMAT>(b[j], held, v4f{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
                     for (int r = 0; r < 4; r++) {
                         before[j][r] = fmaf(d[j][r], f[B_ROWS == 1 ? j : 0][B_ROWS == 1 ? r : 0], before[j][r]);
                         if constexpr (B_ROWS == 1) f[j][r] = __uint_as_float(sa[0]) * __uint_as_float(sb[j][r]);
                     }
-                    if constexpr (WAY == kWide) asm volatile("" : "+v"(before[j]));  // (else the scheduler gathers the sums)
+                    if constexpr (is_wide(WAY)) asm volatile("" : "+v"(before[j]));  // (else the scheduler gathers the sums)
                     d[j] = now;
                 }
                 if constexpr (B_ROWS != 1) f[0][0] = __uint_as_float(sa[0]) * __uint_as_float(sb[0][0]);
@@ -405,7 +415,12 @@ __global__ __launch_bounds__(256) void k_f8_join(Product p, const float* __restr
 
 template <class F>
 hipError_t with_way(int way, F&& f) {
-    return way == kScaled ? f(Int<kScaled>{}) : way == kExponents ? f(Int<kExponents>{}) : f(Int<kWide>{});
+    switch (way) {
+        case kScaled: return f(Int<kScaled>{});
+        case kExponents: return f(Int<kExponents>{});
+        case kWide: return f(Int<kWide>{});
+        default: return f(Int<kWideExponents>{});
+    }
 }
 
 }  // namespace
@@ -465,9 +480,10 @@ hipError_t launch_f8_matmul(const fmtc_f8& a, const fmtc_f8& b, const float* d_b
                             int64_t ld_out, int accumulate, void* d_ws, hipStream_t s) {
     Product p{static_cast<const uint8_t*>(a.d_codes), static_cast<const uint8_t*>(b.d_codes), a.d_scales, b.d_scales,
               a.rows, b.rows, (a.depth + kF8Block - 1) / kF8Block, a.ld, b.ld, a.ld_scales, b.ld_scales, ld_out,
-              d_bias, d_out, out_type, accumulate, a.scale, 0, 0};
-    const int way = out_type == FMTC_F32 ? kWide : a.scale == FMTC_SCALE_E8M0 ? kExponents : kScaled;
-    Plan plan = make_plan(p.M, p.N, a.depth, way == kWide);
+              d_bias, d_out, out_type, accumulate, 0, 0};
+    const bool exponents = a.scale == FMTC_SCALE_E8M0;
+    const int way = out_type == FMTC_F32 ? (exponents ? kWideExponents : kWide) : exponents ? kExponents : kScaled;
+    Plan plan = make_plan(p.M, p.N, a.depth, is_wide(way));
     if (p.ld_a >= (1 << 23) || p.ld_b >= (1 << 23)) plan = {kRows, 1, p.blocks};  // (a tile's offsets are 32 bits)
     p.split_blocks = plan.split_blocks;
     Product inner = p;
@@ -490,7 +506,7 @@ hipError_t launch_f8_matmul(const fmtc_f8& a, const fmtc_f8& b, const float* d_b
                     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds);
                     return e != hipSuccess ? e : launch(K_F8_MATMUL, kernel, dim3((unsigned)(tm * tn * plan.splits)), dim3(S::kThreads), S::kLds, s, inner, (uint32_t)tm, (uint32_t)tn);
                 };
-                if (plan.kernel == kTiles256) return tiles(Tile<2, 4, W == kWide ? 4 : 8>{});
+                if (plan.kernel == kTiles256) return tiles(Tile<2, 4, is_wide(W) ? 4 : 8>{});
                 if (plan.kernel == kTiles128) return tiles(Tile<2, 2, 4>{});
                 const int64_t n_tiles = (p.N + 15) / 16;
                 if (p.M <= 16)
