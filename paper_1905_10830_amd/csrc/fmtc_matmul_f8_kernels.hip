@@ -195,25 +195,35 @@ __global__ __launch_bounds__(64 * kRowsWaves) void k_f8_matmul_rows(Product p, u
 //
 // Rows of 128 bytes in LDS, the 16-byte pieces of a row exchanged by a key of the row, so that 16 lanes that read the same
 // piece of 16 rows touch every bank once.  The results leave through LDS too, 64 columns of a row at a time.
-template <int WM_, int WN_, int MT_>
+template <int WM_, int WN_, int MT_, int STAGES_>
 struct Tile {
-    static constexpr int WM = WM_, WN = WN_, MT = MT_, NT = 4;
+    static constexpr int WM = WM_, WN = WN_, MT = MT_, NT = 4, kStages = STAGES_;
     static constexpr int kThreads = 64 * WM * WN, BM = WM * MT * 16, BN = WN * NT * 16;
     static constexpr int kStage = (BM + BN) * kF8Block, kScales = 4 * kThreads;
     static constexpr int kLoads = (BM + BN) / 8 / (WM * WN);  // loads of 8 rows a wavefront, a's and b's in one range
     static constexpr int kPitch = 68, kOutRows = 64;         // results in LDS: a wavefront's 64 rows x 64 columns at a time
-    static constexpr int kLoop = 2 * (kStage + kScales), kOut = WM * WN * kOutRows * kPitch * 4;
+    static constexpr int kLoop = kStages * (kStage + kScales), kOut = WM * WN * kOutRows * kPitch * 4;
     static constexpr int kLds = kLoop > kOut ? kLoop : kOut;
     static_assert((BM + BN) % (8 * WM * WN) == 0 && BM % 64 == 0 && MT % 4 == 0);
-    static_assert(BM + BN <= kThreads);  // a thread moves one scale
+    static_assert(BM + BN <= kThreads);  // a lane moves one scale
+    static_assert((kStages & (kStages - 1)) == 0);
 };
 __device__ __forceinline__ int row_key(int row) { return (row >> 1) & 7; }
 
-// 16 bytes a lane from base + off straight into LDS, lane l to lds_base + 16 l (the caller counts its loads in flight)
-__device__ __forceinline__ void load_to_lds16(const uint8_t* base, uint32_t off, uint32_t lds_base) {
+// 16 bytes, 4 bytes or a byte (as a word) a lane from base + off straight into LDS, lane l to lds_base + 16 l or 4 l; the
+// caller counts its loads in flight
+template <int BYTES>
+__device__ __forceinline__ void load_to_lds_at(const void* base, uint32_t off, uint32_t lds_base) {
     uint32_t keep;
-    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b32 m0, %0"
-                 : "=&s"(keep) : "v"(off), "s"(base), "s"(lds_base) : "memory");
+    if constexpr (BYTES == 16)
+        asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b32 m0, %0"
+                     : "=&s"(keep) : "v"(off), "s"(base), "s"(lds_base) : "memory");
+    else if constexpr (BYTES == 4)
+        asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2\n\ts_mov_b32 m0, %0"
+                     : "=&s"(keep) : "v"(off), "s"(base), "s"(lds_base) : "memory");
+    else
+        asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_ubyte %1, %2\n\ts_mov_b32 m0, %0"
+                     : "=&s"(keep) : "v"(off), "s"(base), "s"(lds_base) : "memory");
 }
 
 template <int FORMAT, int WAY, int B_ROWS, class S>
@@ -244,48 +254,60 @@ __global__ __launch_bounds__(S::kThreads, 2) void k_f8_matmul_tiles(Product p, u
         off[i] = (uint32_t)r * (uint32_t)(of_a ? p.ld_a : p.ld_b) + 16 * ((lane & 7) ^ row_key(row));
     }
     const uint32_t lds_at = (uint32_t)(uintptr_t)(lds_void_t*)lds;
-    // A quarter of a step's loads: all at once, the queue of loads is full and the wavefront stands still.  (f16: the products
-    // take twice as long and come less dense, the loads are best out of the way: 1112 us in quarters, 1038 us, 8192^3.)
-    constexpr bool kQuarters = !is_wide(WAY);
-    auto fetch = [&](int64_t kb, uint32_t stage, int quarter) {
-        const uint32_t to = lds_at + stage * S::kStage + wave * S::kLoads * 1024;
-#pragma unroll
-        for (int i = quarter * S::kLoads / 4; i < (quarter + 1) * S::kLoads / 4; i++)
-            load_to_lds16(((wave * S::kLoads + i) * 8 < S::BM ? from_a : from_b) + kb * kF8Block, off[i], to + i * 1024);
-    };
-    // scales: a thread has that of a row of a or of b, as a float or an exponent
-    uint32_t* const scales = reinterpret_cast<uint32_t*>(lds + 2 * S::kStage);
+    // Scales: a lane moves that of a row of a or of b (past both: the last of b again), as it is straight into LDS, or, for the
+    // f16 way that would make floats of them again and again, through a register in which it becomes one.
+    constexpr bool kStraight = WAY != kWideExponents;
+    static_assert(kStraight || S::kStages == 2);
+    uint32_t mine = 0;
+    constexpr int kScaleBytes = scale_kind(WAY) == FMTC_SCALE_F32 ? 4 : 1, kStages = S::kStages;
+    uint32_t* const scales = reinterpret_cast<uint32_t*>(lds + kStages * S::kStage);
     const bool scale_of_a = wave * 64 < S::BM;
-    const void* const from_s = scale_of_a ? p.sa : p.sb;
-    const int64_t step_s = scale_of_a ? p.ld_sa : p.ld_sb, first_s = (scale_of_a ? m0 : n0 / B_ROWS) + kb0 * step_s;
-    uint32_t off_s, mine = 0;
+    const int64_t step_s = scale_of_a ? p.ld_sa : p.ld_sb;
+    const uint8_t* const from_s = static_cast<const uint8_t*>(scale_of_a ? p.sa : p.sb) + ((scale_of_a ? m0 : n0 / B_ROWS) + kb0 * step_s) * kScaleBytes;
+    uint32_t off_s;
     if (scale_of_a) off_s = t < rows_a ? t : rows_a - 1;
     else off_s = (t - S::BM < rows_b ? t - S::BM : rows_b - 1) / B_ROWS;
-    auto fetch_scale = [&](int64_t kb) {
-        const int64_t at = first_s + kb * step_s + off_s;
-        mine = load_scale<scale_kind(WAY)>(from_s, at);  // (made a float where it is put: the load has a step's time)
+    off_s *= kScaleBytes;
+    // A quarter of a step's loads, the scales with the first: all at once, the queue of loads is full and the wavefront stands
+    // still.  (f16: the products take twice as long and come less dense, the loads are best out of the way: 1112 us in
+    // quarters, 1038 us, 8192^3.)  Past the last block: that one again, into a place that is free; not used, and no branch in
+    // the loop.
+    constexpr bool kQuarters = !is_wide(WAY);
+    const int64_t last = blocks - 1;
+    auto fetch = [&](int64_t kb, int quarter) {
+        const uint32_t stage = (uint32_t)kb & (kStages - 1), to = lds_at + stage * S::kStage + wave * S::kLoads * 1024;
+        if (kb > last) kb = last;
+        if (quarter == 0) {
+            const uint8_t* const from = from_s + kb * step_s * kScaleBytes;
+            if constexpr (kStraight) load_to_lds_at<kScaleBytes>(from, off_s, lds_at + kStages * S::kStage + stage * S::kScales + wave * 256);
+            else mine = from[off_s];
+        }
+#pragma unroll
+        for (int i = quarter * S::kLoads / 4; i < (quarter + 1) * S::kLoads / 4; i++)
+            load_to_lds_at<16>(((wave * S::kLoads + i) * 8 < S::BM ? from_a : from_b) + kb * kF8Block, off[i], to + i * 1024);
     };
-    auto put_scale = [&](int64_t kb) { scales[(kb & 1) * S::kThreads + t] = WAY == kExponents ? mine : scale_bits<scale_kind(WAY)>(mine); };
+    auto put_scale = [&](int64_t kb) {
+        if constexpr (!kStraight) scales[((uint32_t)kb & (kStages - 1)) * S::kThreads + t] = scale_bits<FMTC_SCALE_E8M0>(mine);
+    };
+    constexpr int kEach = S::kLoads + 1, kFirst = 1 + (kQuarters ? S::kLoads / 2 : S::kLoads);  // loads of a step, of its first part
 
     const int row_a = wm * MT * 16 + i16, row_b = S::BM + wn * 64 + i16, key = row_key(i16);  // (the key of row + 16 i, too)
     auto piece = [&](int64_t kb, int row) {
-        const uint8_t* at = lds + (kb & 1) * S::kStage + row * kF8Block;
+        const uint8_t* at = lds + ((uint32_t)kb & (kStages - 1)) * S::kStage + row * kF8Block;
         const v4i lo = *reinterpret_cast<const v4i*>(at + 16 * (g ^ key)), hi = *reinterpret_cast<const v4i*>(at + 16 * ((4 + g) ^ key));
         return v8i{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
     };
 
     v4f acc[MT][NT] = {};
-    // (past the last block: that one again, into the place that is free; not used, and no branch in the loop)
-    const int64_t last = blocks - 1;
+    // all blocks' loads that fit, and the first part of those of the last place's; the rest of them in the first step
 #pragma unroll
-    for (int q = 0; q < 4; q++) fetch(0, 0, q);
-    fetch_scale(0);
-    wait_loads<0>();
-    put_scale(0);
+    for (int k = 0; k < kStages; k++) {
+#pragma unroll
+        for (int q = 0; q < (kQuarters && k == kStages - 1 ? 2 : 4); q++) fetch(k, q);
+        if (k == 0) put_scale(0);
+    }
+    wait_loads<(kStages - 2) * kEach + kFirst>();
     __syncthreads();
-    fetch_scale(last < 1 ? last : 1);
-#pragma unroll
-    for (int q = 0; q < (kQuarters ? 2 : 4); q++) fetch(last < 1 ? last : 1, 1, q);
     // b's tiles as the way takes them; the products of a tile of a, added to the sums while the next one is multiplied
     using Held = typename std::conditional<is_wide(WAY), Wide, v8i>::type;
     auto hold = [&](v8i raw) {
@@ -297,11 +319,11 @@ __global__ __launch_bounds__(S::kThreads, 2) void k_f8_matmul_tiles(Product p, u
     uint32_t sa[3], sb[NT][4];
     auto read_a = [&](int to, int64_t kb, int i) {
         a[to] = piece(kb, row_a + 16 * i);
-        sa[to] = scales[(kb & 1) * S::kThreads + row_a + 16 * i];
+        sa[to] = scales[((uint32_t)kb & (kStages - 1)) * S::kThreads + row_a + 16 * i];
     };
     auto read_b = [&](int64_t kb, int j) {
         b[j] = hold(piece(kb, row_b + 16 * j));
-        const uint32_t* s = scales + (kb & 1) * S::kThreads;
+        const uint32_t* s = scales + ((uint32_t)kb & (kStages - 1)) * S::kThreads;
         if constexpr (WAY == kExponents) {
             sb[j][0] = s[row_b + 16 * j];
         } else if constexpr (B_ROWS == 1) {
@@ -323,16 +345,15 @@ __global__ __launch_bounds__(S::kThreads, 2) void k_f8_matmul_tiles(Product p, u
         for (int i = 0; i < MT; i++) {
             if (i == MT - 2) {
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the last tiles of a are in registers
-                wait_loads<0>();                                    // the next step's operands (this wavefront's) are in LDS
+                wait_loads<(kStages - 2) * kEach>();                // the next step's operands (this wavefront's) are in LDS
                 put_scale(kb + 1);
                 __syncthreads();
-                fetch_scale(kb + 2 < last ? kb + 2 : last);
             }
             if (i == MT - 2 || (kQuarters && i == MT - 1)) {
 #pragma unroll
-                for (int q = i - (MT - 2); q < (kQuarters ? i - (MT - 2) + 1 : 4); q++) fetch(kb + 2 < last ? kb + 2 : last, (uint32_t)kb & 1, q);
+                for (int q = i - (MT - 2); q < (kQuarters ? i - (MT - 2) + 1 : 4); q++) fetch(kb + kStages, q);
             }
-            if (kQuarters && i < 2) fetch(kb + 1 < last ? kb + 1 : last, (uint32_t)(kb + 1) & 1, i + 2);
+            if (kQuarters && i < 2) fetch(kb + kStages - 1, i + 2);
             // (past the last step: what LDS holds, not used)
             if (i < MT - 2) read_a(2, kb, i + 2);
             else read_a(2, kb + 1, i + 2 - MT);
@@ -344,12 +365,12 @@ __global__ __launch_bounds__(S::kThreads, 2) void k_f8_matmul_tiles(Product p, u
                 }
             } else {
                 v4f* const before = acc[i ? i - 1 : MT - 1];
-                const auto held = [&] { if constexpr (is_wide(WAY)) return widen<FORMAT>(a[0]); else return a[0]; }();
+                const auto with = [&] { if constexpr (is_wide(WAY)) return widen<FORMAT>(a[0]); else return a[0]; }();
 #pragma unroll
                 for (int j = 0; j < NT; j++) {
                     v4f now;
-                    if constexpr (is_wide(WAY)) now = mfma_block_wide(b[j], held, v4f{0.f, 0.f, 0.f, 0.f});
-                    else now = mfma_block<FORMAT>(b[j], held, v4f{0.f, 0.f, 0.f, 0.f});
+                    if constexpr (is_wide(WAY)) now = mfma_block_wide(b[j], with, v4f{0.f, 0.f, 0.f, 0.f});
+                    else now = mfma_block<FORMAT>(b[j], with, v4f{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
                     for (int r = 0; r < 4; r++) {
                         before[j][r] = fmaf(d[j][r], f[B_ROWS == 1 ? j : 0][B_ROWS == 1 ? r : 0], before[j][r]);
@@ -413,6 +434,9 @@ __global__ __launch_bounds__(256) void k_f8_join(Product p, const float* __restr
     store_out(p.out, p.out_type, p.ld_out, m, n, p.N, v, p.bias, p.accumulate);
 }
 
+// rows of the large tile: half as many where the operands in f16, or a scale for every row of b, take the registers
+constexpr int kernel256_rows(int way, int b_rows) { return is_wide(way) || (way == kScaled && b_rows == 1) ? 128 : 256; }
+
 template <class F>
 hipError_t with_way(int way, F&& f) {
     switch (way) {
@@ -430,11 +454,13 @@ namespace {
 // Which kernel, and in how many parts of the depth: the least of the times that a product of these sizes is expected to
 // take, in us, from what each kernel takes to start and end and for a block of the depth, alone on a compute unit and with
 // all of them busy.  The numbers are fits to measured times over 17 to 4096 rows, 512 to 8192 columns and a depth of 512 to
-// 8192 (with f32 scales): 128 x 4096 x 4096 rows 22.7, tiles of 128 30.4, in 4 parts 21.6; 1024 x 1024 x 4096 40.7, 30.6, 25.9
-// in 4 parts; 4096 x 1024 x 1024 45.2, 14.3, tiles of 256 21.6; 4096^3 -, 87.8, 63.9; 512 x 8192 x 8192 -, 66.6, 85.1, and
-// 52.9 in 4 parts of tiles of 256.  Up to 16 rows the wavefronts of the first kernel waste nothing: always that one.
+// 8192.  With f32 scales and bf16 results: 128 x 4096 x 4096 rows 23.2, tiles of 128 26.1, in 4 parts 19.8; 1024 x 1024 x 4096
+// 41.7, 26.3, 24.1 in 4 parts; 4096 x 1024 x 1024 45.8, 12.8, tiles of 256 21.6; 4096^3 -, 87.4, 65.7.  Four steps' operands
+// in LDS (one workgroup a compute unit, not two) where that holds all tiles: 1024 x 4096 x 4096 34.4 -> 28.9; beyond,
+// 2048 x 4096 x 4096, 45.0 -> 53.7; alone they gain nothing (512 x 512 x 8192 45.1, 43.9), nor in f16.  Up to 16 rows the
+// wavefronts of the first kernel waste nothing: always that one.
 struct Plan { int kernel, splits; int64_t split_blocks; };
-enum { kRows = 0, kTiles128 = 1, kTiles256 = 2 };
+enum { kRows = 0, kTiles128 = 1, kTiles256 = 2, kTiles128Deep = 3 };
 constexpr double kCus = 256;
 
 Plan make_plan(int64_t M, int64_t N, int64_t K, bool wide) {
@@ -448,15 +474,16 @@ Plan make_plan(int64_t M, int64_t N, int64_t K, bool wide) {
             const int64_t bm = kernel == kTiles256 && !wide ? 256 : 128, bn = kernel == kTiles256 ? 256 : 128;
             const int64_t per = (blocks + want - 1) / want, splits = (blocks + per - 1) / per;
             const double groups = (double)((M + bm - 1) / bm) * ((N + bn - 1) / bn) * splits;
+            const bool deep = kernel == kTiles128 && !wide && groups <= kCus && groups > kCus / 4;
             const double busy = fmin(1.0, groups / kCus), rounds = ceil(groups / kCus);
             double start, step;
-            if (kernel == kTiles128) start = wide ? 8.0 : 6.5, step = wide ? 1.22 : 0.74 + 0.16 * busy;
+            if (kernel == kTiles128) start = wide ? 7.0 : 6.0, step = wide ? 1.05 + 0.1 * busy : deep ? 0.58 + 0.1 * busy : 0.6 + 0.1 * busy;
             else start = wide ? 9.0 : 11.0, step = wide ? 1.68 + 0.35 * busy : 1.14 + 0.5 * busy;
             double t = start + step * per * rounds;
             if (splits > 1) t += 4.0 + 1e-6 * splits * M * N;  // the parts' sums written and read, 8 bytes at 8 TB/s
             if (t < least) {
                 least = t;
-                best = {kernel, (int)splits, per};
+                best = {deep ? (int)kTiles128Deep : kernel, (int)splits, per};
             }
         }
     return best;
@@ -506,8 +533,10 @@ hipError_t launch_f8_matmul(const fmtc_f8& a, const fmtc_f8& b, const float* d_b
                     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds);
                     return e != hipSuccess ? e : launch(K_F8_MATMUL, kernel, dim3((unsigned)(tm * tn * plan.splits)), dim3(S::kThreads), S::kLds, s, inner, (uint32_t)tm, (uint32_t)tn);
                 };
-                if (plan.kernel == kTiles256) return tiles(Tile<2, 4, is_wide(W) ? 4 : 8>{});
-                if (plan.kernel == kTiles128) return tiles(Tile<2, 2, 4>{});
+                if (plan.kernel == kTiles256) return tiles(Tile<2, 4, kernel256_rows(W, B) / 32, 2>{});
+                if (plan.kernel == kTiles128) return tiles(Tile<2, 2, 4, 2>{});
+                if constexpr (!is_wide(W))
+                    if (plan.kernel == kTiles128Deep) return tiles(Tile<2, 2, 4, 4>{});
                 const int64_t n_tiles = (p.N + 15) / 16;
                 if (p.M <= 16)
                     return launch(K_F8_MATMUL, k_f8_matmul_rows<F, W, B, 1>, dim3((unsigned)n_tiles), dim3(64 * kRowsWaves), 0, s, p,
