@@ -81,6 +81,39 @@ __device__ __forceinline__ void store8(T* p, int64_t n, const float (&v)[8]) {
     }
 }
 
+// 8 values as they lie in memory, in whole registers
+template <class T>
+struct Raw {
+    static constexpr int kWords = 2 * sizeof(T), kPer = 4 / sizeof(T);
+    uint32_t w[kWords];
+    // values c .. c + 7 of a row of C.  One load without a branch, so that many can be on their way together: lanes past the
+    // row read its first values, which their caller has no use for.  Only the lane at the end of a row whose length is no
+    // multiple of 8 goes value by value (0 beyond the end).
+    __device__ __forceinline__ void load(const T* row, int64_t c, int64_t C) {
+        if (C >= 8) __builtin_memcpy(w, row + (c + 8 <= C ? c : 0), sizeof w);
+        if (c < C && c + 8 > C) {
+#pragma unroll
+            for (int i = 0; i < kWords; i++) {
+                w[i] = 0;
+#pragma unroll
+                for (int j = 0; j < kPer; j++)
+                    if (c + i * kPer + j < C) {
+                        if constexpr (kPer == 2) w[i] |= (uint32_t)__builtin_bit_cast(uint16_t, row[c + i * kPer + j]) << (16 * j);
+                        else w[i] = __builtin_bit_cast(uint32_t, row[c + i]);
+                    }
+            }
+        }
+    }
+    __device__ __forceinline__ void zero_unless(bool live) {
+#pragma unroll
+        for (int i = 0; i < kWords; i++) w[i] = live ? w[i] : 0u;
+    }
+    __device__ __forceinline__ float operator[](int i) const {
+        if constexpr (kPer == 1) return __uint_as_float(w[i]);
+        else return to_f32(__builtin_bit_cast(T, (uint16_t)(w[i >> 1] >> (16 * (i & 1)))));
+    }
+};
+
 // a reduction over a row of 16 lanes; every lane of the row gets the result
 template <int CTRL>
 __device__ __forceinline__ float dpp_f32(float v) {

@@ -430,6 +430,7 @@ __global__ __launch_bounds__(256) void k_f8_join(Product p, const float* __restr
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, m = i / quads, n = (i - m * quads) * 4;
     if (m >= p.M) return;
     v4f v = *reinterpret_cast<const v4f*>(part + m * ld + n);
+#pragma unroll 4
     for (int z = 1; z < splits; z++) v += *reinterpret_cast<const v4f*>(part + z * p.split_out + m * ld + n);
     store_out(p.out, p.out_type, p.ld_out, m, n, p.N, v, p.bias, p.accumulate);
 }
@@ -468,7 +469,7 @@ Plan make_plan(int64_t M, int64_t N, int64_t K, bool wide) {
     Plan best{kRows, 1, blocks};
     if (M <= 16) return best;
     const double row_groups = (double)((M + 63) / 64) * ((N + 15) / 16);
-    double least = 2.5 + 2.3 * ((blocks + kRowsWaves - 1) / kRowsWaves) * fmax(1.0, row_groups / kCus);
+    double least = 2.5 + (wide ? 2.6 : 2.3) * ((blocks + kRowsWaves - 1) / kRowsWaves) * ceil(row_groups / kCus);
     for (int kernel = kTiles128; kernel <= (M > 128 && N > 128 ? kTiles256 : kTiles128); kernel++)
         for (int64_t want = 1; want <= 16 && want <= blocks; want *= 2) {
             const int64_t bm = kernel == kTiles256 && !wide ? 256 : 128, bn = kernel == kTiles256 ? 256 : 128;

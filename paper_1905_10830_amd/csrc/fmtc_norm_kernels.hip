@@ -47,33 +47,6 @@ struct RowSums {
     }
 };
 
-// 8 values as they lie in memory, of which the first n exist, in whole registers
-template <class T>
-struct Raw {
-    static constexpr int kWords = 2 * sizeof(T), kPer = 4 / sizeof(T);
-    uint32_t w[kWords];
-    __device__ __forceinline__ void load(const T* p, int n) {
-        if (n >= 8) {
-            __builtin_memcpy(w, p, sizeof w);
-            return;
-        }
-#pragma unroll
-        for (int i = 0; i < kWords; i++) {
-            w[i] = 0;
-#pragma unroll
-            for (int j = 0; j < kPer; j++)
-                if (i * kPer + j < n) {
-                    if constexpr (kPer == 2) w[i] |= (uint32_t)__builtin_bit_cast(uint16_t, p[i * kPer + j]) << (16 * j);
-                    else w[i] = __builtin_bit_cast(uint32_t, p[i]);
-                }
-        }
-    }
-    __device__ __forceinline__ float operator[](int i) const {
-        if constexpr (kPer == 1) return __uint_as_float(w[i]);
-        else return to_f32(__builtin_bit_cast(T, (uint16_t)(w[i >> 1] >> (16 * (i & 1)))));
-    }
-};
-
 template <class T>
 __device__ __forceinline__ const T* at(const void* p, int64_t i) { return static_cast<const T*>(p) + i; }
 template <class T>
@@ -136,8 +109,8 @@ __global__ __launch_bounds__(norm_threads(TPR)) void k_block_norm(fmtc_norm p, N
 #pragma unroll
         for (int g = 0; g < VPT; g++) {
             const int c = 8 * (g * TPR + lane);
-            next_h[g].load(at<T>(p.d_h, row * p.ld_h + c), C - c);
-            if (p.d_y) next_y[g].load(at<T>(p.d_y, row * p.ld_y + c), C - c);
+            next_h[g].load(at<T>(p.d_h, row * p.ld_h), c, C);
+            if (p.d_y) next_y[g].load(at<T>(p.d_y, row * p.ld_y), c, C);
         }
     };
     // (the rows of a workgroup walk together: in a pass past the end a row's lanes work on the last row and store nothing)
@@ -177,9 +150,12 @@ __global__ __launch_bounds__(norm_threads(TPR)) void k_block_norm(fmtc_norm p, N
             if (p.d_w_post) {
                 float sum[1] = {0.f};
 #pragma unroll
-                for (int g = 0; g < VPT; g++)
+                for (int g = 0; g < VPT; g++) {
+                    float s = 0.f;
 #pragma unroll
-                    for (int i = 0; i < 8; i++) sum[0] = fmaf(y[g][i], y[g][i], sum[0]);
+                    for (int i = 0; i < 8; i++) s = fmaf(y[g][i], y[g][i], s);
+                    if (8 * (g * TPR + lane) < C) sum[0] += s;  // (lanes past the row hold values that are not theirs)
+                }
                 Sum::run(sum, slot, turn);
                 r_y = 1.f / sqrtf(sum[0] * rC + p.eps);
             }
@@ -203,16 +179,19 @@ __global__ __launch_bounds__(norm_threads(TPR)) void k_block_norm(fmtc_norm p, N
         if (p.d_w_pre) {
             float sum[1] = {0.f};
 #pragma unroll
-            for (int g = 0; g < VPT; g++)
+            for (int g = 0; g < VPT; g++) {
+                float s = 0.f;
 #pragma unroll
-                for (int i = 0; i < 8; i++) sum[0] = fmaf(h[g][i], h[g][i], sum[0]);
+                for (int i = 0; i < 8; i++) s = fmaf(h[g][i], h[g][i], s);
+                if (8 * (g * TPR + lane) < C) sum[0] += s;
+            }
             Sum::run(sum, slot, turn);
             r_h = 1.f / sqrtf(sum[0] * rC + p.eps);
 #pragma unroll
             for (int g = 0; g < VPT; g++) {
                 const int c = 8 * (g * TPR + lane);
 #pragma unroll
-                for (int i = 0; i < 8; i++) h[g][i] = h[g][i] * r_h * w_pre[g][i];
+                for (int i = 0; i < 8; i++) h[g][i] = c < C ? h[g][i] * r_h * w_pre[g][i] : 0.f;
                 if (!live) continue;
                 if (out.n) store8(at<T>(out.n, row * out.ld_n + c), C - c, h[g]);
                 if (out.codes.d_codes) {
@@ -250,11 +229,10 @@ __host__ __device__ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + 
 constexpr int lanes_of(int C) { return C <= 128 ? 16 : C <= 512 ? 64 : C <= 1024 ? 128 : C <= 2048 ? 256 : C <= 4096 ? 512 : 1024; }
 
 Strips make_strips(int64_t rows, int C, int64_t rows_per_gate) {
-    // as many strips as 256 compute units walk at a time with 16 wavefronts each, of at least 4 rows: the strips' sums stay a
-    // small part of the traffic
-    const int64_t want = 256 * 1024 / lanes_of(C);
-    int64_t each = ceil_div(rows, want);
-    if (each < 4) each = 4;
+    // as many strips as 256 compute units walk at a time with 16 wavefronts each: the sums of a large tensor's strips are a
+    // small part of the traffic, and a small tensor has every row on its way at once (500 x 960, a gate for every row: 17.7 us
+    // in strips of 4 rows)
+    const int64_t want = 256 * 1024 / lanes_of(C), each = ceil_div(rows, want);
     Strips s{};
     if (rows_per_gate <= 0) {
         s.rows = each;
@@ -358,12 +336,12 @@ __global__ __launch_bounds__(norm_threads(TPR), 4) void k_block_norm_backward(fm
 #pragma unroll
         for (int g = 0; g < VPT; g++) {
             const int c = 8 * (g * TPR + lane);
-            if (q.dh) next_t[g].load(at<T>(q.dh, row * q.ld_dh + c), C - c);
+            if (q.dh) next_t[g].load(at<T>(q.dh, row * q.ld_dh), c, C);
             if (q.dn) {
-                next_h[g].load(at<T>(p.d_h, row * p.ld_h + c), C - c);
-                next_n[g].load(at<T>(q.dn, row * q.ld_dn + c), C - c);
+                next_h[g].load(at<T>(p.d_h, row * p.ld_h), c, C);
+                next_n[g].load(at<T>(q.dn, row * q.ld_dn), c, C);
             }
-            if (p.d_y) next_y[g].load(at<T>(p.d_y, row * p.ld_y + c), C - c);
+            if (p.d_y) next_y[g].load(at<T>(p.d_y, row * p.ld_y), c, C);
         }
         if (p.d_w_post) next_r_y = q.stats[row];
         next_r_h = q.stats[p.rows + row];
@@ -389,7 +367,8 @@ __global__ __launch_bounds__(norm_threads(TPR), 4) void k_block_norm_backward(fm
         float t[VPT][8], hn[VPT][8], y[VPT][8];  // (dh + r_h a, to become the whole gradient; h' and y normalised)
         float sum[3] = {0.f, 0.f, 0.f};          // <a, hn>, <scale gate w_post yn, t>, <scale gate w_post yn, hn>
 #pragma unroll
-        for (int g = 0; g < VPT; g++)
+        for (int g = 0; g < VPT; g++) {
+            float part[3] = {0.f, 0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < 8; i++) {
                 t[g][i] = q.dh && live ? next_t[g][i] : 0.f;
@@ -398,17 +377,21 @@ __global__ __launch_bounds__(norm_threads(TPR), 4) void k_block_norm_backward(fm
                     hn[g][i] = next_h[g][i] * r_h;
                     const float dn = next_n[g][i], a = dn * w_pre[g][i];
                     d_pre[g][i] = fmaf(dn, hn[g][i], d_pre[g][i]);
-                    sum[0] = fmaf(a, hn[g][i], sum[0]);
+                    part[0] = fmaf(a, hn[g][i], part[0]);
                     t[g][i] = fmaf(r_h, a, t[g][i]);
                 }
                 y[g][i] = 0.f;
                 if (p.d_y && live) {
                     y[g][i] = next_y[g][i] * r_y;
                     const float c = gain[g][i] * y[g][i];
-                    sum[1] = fmaf(c, t[g][i], sum[1]);
-                    sum[2] = fmaf(c, hn[g][i], sum[2]);
+                    part[1] = fmaf(c, t[g][i], part[1]);
+                    part[2] = fmaf(c, hn[g][i], part[2]);
                 }
             }
+            if (8 * (g * TPR + lane) < C)  // (lanes past the row hold values that are not theirs)
+#pragma unroll
+                for (int k = 0; k < 3; k++) sum[k] += part[k];
+        }
         if (row + 1 < end) fetch(row + 1);
         Sum::run(sum, slot, turn);
         const float mean_h = r_h * sum[0] * rC, mean_y = p.d_w_post ? (sum[1] - mean_h * sum[2]) * rC : 0.f;

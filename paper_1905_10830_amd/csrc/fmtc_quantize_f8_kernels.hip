@@ -39,9 +39,16 @@ __global__ __launch_bounds__(256) void k_f8_quantize_tiles(const T* __restrict__
     const int t = threadIdx.x, lane_c = t & 15, lane_r = t >> 4;
     const int64_t rb = blockIdx.x / col_blocks, cb = blockIdx.x - rb * col_blocks;
     const int64_t row0 = rb * kF8Block + lane_r * 8, c0 = cb * kF8Block + lane_c * 8;
+    Raw<T> raw[8];
+#pragma unroll
+    for (int i = 0; i < 8; i++) raw[i].load(x + (row0 + i < rows ? row0 + i : rows - 1) * ld_x, c0, cols);
     float v[8][8];
 #pragma unroll
-    for (int i = 0; i < 8; i++) load8(x + (row0 + i) * ld_x + c0, row0 + i < rows ? cols - c0 : 0, v[i]);
+    for (int i = 0; i < 8; i++) {
+        raw[i].zero_unless(row0 + i < rows && c0 < cols);
+#pragma unroll
+        for (int j = 0; j < 8; j++) v[i][j] = raw[i][j];
+    }
 
     float inv_row[8];
     if constexpr (WEIGHTS) {
@@ -136,13 +143,23 @@ __global__ __launch_bounds__(256) void k_f8_quantize_tiles(const T* __restrict__
     }
 }
 
-__global__ __launch_bounds__(256) void k_column_sums(const float* __restrict__ part, int64_t n, int64_t cols,
-                                                     float* __restrict__ out, int accumulate) {
-    const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (c >= cols) return;
+// 32 columns a workgroup, 32 slices of the rows, added up in order
+__global__ __launch_bounds__(1024) void k_column_sums(const float* __restrict__ part, int64_t n, int64_t cols,
+                                                      float* __restrict__ out, int accumulate) {
+    __shared__ float slice[32][33];
+    const int col = threadIdx.x & 31, k = threadIdx.x >> 5;
+    const int64_t c = (int64_t)blockIdx.x * 32 + col;
     float sum = 0.f;
-    for (int64_t i = 0; i < n; i++) sum += part[i * cols + c];
-    out[c] = accumulate ? out[c] + sum : sum;
+    if (c < cols)
+#pragma unroll 4
+        for (int64_t i = k; i < n; i += 32) sum += part[i * cols + c];
+    slice[k][col] = sum;
+    __syncthreads();
+    if (k == 0 && c < cols) {
+#pragma unroll
+        for (int i = 1; i < 32; i++) sum += slice[i][col];
+        out[c] = accumulate ? out[c] + sum : sum;
+    }
 }
 
 __global__ __launch_bounds__(256) void k_fill_rows(float* __restrict__ out, int64_t cols, int64_t ld, int64_t n) {
@@ -177,7 +194,7 @@ hipError_t launch_f8_quantize(const void* d_x, int type, int64_t rows, int64_t c
 }
 
 hipError_t launch_column_sums(const float* d_part, int64_t n, int64_t cols, float* d_out, int accumulate, hipStream_t s) {
-    return launch(K_F8_QUANTIZE, k_column_sums, dim3((unsigned)((cols + 255) / 256)), dim3(256), 0, s, d_part, n, cols, d_out,
+    return launch(K_F8_QUANTIZE, k_column_sums, dim3((unsigned)((cols + 31) / 32)), dim3(1024), 0, s, d_part, n, cols, d_out,
                   accumulate);
 }
 
