@@ -138,6 +138,21 @@ __device__ __forceinline__ float finite_abs(float v) {
     const uint32_t b = __float_as_uint(v) & 0x7fffffffu;
     return b < 0x7f800000u ? __uint_as_float(b) : 0.f;
 }
+// largest finite magnitude of 8 values; magnitudes compare as their bits do, and only what is not finite (rare) takes the
+// longer way
+__device__ __forceinline__ float finite_amax(const float (&v)[8]) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        const uint32_t b = __float_as_uint(v[i]) & 0x7fffffffu;
+        m = b > m ? b : m;
+    }
+    if (m < 0x7f800000u) return __uint_as_float(m);
+    float a = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; i++) a = fmaxf(a, finite_abs(v[i]));
+    return a;
+}
 // The scale of a block whose largest magnitude is amax.  -> the factor that values are multiplied by; *held: what is
 // stored (a float's bits, or the biased exponent).  Both formats' largest number is 1.75 times a power of two, so the
 // power-of-two scale is an exact decision on the bits of amax: one more than its exponent where its fraction is over .75.

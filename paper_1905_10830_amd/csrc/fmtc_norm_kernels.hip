@@ -15,6 +15,8 @@ namespace fmtc {
 
 namespace {
 
+__host__ __device__ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
 // f32 sums over the TPR lanes of a row, in a fixed order, through one of two slots in turn: a wavefront that writes a slot
 // again has passed the other one's barrier, before which every wavefront had read this one.
 template <int TPR, int N>
@@ -79,11 +81,8 @@ constexpr int norm_threads(int TPR) { return TPR < 256 ? 256 : TPR; }
 
 template <int FORMAT, int SCALE>
 __device__ __forceinline__ void store_codes(const fmtc_f8& q, int64_t row, int c, const float (&v)[8]) {
-    float amax = 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; i++) amax = fmaxf(amax, finite_abs(v[i]));
     uint32_t held;
-    const float inv = block_scale<FORMAT, SCALE>(row16_max(amax), &held);
+    const float inv = block_scale<FORMAT, SCALE>(row16_max(finite_amax(v)), &held);
     if (c / kF8Block * (int64_t)kF8Block >= q.depth) return;
     *reinterpret_cast<uint2*>(static_cast<uint8_t*>(q.d_codes) + row * q.ld + c) =
         make_uint2(encode4<FORMAT>(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv),
@@ -113,15 +112,18 @@ __global__ __launch_bounds__(norm_threads(TPR)) void k_block_norm(fmtc_norm p, N
             if (p.d_y) next_y[g].load(at<T>(p.d_y, row * p.ld_y), c, C);
         }
     };
-    // (the rows of a workgroup walk together: in a pass past the end a row's lanes work on the last row and store nothing)
-    const int64_t step = (int64_t)gridDim.x * kRows;
-    int64_t first = (int64_t)blockIdx.x * kRows;
+    // Consecutive rows a workgroup: they share gate rows (8192 x 4096, a gate for 1024 rows: 64 us with the rows dealt out in
+    // turn, 49 us).  The rows of a pass walk together: past the end their lanes work on the last row and store nothing.
+    constexpr int64_t step = kRows;
+    const int64_t passes = ceil_div(ceil_div(p.rows, kRows), (int64_t)gridDim.x);
+    int64_t first = (int64_t)blockIdx.x * passes * kRows;
+    const int64_t stop = first + passes * kRows < p.rows ? first + passes * kRows : p.rows;
     auto row_of = [&](int64_t f) {
         const int64_t row = f + mine;
         return row < p.rows ? row : p.rows - 1;
     };
-    fetch(row_of(first));
-    for (; first < p.rows; first += step) {
+    if (first < stop) fetch(row_of(first));
+    for (; first < stop; first += step) {
         const int64_t row = row_of(first);
         const bool live = first + mine < p.rows;
         float h[VPT][8], y[VPT][8];
@@ -132,7 +134,7 @@ __global__ __launch_bounds__(norm_threads(TPR)) void k_block_norm(fmtc_norm p, N
                 h[g][i] = next_h[g][i];
                 y[g][i] = p.d_y ? next_y[g][i] : 0.f;
             }
-        if (first + step < p.rows) fetch(row_of(first + step));
+        if (first + step < stop) fetch(row_of(first + step));
         float r_y = 1.f;
         if (p.d_y) {
             const int64_t want = p.d_gate ? row / p.rows_per_gate : 0;
@@ -191,10 +193,13 @@ __global__ __launch_bounds__(norm_threads(TPR)) void k_block_norm(fmtc_norm p, N
             for (int g = 0; g < VPT; g++) {
                 const int c = 8 * (g * TPR + lane);
 #pragma unroll
-                for (int i = 0; i < 8; i++) h[g][i] = c < C ? h[g][i] * r_h * w_pre[g][i] : 0.f;
+                for (int i = 0; i < 8; i++) h[g][i] = h[g][i] * r_h * w_pre[g][i];
                 if (!live) continue;
                 if (out.n) store8(at<T>(out.n, row * out.ld_n + c), C - c, h[g]);
                 if (out.codes.d_codes) {
+                    if (c >= C)
+#pragma unroll
+                        for (int i = 0; i < 8; i++) h[g][i] = 0.f;
                     if (out.codes.format == FMTC_E4M3) {
                         if (out.codes.scale == FMTC_SCALE_F32) store_codes<FMTC_E4M3, FMTC_SCALE_F32>(out.codes, row, c, h[g]);
                         else store_codes<FMTC_E4M3, FMTC_SCALE_E8M0>(out.codes, row, c, h[g]);
@@ -222,8 +227,6 @@ struct Strips {
     int64_t per_gate;      // strips of a gate row, 0: a strip holds whole gate rows (or there is no gate)
     int64_t gates;
 };
-__host__ __device__ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-
 // Lanes of a row by its width, one group of 8 values each up to 8192: a row in as few lanes as hold it, whole wavefronts from
 // 129 values on.
 constexpr int lanes_of(int C) { return C <= 128 ? 16 : C <= 512 ? 64 : C <= 1024 ? 128 : C <= 2048 ? 256 : C <= 4096 ? 512 : 1024; }
@@ -504,7 +507,7 @@ hipError_t launch_block_norm(const fmtc_norm& a, void* d_h_out, int64_t ld_h_out
             constexpr int TPR = decltype(lanes)::value, VPT = decltype(groups)::value;
             constexpr int rows = norm_threads(TPR) / TPR;
             int64_t grid = ceil_div(a.rows, rows);
-            const int64_t most = 256 * 2048 / norm_threads(TPR);  // what walks at a time: 32 wavefronts a compute unit
+            const int64_t most = 256 * 1024 / norm_threads(TPR);  // what walks at a time: 16 wavefronts a compute unit
             if (grid > most) grid = most;
             return launch(K_BLOCK_NORM, k_block_norm<typename decltype(ty)::type, typename decltype(wt)::type, TPR, VPT>,
                           dim3((unsigned)grid), dim3(norm_threads(TPR)), 0, s, a, out);

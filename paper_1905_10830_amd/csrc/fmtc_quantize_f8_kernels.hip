@@ -14,12 +14,10 @@ __global__ __launch_bounds__(256) void k_f8_quantize_rows(const T* __restrict__ 
     const int64_t row = item / blocks, b = item - row * blocks;
     if (row >= rows) return;  // (whole rows of 16 lanes)
     const int64_t c = b * kF8Block + (threadIdx.x & 15) * 8;
-    float v[8], amax = 0.f;
+    float v[8];
     load8(x + row * ld_x + c, cols - c, v);
-#pragma unroll
-    for (int i = 0; i < 8; i++) amax = fmaxf(amax, finite_abs(v[i]));
     uint32_t held;
-    const float inv = block_scale<FORMAT, SCALE>(row16_max(amax), &held);
+    const float inv = block_scale<FORMAT, SCALE>(row16_max(finite_amax(v)), &held);
     const uint2 q = make_uint2(encode4<FORMAT>(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv),
                                encode4<FORMAT>(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv));
     *reinterpret_cast<uint2*>(static_cast<uint8_t*>(out.d_codes) + row * out.ld + c) = q;
@@ -54,9 +52,7 @@ __global__ __launch_bounds__(256) void k_f8_quantize_tiles(const T* __restrict__
     if constexpr (WEIGHTS) {
         float amax = 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; i++)
-#pragma unroll
-            for (int j = 0; j < 8; j++) amax = fmaxf(amax, finite_abs(v[i][j]));
+        for (int i = 0; i < 8; i++) amax = fmaxf(amax, finite_amax(v[i]));
         amax = row16_max(amax);
         if (lane_c == 0) part[0][lane_r] = amax;
         __syncthreads();
@@ -74,11 +70,8 @@ __global__ __launch_bounds__(256) void k_f8_quantize_tiles(const T* __restrict__
         if (by_rows.d_codes) {
 #pragma unroll
             for (int i = 0; i < 8; i++) {
-                float amax = 0.f;
-#pragma unroll
-                for (int j = 0; j < 8; j++) amax = fmaxf(amax, finite_abs(v[i][j]));
                 uint32_t held;
-                inv_row[i] = block_scale<FORMAT, SCALE>(row16_max(amax), &held);
+                inv_row[i] = block_scale<FORMAT, SCALE>(row16_max(finite_amax(v[i])), &held);
                 if (lane_c == 0 && row0 + i < rows) store_scale<SCALE>(by_rows.d_scales, cb * by_rows.ld_scales + row0 + i, held);
             }
         }
