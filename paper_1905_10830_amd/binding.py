@@ -740,8 +740,11 @@ def f8_matmul(a, b, bias=None, out=None, dtype=None, accumulate=False, workspace
     if out is None:
         if accumulate:
             raise ValueError("accumulate needs the output that is added to")
+        kind, ld = _dtype(dtype or torch.bfloat16), N
         out = _matrix(M, N, dtype or torch.bfloat16, a.codes.device)
-    ptr, kind, ld = _rows(out, "out", N, M, dtype)
+        ptr = out.data_ptr()
+    else:
+        ptr, kind, ld = _rows(out, "out", N, M, dtype)
     lib = load_library()
     workspace, ws, size = _workspace(workspace, lib.fmtc_f8_matmul_workspace_size(M, N, a.depth), out.device)
     _check(lib.fmtc_f8_matmul(_f8(a), _f8(b), _vector(bias, "bias", N, torch.float32), ptr, kind, ld, int(accumulate), ws, size,
@@ -787,14 +790,15 @@ def _norm_args(y, h, w_post, w_pre, gate, rows_per_gate, skip, scale, eps):
     h_ptr, kind, ld_h = _rows(h, "h")
     y_ptr, _, ld_y = _rows(y, "y", C, P, h.dtype) if y is not None else (None, 0, 0)
     like = w_pre if w_pre is not None else w_post if w_post is not None else gate
-    if like is not None and any(t is not None and t.dtype != like.dtype for t in (w_post, w_pre, gate)):
+    weights = None if like is None else like.dtype
+    if (w_post is not None and w_post.dtype != weights) or (gate is not None and gate.dtype != weights):
         raise ValueError("w_post, w_pre and gate have different types")
     if gate is None:
         rows_per_gate, gate_ptr = 0, None
     else:
         rows_per_gate = int(rows_per_gate) or max(P, 1)
         gate_ptr = _vector(gate, "gate", -(-P // rows_per_gate) * C if P and rows_per_gate > 0 else gate.numel())
-    return _Norm(P, C, kind, F32 if like is None else _dtype(like.dtype), 0, y_ptr, h_ptr, ld_y, ld_h, _vector(w_post, "w_post", C),
+    return _Norm(P, C, kind, F32 if like is None else _dtype(weights), 0, y_ptr, h_ptr, ld_y, ld_h, _vector(w_post, "w_post", C),
                  _vector(w_pre, "w_pre", C), gate_ptr, rows_per_gate, skip, scale, eps)
 
 
@@ -808,19 +812,29 @@ def block_norm(y, h, w_post, w_pre, gate=None, rows_per_gate=0, skip=1.0, scale=
 
     a = _norm_args(y, h, w_post, w_pre, gate, rows_per_gate, skip, scale, eps)
     P, C = h.shape
+    kind, device = h.dtype, h.device
+    h_ptr, h_ld = None, C
     if h_out is None:
-        h_out = _matrix(P, C, h.dtype, h.device)
+        h_out = _matrix(P, C, kind, device)
+        h_ptr = h_out.data_ptr()
     elif h_out is False:
         h_out = None
-    if n_out is None and w_pre is not None:
-        n_out = _matrix(P, C, h.dtype, h.device)
+    else:
+        h_ptr, _, h_ld = _rows(h_out, "h_out", C, P, kind)
+    n_ptr, n_ld, n_codes = None, C, None
+    if isinstance(n_out, F8):
+        n_codes = n_out
+    elif n_out is not None:
+        n_ptr, _, n_ld = _rows(n_out, "n_out", C, P, kind)
+    elif w_pre is not None:
+        n_out = _matrix(P, C, kind, device)
+        n_ptr = n_out.data_ptr()
     if stats is True:
-        stats = _matrix(2, P, torch.float32, h.device)
-    h_ptr, _, h_ld = _rows(h_out, "h_out", C, P, h.dtype) if h_out is not None else (None, 0, 0)
-    n_codes = n_out if isinstance(n_out, F8) else None
-    n_ptr, _, n_ld = _rows(n_out, "n_out", C, P, h.dtype) if n_out is not None and n_codes is None else (None, 0, 0)
-    _check(load_library().fmtc_block_norm(ctypes.byref(a), h_ptr, h_ld, n_ptr, n_ld, _f8(n_codes),
-                                          _vector(stats, "stats", 2 * P, torch.float32), _stream()))
+        stats = _matrix(2, P, torch.float32, device)
+        s_ptr = stats.data_ptr()
+    else:
+        s_ptr = _vector(stats, "stats", 2 * P, torch.float32)
+    _check(load_library().fmtc_block_norm(ctypes.byref(a), h_ptr, h_ld, n_ptr, n_ld, _f8(n_codes), s_ptr, _stream()))
     return h_out, n_out, stats
 
 
@@ -837,14 +851,21 @@ def block_norm_backward(dn, dh, y, h_out, stats, w_post, w_pre, gate=None, rows_
 
     a = _norm_args(y, h_out, w_post, w_pre, gate, rows_per_gate, skip, scale, 0.0)
     P, C = h_out.shape
+    kind, device = h_out.dtype, h_out.device
     new = lambda like: torch.empty_like(like, dtype=torch.float32) if like is not None else None  # noqa: E731
     dw_post, dw_pre, dgate = new(w_post), new(w_pre), new(gate)
+    of = lambda t, what: _rows(t, what, C, P, kind) if t is not None else (None, 0, 0)  # noqa: E731
+    (dn_p, _, dn_ld), (dh_p, _, dh_ld) = of(dn, "dn"), of(dh, "dh")
     if dy is None and y is not None:
-        dy = _matrix(P, C, h_out.dtype, h_out.device)
+        dy = _matrix(P, C, kind, device)
+        dy_p, dy_ld = dy.data_ptr(), C
+    else:
+        dy_p, _, dy_ld = of(dy, "dy")
     if dh_in is None:
-        dh_in = _matrix(P, C, h_out.dtype, h_out.device)
-    of = lambda t, what: _rows(t, what, C, P, h_out.dtype) if t is not None else (None, 0, 0)  # noqa: E731
-    (dn_p, _, dn_ld), (dh_p, _, dh_ld), (dy_p, _, dy_ld), (di_p, _, di_ld) = of(dn, "dn"), of(dh, "dh"), of(dy, "dy"), of(dh_in, "dh_in")
+        dh_in = _matrix(P, C, kind, device)
+        di_p, di_ld = dh_in.data_ptr(), C
+    else:
+        di_p, _, di_ld = of(dh_in, "dh_in")
     ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
     lib = load_library()
     workspace, ws, size = _workspace(workspace, lib.fmtc_block_norm_workspace_size(P, C, a.rows_per_gate), h_out.device)

@@ -134,9 +134,10 @@ struct Product {
 
 // Few rows: 16 MT rows x 16 NT columns per workgroup, operands straight from memory to registers; the workgroup's wavefronts
 // take the blocks of the depth in turn and add their sums up in LDS (in the wavefronts' order).  Bound by the weights' bytes;
-// the rows of a come out of the caches once for every workgroup, so two tiles of columns share them where that leaves a
-// workgroup for every compute unit.  1 x 8192 x 8192 13.4 us (5.0 TB/s), 13 rows 16.9 us, 1 x 4096 x 4096 5.9 us; loads of
-// two or four blocks ahead gain nothing (13.4 -> 14.5 us).
+// the rows of a come out of the caches once for every workgroup, so beyond 16 of them two tiles of columns share them where
+// that leaves a workgroup for every compute unit (64 x 8192 x 2048 12.7 -> 9.7 us; 13 x 8192 x 8192 would lose, 15.7 -> 19.5 us
+// with the weights in the memory-side cache).  1 x 8192 x 8192 13.4 us (5.0 TB/s), 1 x 4096 x 4096 5.9 us; loads of two or four
+// blocks ahead gain nothing (13.4 -> 14.5 us).
 constexpr int kRowsWaves = 8;
 template <int FORMAT, int WAY, int B_ROWS, int MT, int NT>
 __global__ __launch_bounds__(64 * kRowsWaves) void k_f8_matmul_rows(Product p, uint32_t n_tiles) {
@@ -513,8 +514,8 @@ Plan make_plan(int64_t M, int64_t N, int64_t K, bool wide) {
     return best;
 }
 
-// (few rows) two tiles of columns a workgroup
-bool rows_in_pairs(int64_t M, int64_t N) { return M > 8 && (double)((M + 63) / 64) * ((N + 31) / 32) >= kCus; }
+// (first kernel, more than 16 rows) two tiles of columns a workgroup
+bool rows_in_pairs(int64_t M, int64_t N) { return M > 16 && (double)((M + 63) / 64) * ((N + 31) / 32) >= kCus; }
 
 int64_t split_ld(int64_t N) { return (N + 3) / 4 * 4; }
 
@@ -570,9 +571,8 @@ hipError_t launch_f8_matmul(const fmtc_f8& a, const fmtc_f8& b, const float* d_b
                     return launch(K_F8_MATMUL, k_f8_matmul_rows<F, W, B, MT, NT>, dim3((unsigned)(n_tiles * ((p.M + 16 * MT - 1) / (16 * MT)))),
                                   dim3(64 * kRowsWaves), 0, s, p, (uint32_t)n_tiles);
                 };
-                const bool pairs = rows_in_pairs(p.M, p.N);
-                if (p.M <= 16) return pairs ? rows(Int<1>{}, Int<2>{}) : rows(Int<1>{}, Int<1>{});
-                return pairs ? rows(Int<4>{}, Int<2>{}) : rows(Int<4>{}, Int<1>{});
+                if (p.M <= 16) return rows(Int<1>{}, Int<1>{});
+                return rows_in_pairs(p.M, p.N) ? rows(Int<4>{}, Int<2>{}) : rows(Int<4>{}, Int<1>{});
             });
         });
     });
