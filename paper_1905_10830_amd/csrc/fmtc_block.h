@@ -53,20 +53,8 @@ __device__ __forceinline__ bf16 from_f32<bf16>(float v) {
     return bf16{__builtin_bit_cast(uint16_t, r)};
 }
 
-// 8 consecutive values of which the first n exist (0 for the others).  Rows need not be aligned beyond their own type: the
-// hardware takes wide accesses at any address.
-template <class T>
-__device__ __forceinline__ void load8(const T* p, int64_t n, float (&v)[8]) {
-    T t[8];
-    if (n >= 8) {
-        __builtin_memcpy(t, p, sizeof t);
-#pragma unroll
-        for (int i = 0; i < 8; i++) v[i] = to_f32(t[i]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; i++) v[i] = i < n ? to_f32(p[i]) : 0.f;
-    }
-}
+// the first n of 8 consecutive values; rows need not be aligned beyond their own type: the hardware takes wide accesses at
+// any address
 template <class T>
 __device__ __forceinline__ void store8(T* p, int64_t n, const float (&v)[8]) {
     if (n >= 8) {
@@ -86,12 +74,16 @@ template <class T>
 struct Raw {
     static constexpr int kWords = 2 * sizeof(T), kPer = 4 / sizeof(T);
     uint32_t w[kWords];
-    // values c .. c + 7 of a row of C.  One load without a branch, so that many can be on their way together: lanes past the
-    // row read its first values, which their caller has no use for.  Only the lane at the end of a row whose length is no
-    // multiple of 8 goes value by value (0 beyond the end).
+    // Values c .. c + 7 of a row of C: one load without a branch, so that many can be on their way together.  At the end of a
+    // row whose length is no multiple of 8 it takes the row's last 8 values; lanes past the row read its first ones, which
+    // their caller has no use for.
+    template <bool RAGGED>
     __device__ __forceinline__ void load(const T* row, int64_t c, int64_t C) {
-        if (C >= 8) __builtin_memcpy(w, row + (c + 8 <= C ? c : 0), sizeof w);
-        if (c < C && c + 8 > C) {
+        if constexpr (!RAGGED) {
+            __builtin_memcpy(w, row + (c < C ? c : 0), sizeof w);
+        } else if (C >= 8) {
+            __builtin_memcpy(w, row + (c + 8 <= C ? c : c < C ? C - 8 : 0), sizeof w);
+        } else {
 #pragma unroll
             for (int i = 0; i < kWords; i++) {
                 w[i] = 0;
@@ -104,6 +96,27 @@ struct Raw {
             }
         }
     }
+    // when the values are there, in rows whose length is no multiple of 8 (kernels are built for either: without the question
+    // the loads of aligned rows run up to a tenth faster): those at the end of a row to their places, 0 behind them
+    __device__ __forceinline__ void settle(int64_t c, int64_t C) {
+        if (C < 8) return;
+        const int by = c < C && c + 8 > C ? (int)(c + 8 - C) : 0;
+        int step = kWords / 2;
+#pragma unroll
+        for (int bit = 4; bit * kPer >= kPer * kPer; bit >>= 1, step >>= 1)
+#pragma unroll
+            for (int i = 0; i < kWords; i++) {
+                const uint32_t from = i + step < kWords ? w[i + step] : 0u;
+                w[i] = by & bit ? from : w[i];
+            }
+        if constexpr (kPer == 2) {
+#pragma unroll
+            for (int i = 0; i < kWords; i++) {
+                const uint32_t above = i + 1 < kWords ? w[i + 1] : 0u;
+                w[i] = by & 1 ? w[i] >> 16 | above << 16 : w[i];
+            }
+        }
+    }
     __device__ __forceinline__ void zero_unless(bool live) {
 #pragma unroll
         for (int i = 0; i < kWords; i++) w[i] = live ? w[i] : 0u;
@@ -113,6 +126,14 @@ struct Raw {
         else return to_f32(__builtin_bit_cast(T, (uint16_t)(w[i >> 1] >> (16 * (i & 1)))));
     }
 };
+template <bool RAGGED, class T>
+__device__ __forceinline__ void load8(const T* row, int64_t c, int64_t C, float (&v)[8]) {
+    Raw<T> raw;
+    raw.template load<RAGGED>(row, c, C);
+    if constexpr (RAGGED) raw.settle(c, C);
+#pragma unroll
+    for (int i = 0; i < 8; i++) v[i] = raw[i];
+}
 
 // a reduction over a row of 16 lanes; every lane of the row gets the result
 template <int CTRL>

@@ -54,12 +54,12 @@ __device__ __forceinline__ const T* at(const void* p, int64_t i) { return static
 template <class T>
 __device__ __forceinline__ T* at(void* p, int64_t i) { return static_cast<T*>(p) + i; }
 
-template <class W, int TPR, int VPT>
+template <class W, int TPR, int VPT, bool RAGGED>
 __device__ __forceinline__ void load_params(const void* p, int64_t row, int C, int lane, float (&v)[VPT][8]) {
 #pragma unroll
     for (int g = 0; g < VPT; g++) {
         const int c = 8 * (g * TPR + lane);
-        load8(at<W>(p, row * C + c), C - c, v[g]);
+        load8<RAGGED>(at<W>(p, row * C), c, C, v[g]);
     }
 }
 
@@ -90,7 +90,7 @@ __device__ __forceinline__ void store_codes(const fmtc_f8& q, int64_t row, int c
     if (c % kF8Block == 0) store_scale<SCALE>(q.d_scales, c / kF8Block * q.ld_scales + row, held);
 }
 
-template <class T, class W, int TPR, int VPT>
+template <class T, class W, int TPR, int VPT, bool RAGGED>
 __global__ __launch_bounds__(norm_threads(TPR)) void k_block_norm(fmtc_norm p, NormOut out) {
     constexpr int kRows = norm_threads(TPR) / TPR;
     using Sum = RowSums<TPR, 1>;
@@ -102,14 +102,14 @@ __global__ __launch_bounds__(norm_threads(TPR)) void k_block_norm(fmtc_norm p, N
     const float rC = 1.f / (float)C;
     float w_pre[VPT][8], gate[VPT][8];
     int64_t gate_row = -1;
-    if (p.d_w_pre) load_params<W, TPR, VPT>(p.d_w_pre, 0, C, lane, w_pre);
+    if (p.d_w_pre) load_params<W, TPR, VPT, RAGGED>(p.d_w_pre, 0, C, lane, w_pre);
     Raw<T> next_h[VPT], next_y[VPT];
     auto fetch = [&](int64_t row) {
 #pragma unroll
         for (int g = 0; g < VPT; g++) {
             const int c = 8 * (g * TPR + lane);
-            next_h[g].load(at<T>(p.d_h, row * p.ld_h), c, C);
-            if (p.d_y) next_y[g].load(at<T>(p.d_y, row * p.ld_y), c, C);
+            next_h[g].template load<RAGGED>(at<T>(p.d_h, row * p.ld_h), c, C);
+            if (p.d_y) next_y[g].template load<RAGGED>(at<T>(p.d_y, row * p.ld_y), c, C);
         }
     };
     // Consecutive rows a workgroup: they share gate rows (8192 x 4096, a gate for 1024 rows: 64 us with the rows dealt out in
@@ -126,6 +126,12 @@ __global__ __launch_bounds__(norm_threads(TPR)) void k_block_norm(fmtc_norm p, N
     for (; first < stop; first += step) {
         const int64_t row = row_of(first);
         const bool live = first + mine < p.rows;
+        if constexpr (RAGGED)
+#pragma unroll
+            for (int g = 0; g < VPT; g++) {
+                next_h[g].settle(8 * (g * TPR + lane), C);
+                if (p.d_y) next_y[g].settle(8 * (g * TPR + lane), C);
+            }
         float h[VPT][8], y[VPT][8];
 #pragma unroll
         for (int g = 0; g < VPT; g++)
@@ -135,14 +141,15 @@ __global__ __launch_bounds__(norm_threads(TPR)) void k_block_norm(fmtc_norm p, N
                 y[g][i] = p.d_y ? next_y[g][i] : 0.f;
             }
         if (first + step < stop) fetch(row_of(first + step));
+        __builtin_amdgcn_sched_barrier(0);  // (the loads stay here, a row ahead of their use: 125 -> 115 us, 16384 x 4096)
         float r_y = 1.f;
         if (p.d_y) {
             const int64_t want = p.d_gate ? row / p.rows_per_gate : 0;
             if (want != gate_row) {  // scale gate w_post: what the normalised y is multiplied by
                 gate_row = want;
-                if (p.d_gate) load_params<W, TPR, VPT>(p.d_gate, want, C, lane, gate);
+                if (p.d_gate) load_params<W, TPR, VPT, RAGGED>(p.d_gate, want, C, lane, gate);
                 float w[VPT][8];
-                if (p.d_w_post) load_params<W, TPR, VPT>(p.d_w_post, 0, C, lane, w);
+                if (p.d_w_post) load_params<W, TPR, VPT, RAGGED>(p.d_w_post, 0, C, lane, w);
 #pragma unroll
                 for (int g = 0; g < VPT; g++)
 #pragma unroll
@@ -266,7 +273,7 @@ struct NormGrads {
     Strips strips;
 };
 
-template <class T, class W, int TPR, int VPT>
+template <class T, class W, int TPR, int VPT, bool RAGGED>
 __global__ __launch_bounds__(norm_threads(TPR), 4) void k_block_norm_backward(fmtc_norm p, NormGrads q) {
     constexpr int kThreads = norm_threads(TPR), kRows = kThreads / TPR;
     constexpr bool kHold = VPT == 1;  // the weights stay in registers; else they come from the cache for every row
@@ -300,14 +307,14 @@ __global__ __launch_bounds__(norm_threads(TPR), 4) void k_block_norm_backward(fm
             for (int i = 0; i < 8; i++) gain[g][i] = p.scale;
         float v[VPT][8];
         if (p.d_gate) {
-            load_params<W, TPR, VPT>(p.d_gate, gate_row, C, lane, v);
+            load_params<W, TPR, VPT, RAGGED>(p.d_gate, gate_row, C, lane, v);
 #pragma unroll
             for (int g = 0; g < VPT; g++)
 #pragma unroll
                 for (int i = 0; i < 8; i++) gain[g][i] *= v[g][i];
         }
         if (p.d_w_post) {
-            load_params<W, TPR, VPT>(p.d_w_post, 0, C, lane, v);
+            load_params<W, TPR, VPT, RAGGED>(p.d_w_post, 0, C, lane, v);
 #pragma unroll
             for (int g = 0; g < VPT; g++)
 #pragma unroll
@@ -322,8 +329,8 @@ __global__ __launch_bounds__(norm_threads(TPR), 4) void k_block_norm_backward(fm
             float gate[8], w_post[8];
 #pragma unroll
             for (int i = 0; i < 8; i++) gate[i] = w_post[i] = 1.f;
-            if (p.d_gate) load8(at<W>(p.d_gate, gate_row * C + c), C - c, gate);
-            if (p.d_w_post) load8(at<W>(p.d_w_post, c), C - c, w_post);
+            if (p.d_gate) load8<RAGGED>(at<W>(p.d_gate, gate_row * C), c, C, gate);
+            if (p.d_w_post) load8<RAGGED>(at<W>(p.d_w_post, 0), c, C, w_post);
 #pragma unroll
             for (int i = 0; i < 8; i++) {
                 d_post[g][i] = fmaf(gate[i], z[g][i], d_post[g][i]);
@@ -339,12 +346,12 @@ __global__ __launch_bounds__(norm_threads(TPR), 4) void k_block_norm_backward(fm
 #pragma unroll
         for (int g = 0; g < VPT; g++) {
             const int c = 8 * (g * TPR + lane);
-            if (q.dh) next_t[g].load(at<T>(q.dh, row * q.ld_dh), c, C);
+            if (q.dh) next_t[g].template load<RAGGED>(at<T>(q.dh, row * q.ld_dh), c, C);
             if (q.dn) {
-                next_h[g].load(at<T>(p.d_h, row * p.ld_h), c, C);
-                next_n[g].load(at<T>(q.dn, row * q.ld_dn), c, C);
+                next_h[g].template load<RAGGED>(at<T>(p.d_h, row * p.ld_h), c, C);
+                next_n[g].template load<RAGGED>(at<T>(q.dn, row * q.ld_dn), c, C);
             }
-            if (p.d_y) next_y[g].load(at<T>(p.d_y, row * p.ld_y), c, C);
+            if (p.d_y) next_y[g].template load<RAGGED>(at<T>(p.d_y, row * p.ld_y), c, C);
         }
         if (p.d_w_post) next_r_y = q.stats[row];
         next_r_h = q.stats[p.rows + row];
@@ -352,7 +359,7 @@ __global__ __launch_bounds__(norm_threads(TPR), 4) void k_block_norm_backward(fm
     if (first < end) fetch(first);
     if (p.d_gate && first < end) gate_row = first / p.rows_per_gate;
     if constexpr (kHold) {
-        if (p.d_w_pre) load_params<W, TPR, VPT>(p.d_w_pre, 0, C, lane, w_pre);
+        if (p.d_w_pre) load_params<W, TPR, VPT, RAGGED>(p.d_w_pre, 0, C, lane, w_pre);
         load_gain();
     }
     for (int64_t k = 0; k < q.strips.rows; k++) {
@@ -363,15 +370,24 @@ __global__ __launch_bounds__(norm_threads(TPR), 4) void k_block_norm_backward(fm
             if constexpr (kHold) load_gain();
         }
         if constexpr (!kHold) {
-            if (p.d_w_pre) load_params<W, TPR, VPT>(p.d_w_pre, 0, C, lane, w_pre);
+            if (p.d_w_pre) load_params<W, TPR, VPT, RAGGED>(p.d_w_pre, 0, C, lane, w_pre);
             load_gain();
         }
+        if constexpr (RAGGED)
+#pragma unroll
+            for (int g = 0; g < VPT; g++) {
+                const int c = 8 * (g * TPR + lane);
+                if (q.dh) next_t[g].settle(c, C);
+                if (q.dn) next_h[g].settle(c, C), next_n[g].settle(c, C);
+                if (p.d_y) next_y[g].settle(c, C);
+            }
         const float r_y = next_r_y, r_h = next_r_h;
         float t[VPT][8], hn[VPT][8], y[VPT][8];  // (dh + r_h a, to become the whole gradient; h' and y normalised)
         float sum[3] = {0.f, 0.f, 0.f};          // <a, hn>, <scale gate w_post yn, t>, <scale gate w_post yn, hn>
 #pragma unroll
         for (int g = 0; g < VPT; g++) {
             float part[3] = {0.f, 0.f, 0.f};
+            const int c0 = 8 * (g * TPR + lane);
 #pragma unroll
             for (int i = 0; i < 8; i++) {
                 t[g][i] = q.dh && live ? next_t[g][i] : 0.f;
@@ -391,7 +407,7 @@ __global__ __launch_bounds__(norm_threads(TPR), 4) void k_block_norm_backward(fm
                     part[2] = fmaf(c, hn[g][i], part[2]);
                 }
             }
-            if (8 * (g * TPR + lane) < C)  // (lanes past the row hold values that are not theirs)
+            if (c0 < C)  // (lanes past the row hold values that are not theirs)
 #pragma unroll
                 for (int k = 0; k < 3; k++) sum[k] += part[k];
         }
@@ -480,14 +496,16 @@ __global__ __launch_bounds__(1024) void k_strip_sums(const float* __restrict__ p
 
 template <class F>
 hipError_t with_width(int C, F&& f) {
-    switch (lanes_of(C)) {
-        case 16: return f(Int<16>{}, Int<1>{});
-        case 64: return f(Int<64>{}, Int<1>{});
-        case 128: return f(Int<128>{}, Int<1>{});
-        case 256: return f(Int<256>{}, Int<1>{});
-        case 512: return f(Int<512>{}, Int<1>{});
-        default: return C <= 8192 ? f(Int<1024>{}, Int<1>{}) : f(Int<1024>{}, Int<2>{});
-    }
+    return with_bit(C % 8 != 0, [&](auto ragged) {
+        switch (lanes_of(C)) {
+            case 16: return f(Int<16>{}, Int<1>{}, ragged);
+            case 64: return f(Int<64>{}, Int<1>{}, ragged);
+            case 128: return f(Int<128>{}, Int<1>{}, ragged);
+            case 256: return f(Int<256>{}, Int<1>{}, ragged);
+            case 512: return f(Int<512>{}, Int<1>{}, ragged);
+            default: return C <= 8192 ? f(Int<1024>{}, Int<1>{}, ragged) : f(Int<1024>{}, Int<2>{}, ragged);
+        }
+    });
 }
 template <class F>
 hipError_t with_types(int type, int weight_type, F&& f) {
@@ -503,13 +521,14 @@ hipError_t launch_block_norm(const fmtc_norm& a, void* d_h_out, int64_t ld_h_out
                              const fmtc_f8* n_codes, float* d_stats, hipStream_t s) {
     NormOut out{d_h_out, d_n, ld_h_out, ld_n, n_codes ? *n_codes : fmtc_f8{}, d_stats};
     return with_types(a.type, a.weight_type, [&](auto ty, auto wt) {
-        return with_width(a.C, [&](auto lanes, auto groups) {
+        return with_width(a.C, [&](auto lanes, auto groups, auto ragged) {
             constexpr int TPR = decltype(lanes)::value, VPT = decltype(groups)::value;
+            constexpr bool RAGGED = decltype(ragged)::value;
             constexpr int rows = norm_threads(TPR) / TPR;
             int64_t grid = ceil_div(a.rows, rows);
             const int64_t most = 256 * 1024 / norm_threads(TPR);  // what walks at a time: 16 wavefronts a compute unit
             if (grid > most) grid = most;
-            return launch(K_BLOCK_NORM, k_block_norm<typename decltype(ty)::type, typename decltype(wt)::type, TPR, VPT>,
+            return launch(K_BLOCK_NORM, k_block_norm<typename decltype(ty)::type, typename decltype(wt)::type, TPR, VPT, RAGGED>,
                           dim3((unsigned)grid), dim3(norm_threads(TPR)), 0, s, a, out);
         });
     });
@@ -533,9 +552,10 @@ hipError_t launch_block_norm_backward(const fmtc_norm& a, const float* d_stats, 
     NormGrads q{d_stats, d_dn, d_dh, d_dy, d_dh_in, ld_dn, ld_dh, ld_dy, ld_dh_in,
                 d_dw_post ? post : nullptr, d_dw_pre ? pre : nullptr, gate, d_dgate, st};
     hipError_t e = with_types(a.type, a.weight_type, [&](auto ty, auto wt) {
-        return with_width(a.C, [&](auto lanes, auto per) {
+        return with_width(a.C, [&](auto lanes, auto per, auto ragged) {
             constexpr int TPR = decltype(lanes)::value, VPT = decltype(per)::value;
-            return launch(K_BLOCK_NORM_BACKWARD, k_block_norm_backward<typename decltype(ty)::type, typename decltype(wt)::type, TPR, VPT>,
+            constexpr bool RAGGED = decltype(ragged)::value;
+            return launch(K_BLOCK_NORM_BACKWARD, k_block_norm_backward<typename decltype(ty)::type, typename decltype(wt)::type, TPR, VPT, RAGGED>,
                           dim3((unsigned)groups), dim3(norm_threads(TPR)), 0, s, a, q);
         });
     });

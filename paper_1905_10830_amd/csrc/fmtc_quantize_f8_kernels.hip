@@ -7,7 +7,7 @@ namespace fmtc {
 namespace {
 
 // 1 x 128 blocks along the rows: 16 lanes hold a block, 8 values each.
-template <class T, int FORMAT, int SCALE>
+template <class T, int FORMAT, int SCALE, bool RAGGED>
 __global__ __launch_bounds__(256) void k_f8_quantize_rows(const T* __restrict__ x, int64_t rows, int64_t cols, int64_t ld_x,
                                                           uint32_t blocks, fmtc_f8 out) {
     const int64_t item = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
@@ -15,7 +15,10 @@ __global__ __launch_bounds__(256) void k_f8_quantize_rows(const T* __restrict__ 
     if (row >= rows) return;  // (whole rows of 16 lanes)
     const int64_t c = b * kF8Block + (threadIdx.x & 15) * 8;
     float v[8];
-    load8(x + row * ld_x + c, cols - c, v);
+    load8<RAGGED>(x + row * ld_x, c, cols, v);
+    if (c >= cols)
+#pragma unroll
+        for (int i = 0; i < 8; i++) v[i] = 0.f;
     uint32_t held;
     const float inv = block_scale<FORMAT, SCALE>(row16_max(finite_amax(v)), &held);
     const uint2 q = make_uint2(encode4<FORMAT>(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv),
@@ -27,7 +30,7 @@ __global__ __launch_bounds__(256) void k_f8_quantize_rows(const T* __restrict__ 
 // A tile of 128 x 128 values per workgroup, kept in registers (8 rows x 8 columns a lane) between the maxima and the codes:
 // the second output costs no second read.  The transposed codes go through LDS, 8 bytes (8 rows of a column) at a time, at
 // places exchanged so that neither the columns' writes nor the rows' reads of 16 lanes meet in a bank.
-template <class T, int FORMAT, int SCALE, bool WEIGHTS>
+template <class T, int FORMAT, int SCALE, bool WEIGHTS, bool RAGGED>
 __global__ __launch_bounds__(256) void k_f8_quantize_tiles(const T* __restrict__ x, int64_t rows, int64_t cols, int64_t ld_x,
                                                            uint32_t col_blocks, fmtc_f8 by_rows, fmtc_f8 by_cols,
                                                            float* __restrict__ col_sums) {
@@ -39,7 +42,10 @@ __global__ __launch_bounds__(256) void k_f8_quantize_tiles(const T* __restrict__
     const int64_t row0 = rb * kF8Block + lane_r * 8, c0 = cb * kF8Block + lane_c * 8;
     Raw<T> raw[8];
 #pragma unroll
-    for (int i = 0; i < 8; i++) raw[i].load(x + (row0 + i < rows ? row0 + i : rows - 1) * ld_x, c0, cols);
+    for (int i = 0; i < 8; i++) raw[i].template load<RAGGED>(x + (row0 + i < rows ? row0 + i : rows - 1) * ld_x, c0, cols);
+    if constexpr (RAGGED)
+#pragma unroll
+        for (int i = 0; i < 8; i++) raw[i].settle(c0, cols);
     float v[8][8];
 #pragma unroll
     for (int i = 0; i < 8; i++) {
@@ -171,16 +177,17 @@ hipError_t launch_f8_quantize(const void* d_x, int type, int64_t rows, int64_t c
         using T = typename decltype(ty)::type;
         return with_bit(any.format, [&](auto fm) {
             return with_bit(any.scale, [&](auto sc) {
-                constexpr int F = decltype(fm)::value, S = decltype(sc)::value;
-                const T* x = static_cast<const T*>(d_x);
-                if (!by_cols && any.block_rows == 1)
-                    return launch(K_F8_QUANTIZE, k_f8_quantize_rows<T, F, S>, dim3((unsigned)((rows * col_blocks + 15) / 16)),
-                                  dim3(256), 0, s, x, rows, cols, ld_x, (uint32_t)col_blocks, a);
-                const dim3 grid((unsigned)(row_blocks * col_blocks));
-                return any.block_rows == 1 ? launch(K_F8_QUANTIZE, k_f8_quantize_tiles<T, F, S, false>, grid, dim3(256), 0, s, x, rows,
-                                                    cols, ld_x, (uint32_t)col_blocks, a, b, d_col_sums)
-                                           : launch(K_F8_QUANTIZE, k_f8_quantize_tiles<T, F, S, true>, grid, dim3(256), 0, s, x, rows,
-                                                    cols, ld_x, (uint32_t)col_blocks, a, b, d_col_sums);
+                return with_bit(cols % 8 != 0, [&](auto rg) {
+                    constexpr int F = decltype(fm)::value, S = decltype(sc)::value;
+                    constexpr bool R = decltype(rg)::value;
+                    const T* x = static_cast<const T*>(d_x);
+                    if (!by_cols && any.block_rows == 1)
+                        return launch(K_F8_QUANTIZE, k_f8_quantize_rows<T, F, S, R>, dim3((unsigned)((rows * col_blocks + 15) / 16)),
+                                      dim3(256), 0, s, x, rows, cols, ld_x, (uint32_t)col_blocks, a);
+                    const dim3 grid((unsigned)(row_blocks * col_blocks));
+                    auto kernel = any.block_rows == 1 ? k_f8_quantize_tiles<T, F, S, false, R> : k_f8_quantize_tiles<T, F, S, true, R>;
+                    return launch(K_F8_QUANTIZE, kernel, grid, dim3(256), 0, s, x, rows, cols, ld_x, (uint32_t)col_blocks, a, b, d_col_sums);
+                });
             });
         });
     });
