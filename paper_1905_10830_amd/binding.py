@@ -839,6 +839,7 @@ def block_norm(y, h, w_post, w_pre, gate=None, rows_per_gate=0, skip=1.0, scale=
 
 
 def block_norm_workspace_size(P, C, rows_per_gate=0):
+    """Bytes for block_norm_backward; rows_per_gate: 0 without a gate, P with one row for all."""
     return load_library().fmtc_block_norm_workspace_size(P, C, rows_per_gate)
 
 
