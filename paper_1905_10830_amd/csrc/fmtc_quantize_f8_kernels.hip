@@ -27,47 +27,54 @@ __global__ __launch_bounds__(256) void k_f8_quantize_rows(const T* __restrict__ 
     if ((threadIdx.x & 15) == 0) store_scale<SCALE>(out.d_scales, b * out.ld_scales + row, held);
 }
 
-// A tile of 128 x 128 values per workgroup, kept in registers (8 rows x 8 columns a lane) between the maxima and the codes:
-// the second output costs no second read.  The transposed codes go through LDS, 8 bytes (8 rows of a column) at a time, at
-// places exchanged so that neither the columns' writes nor the rows' reads of 16 lanes meet in a bank.  8192 x 4096 bf16, both
-// outputs: 25.9 us (5.2 TB/s), 128 x 128 blocks 22.1 us; 8192 x 4095, whose rows begin at odd places, 34.4 us.
+// A tile of 128 x 128 values per workgroup, kept in registers (4 rows x 8 columns a lane) between the maxima and the codes:
+// the second output costs no second read.  The transposed codes go through LDS, 4 bytes (4 rows of a column) at a time, at
+// places exchanged so that the columns' writes and the rows' reads of 16 lanes spread over the banks.  8192 x 4096 bf16, both
+// outputs: 24.1 us (5.6 TB/s), 128 x 128 blocks 21.5 us; 8192 x 4095, whose rows begin at odd places, 32.0 us.  With 8 rows a
+// lane and half the lanes a tile's own time shows: 1024 x 2048 6.1 us, as here 5.0 us; 8192 x 4096 25.7 us.
+constexpr int kTileThreads = 512;
+
 template <class T, int FORMAT, int SCALE, bool WEIGHTS, bool RAGGED>
-__global__ __launch_bounds__(256) void k_f8_quantize_tiles(const T* __restrict__ x, int64_t rows, int64_t cols, int64_t ld_x,
+__global__ __launch_bounds__(kTileThreads) void k_f8_quantize_tiles(const T* __restrict__ x, int64_t rows, int64_t cols, int64_t ld_x,
                                                            uint32_t col_blocks, fmtc_f8 by_rows, fmtc_f8 by_cols,
                                                            float* __restrict__ col_sums) {
-    __shared__ float part[16][kF8Block];
+    constexpr int R = 4, kLaneRows = kTileThreads / 16;
+    static_assert(R * kLaneRows == kF8Block);
+    __shared__ float part[kLaneRows][kF8Block];
     __shared__ float col_inv[kF8Block];
-    __shared__ uint2 tile[kF8Block][16];
+    __shared__ __align__(16) uint32_t tile[kF8Block][kF8Block / 4];
     const int t = threadIdx.x, lane_c = t & 15, lane_r = t >> 4;
     const int64_t rb = blockIdx.x / col_blocks, cb = blockIdx.x - rb * col_blocks;
-    const int64_t row0 = rb * kF8Block + lane_r * 8, c0 = cb * kF8Block + lane_c * 8;
-    Raw<T> raw[8];
+    const int64_t row0 = rb * kF8Block + lane_r * R, c0 = cb * kF8Block + lane_c * 8;
+    Raw<T> raw[R];
 #pragma unroll
-    for (int i = 0; i < 8; i++) raw[i].template load<RAGGED>(x + (row0 + i < rows ? row0 + i : rows - 1) * ld_x, c0, cols);
+    for (int i = 0; i < R; i++) raw[i].template load<RAGGED>(x + (row0 + i < rows ? row0 + i : rows - 1) * ld_x, c0, cols);
     if constexpr (RAGGED)
 #pragma unroll
-        for (int i = 0; i < 8; i++) raw[i].settle(c0, cols);
-    float v[8][8];
+        for (int i = 0; i < R; i++) raw[i].settle(c0, cols);
+    float v[R][8];
 #pragma unroll
-    for (int i = 0; i < 8; i++) {
+    for (int i = 0; i < R; i++) {
         raw[i].zero_unless(row0 + i < rows && c0 < cols);
 #pragma unroll
         for (int j = 0; j < 8; j++) v[i][j] = raw[i][j];
     }
 
-    float inv_row[8];
+    float inv_row[R];
     if constexpr (WEIGHTS) {
         float amax = 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; i++) amax = fmaxf(amax, finite_amax(v[i]));
+        for (int i = 0; i < R; i++) amax = fmaxf(amax, finite_amax(v[i]));
         amax = row16_max(amax);
         if (lane_c == 0) part[0][lane_r] = amax;
         __syncthreads();
-        amax = row16_max(part[0][lane_c]);
+#pragma unroll
+        for (int r = 0; r < kLaneRows; r += 16) amax = fmaxf(amax, part[0][r + lane_c]);
+        amax = row16_max(amax);
         uint32_t held;
         const float inv = block_scale<FORMAT, SCALE>(amax, &held);
 #pragma unroll
-        for (int i = 0; i < 8; i++) inv_row[i] = inv;
+        for (int i = 0; i < R; i++) inv_row[i] = inv;
         if (t < kF8Block) col_inv[t] = inv;
         if (t == 0) {
             if (by_rows.d_codes) store_scale<SCALE>(by_rows.d_scales, cb * by_rows.ld_scales + rb, held);
@@ -76,7 +83,7 @@ __global__ __launch_bounds__(256) void k_f8_quantize_tiles(const T* __restrict__
     } else {
         if (by_rows.d_codes) {
 #pragma unroll
-            for (int i = 0; i < 8; i++) {
+            for (int i = 0; i < R; i++) {
                 uint32_t held;
                 inv_row[i] = block_scale<FORMAT, SCALE>(row16_max(finite_amax(v[i])), &held);
                 if (lane_c == 0 && row0 + i < rows) store_scale<SCALE>(by_rows.d_scales, cb * by_rows.ld_scales + row0 + i, held);
@@ -87,14 +94,14 @@ __global__ __launch_bounds__(256) void k_f8_quantize_tiles(const T* __restrict__
             for (int j = 0; j < 8; j++) {
                 float amax = 0.f;
 #pragma unroll
-                for (int i = 0; i < 8; i++) amax = fmaxf(amax, finite_abs(v[i][j]));
+                for (int i = 0; i < R; i++) amax = fmaxf(amax, finite_abs(v[i][j]));
                 part[lane_r][lane_c * 8 + j] = amax;
             }
             __syncthreads();
             if (t < kF8Block) {
                 float amax = 0.f;
 #pragma unroll
-                for (int r = 0; r < 16; r++) amax = fmaxf(amax, part[r][t]);
+                for (int r = 0; r < kLaneRows; r++) amax = fmaxf(amax, part[r][t]);
                 uint32_t held;
                 col_inv[t] = block_scale<FORMAT, SCALE>(amax, &held);
                 if (cb * kF8Block + t < cols) store_scale<SCALE>(by_cols.d_scales, rb * by_cols.ld_scales + cb * kF8Block + t, held);
@@ -103,7 +110,7 @@ __global__ __launch_bounds__(256) void k_f8_quantize_tiles(const T* __restrict__
     }
     if (by_rows.d_codes) {
 #pragma unroll
-        for (int i = 0; i < 8; i++)
+        for (int i = 0; i < R; i++)
             if (row0 + i < rows) {
                 const float s = inv_row[i];
                 *reinterpret_cast<uint2*>(static_cast<uint8_t*>(by_rows.d_codes) + (row0 + i) * by_rows.ld + c0) =
@@ -116,30 +123,33 @@ __global__ __launch_bounds__(256) void k_f8_quantize_tiles(const T* __restrict__
 #pragma unroll
     for (int j = 0; j < 8; j++) {
         const float s = col_inv[lane_c * 8 + j];
-        tile[lane_c * 8 + j][lane_r ^ lane_c] = make_uint2(encode4<FORMAT>(v[0][j] * s, v[1][j] * s, v[2][j] * s, v[3][j] * s),
-                                                           encode4<FORMAT>(v[4][j] * s, v[5][j] * s, v[6][j] * s, v[7][j] * s));
+        tile[lane_c * 8 + j][2 * (lane_r / 2 ^ lane_c) + lane_r % 2] = encode4<FORMAT>(v[0][j] * s, v[1][j] * s, v[2][j] * s, v[3][j] * s);
         if (col_sums) {
             float sum = 0.f;
 #pragma unroll
-            for (int i = 0; i < 8; i++) sum += v[i][j];
+            for (int i = 0; i < R; i++) sum += v[i][j];
             part[lane_r][lane_c * 8 + j] = sum;
         }
     }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 4; i++) {
-        const int col = (t >> 3) + 32 * i, piece = t & 7, turn = (col >> 3) & 15;
+    for (int i = 0; i < kF8Block * 8 / kTileThreads; i++) {
+        const int col = (t >> 3) + kTileThreads / 8 * i, piece = t & 7, turn = (col >> 3) & 15;
         if (cb * kF8Block + col < cols) {
-            const uint2 a = tile[col][(2 * piece) ^ turn], b = tile[col][(2 * piece + 1) ^ turn];
+            const uint2 a = *reinterpret_cast<const uint2*>(&tile[col][2 * ((2 * piece) ^ turn)]),
+                        b = *reinterpret_cast<const uint2*>(&tile[col][2 * ((2 * piece + 1) ^ turn)]);
             *reinterpret_cast<uint4*>(static_cast<uint8_t*>(by_cols.d_codes) + (cb * kF8Block + col) * by_cols.ld +
                                       rb * kF8Block + piece * 16) = make_uint4(a.x, a.y, b.x, b.y);
         }
     }
     if (col_sums && t < kF8Block && cb * kF8Block + t < cols) {
-        float sum = 0.f;
+        float sum = 0.f, other = 0.f;
 #pragma unroll
-        for (int r = 0; r < 16; r++) sum += part[r][t];
-        col_sums[rb * cols + cb * kF8Block + t] = sum;
+        for (int r = 0; r < kLaneRows / 2; r++) {
+            sum += part[r][t];
+            other += part[r + kLaneRows / 2][t];
+        }
+        col_sums[rb * cols + cb * kF8Block + t] = sum + other;
     }
 }
 
@@ -187,7 +197,7 @@ hipError_t launch_f8_quantize(const void* d_x, int type, int64_t rows, int64_t c
                                       dim3(256), 0, s, x, rows, cols, ld_x, (uint32_t)col_blocks, a);
                     const dim3 grid((unsigned)(row_blocks * col_blocks));
                     auto kernel = any.block_rows == 1 ? k_f8_quantize_tiles<T, F, S, false, R> : k_f8_quantize_tiles<T, F, S, true, R>;
-                    return launch(K_F8_QUANTIZE, kernel, grid, dim3(256), 0, s, x, rows, cols, ld_x, (uint32_t)col_blocks, a, b, d_col_sums);
+                    return launch(K_F8_QUANTIZE, kernel, grid, dim3(kTileThreads), 0, s, x, rows, cols, ld_x, (uint32_t)col_blocks, a, b, d_col_sums);
                 });
             });
         });
