@@ -70,6 +70,39 @@ __device__ __forceinline__ v4f mfma_block_wide(const Wide& b, const Wide& a, v4f
     return c;
 }
 
+// The same in bf16 with the power-of-two scale in the conversion: bf16 has f32's exponents, so that the numbers are as exact.
+typedef __bf16 v8b __attribute__((ext_vector_type(8)));
+template <int FORMAT>
+__device__ __forceinline__ v8b widen8_scaled(int lo, int hi, float scale) {
+    typedef __bf16 v2b __attribute__((ext_vector_type(2)));
+    v2b r[4];
+    if constexpr (FORMAT == FMTC_E4M3) {
+        r[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false);
+        r[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
+        r[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false);
+        r[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
+    } else {
+        r[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(lo, scale, false);
+        r[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(lo, scale, true);
+        r[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(hi, scale, false);
+        r[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(hi, scale, true);
+    }
+    return v8b{r[0][0], r[0][1], r[1][0], r[1][1], r[2][0], r[2][1], r[3][0], r[3][1]};
+}
+struct Scaled { v8b v[4]; };
+template <int FORMAT>
+__device__ __forceinline__ Scaled widen_scaled(v8i q, uint32_t scale) {
+    Scaled w;
+#pragma unroll
+    for (int j = 0; j < 4; j++) w.v[j] = widen8_scaled<FORMAT>(q[2 * j], q[2 * j + 1], __uint_as_float(scale));
+    return w;
+}
+__device__ __forceinline__ v4f mfma_block_wide(const Scaled& b, const Scaled& a, v4f c) {
+#pragma unroll
+    for (int j = 0; j < 4; j++) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b.v[j], a.v[j], c, 0, 0, 0);
+    return c;
+}
+
 // How a product is computed: f32 scales and the 8-bit instruction, power-of-two scales as its operands, or in f16 with either
 // kind of scale
 enum Way { kScaled = 0, kExponents = 1, kWide = 2, kWideExponents = 3 };
@@ -333,11 +366,8 @@ __global__ __launch_bounds__(S::kThreads, 2) void k_f8_matmul_tiles(Product p, u
     wait_loads<(kStages - 2) * kEach + kFirst>();
     __syncthreads();
     // b's tiles as the way takes them; the products of a tile of a, added to the sums while the next one is multiplied
-    using Held = typename std::conditional<is_wide(WAY), Wide, v8i>::type;
-    auto hold = [&](v8i raw) {
-        if constexpr (is_wide(WAY)) return widen<FMTC_E4M3>(raw);
-        else return raw;
-    };
+    using Held = typename std::conditional<WAY == kWideExponents, Scaled, typename std::conditional<WAY == kWide, Wide, v8i>::type>::type;
+    constexpr bool kInside = WAY == kExponents || WAY == kWideExponents;  // the scales are in the operands
     Held b[NT];
     v8i a[3];  // tiles i, i + 1 and i + 2: a tile's read has two tiles' products to arrive under
     uint32_t sa[3], sb[NT][4];
@@ -346,10 +376,14 @@ __global__ __launch_bounds__(S::kThreads, 2) void k_f8_matmul_tiles(Product p, u
         sa[to] = scales[((uint32_t)kb & (kStages - 1)) * S::kThreads + row_a + 16 * i];
     };
     auto read_b = [&](int64_t kb, int j) {
-        b[j] = hold(piece(kb, row_b + 16 * j));
         const uint32_t* s = scales + ((uint32_t)kb & (kStages - 1)) * S::kThreads;
+        const v8i raw = piece(kb, row_b + 16 * j);
+        if constexpr (WAY == kWideExponents) b[j] = widen_scaled<FMTC_E4M3>(raw, s[row_b + 16 * j]);
+        else if constexpr (WAY == kWide) b[j] = widen<FMTC_E4M3>(raw);
+        else b[j] = raw;
         if constexpr (WAY == kExponents) {
             sb[j][0] = s[row_b + 16 * j];
+        } else if constexpr (WAY == kWideExponents) {
         } else if constexpr (B_ROWS == 1) {
             const uint4 v = *reinterpret_cast<const uint4*>(s + S::BM + wn * 64 + 16 * j + 4 * g);
             sb[j][0] = v.x, sb[j][1] = v.y, sb[j][2] = v.z, sb[j][3] = v.w;
@@ -387,6 +421,13 @@ __global__ __launch_bounds__(S::kThreads, 2) void k_f8_matmul_tiles(Product p, u
                     acc[i][j] = mfma_block_scaled<FORMAT>(b[j], a[0], acc[i][j], (int)sb[j][0], (int)sa[0]);
                     if (i == MT - 1) read_b(kb + 1, j);
                 }
+            } else if constexpr (WAY == kWideExponents) {
+                const Scaled with = widen_scaled<FORMAT>(a[0], sa[0]);
+#pragma unroll
+                for (int j = 0; j < NT; j++) acc[i][j] = mfma_block_wide(b[j], with, acc[i][j]);
+                if (i == MT - 1)
+#pragma unroll
+                    for (int j = 0; j < NT; j++) read_b(kb + 1, j);
             } else {
                 v4f* const before = acc[i ? i - 1 : MT - 1];
                 const auto with = [&] { if constexpr (is_wide(WAY)) return widen<FORMAT>(a[0]); else return a[0]; }();
@@ -420,7 +461,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void k_f8_matmul_tiles(Product p, u
             __builtin_amdgcn_sched_barrier(0);
         }
     }
-    if constexpr (WAY != kExponents) {
+    if constexpr (!kInside) {
 #pragma unroll
         for (int j = 0; j < NT; j++)
 #pragma unroll
