@@ -70,7 +70,8 @@ __device__ __forceinline__ v4f mfma_block_wide(const Wide& b, const Wide& a, v4f
     return c;
 }
 
-// The same in bf16 with the power-of-two scale in the conversion: bf16 has f32's exponents, so that the numbers are as exact.
+// With power-of-two scales the same in bf16, the scale in the conversion: bf16 has f32's exponents, so that the numbers are as
+// exact (but for those under 2^-133), and the instruction adds to the running sum itself (4096^3 150 -> 135 us).
 typedef __bf16 v8b __attribute__((ext_vector_type(8)));
 template <int FORMAT>
 __device__ __forceinline__ v8b widen8_scaled(int lo, int hi, float scale) {
@@ -103,8 +104,8 @@ __device__ __forceinline__ v4f mfma_block_wide(const Scaled& b, const Scaled& a,
     return c;
 }
 
-// How a product is computed: f32 scales and the 8-bit instruction, power-of-two scales as its operands, or in f16 with either
-// kind of scale
+// How a product is computed: f32 scales and the 8-bit instruction, power-of-two scales as its operands, f32 scales and f16, or
+// power-of-two scales and bf16
 enum Way { kScaled = 0, kExponents = 1, kWide = 2, kWideExponents = 3 };
 constexpr bool is_wide(int way) { return way >= kWide; }
 constexpr int scale_kind(int way) { return way == kScaled || way == kWide ? FMTC_SCALE_F32 : FMTC_SCALE_E8M0; }
@@ -312,7 +313,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void k_f8_matmul_tiles(Product p, u
     }
     const uint32_t lds_at = (uint32_t)(uintptr_t)(lds_void_t*)lds;
     // Scales: a lane moves that of a row of a or of b (past both: the last of b again), as it is straight into LDS, or, for the
-    // f16 way that would make floats of them again and again, through a register in which it becomes one.
+    // bf16 way that would make floats of them again and again, through a register in which it becomes one.
     constexpr bool kStraight = WAY != kWideExponents;
     static_assert(kStraight || S::kStages == 2);
     uint32_t mine = 0;
@@ -500,8 +501,10 @@ __global__ __launch_bounds__(256) void k_f8_join(Product p, const float* __restr
     store_out(p.out, p.out_type, p.ld_out, m, n, p.N, v, p.bias, p.accumulate);
 }
 
-// rows of the large tile: half as many where the operands in f16, or a scale for every row of b, take the registers
-constexpr int kernel256_rows(int way, int b_rows) { return is_wide(way) || (way == kScaled && b_rows == 1) ? 128 : 256; }
+// rows of the large tile: half as many where operands in f16 with their sums apart, or a scale for every row of b, take the
+// registers.  (bf16 operands with their scales inside: widening is what bounds it, and twice the rows use b's tiles twice as
+// often: 4096^3 135 -> 114 us, 8192^3 879 -> 770 us.)
+constexpr int kernel256_rows(int way, int b_rows) { return way == kWide || (way == kScaled && b_rows == 1) ? 128 : 256; }
 
 template <class F>
 hipError_t with_way(int way, F&& f) {
@@ -520,7 +523,8 @@ namespace {
 // Which kernel, and in how many parts of the depth: the least of the times that a product of these sizes is expected to
 // take, in us, from what each kernel takes to start and end and for a block of the depth, alone on a compute unit and with
 // all of them busy.  The numbers are fits to measured times over 17 to 4096 rows, 512 to 8192 columns and a depth of 512 to
-// 8192.  With f32 scales and bf16 results: 128 x 4096 x 4096 rows 23.2, tiles of 128 26.1, in 4 parts 19.8; 1024 x 1024 x 4096
+// 8192 (16384 for power-of-two scales and f32 results: 4096^3 133 us in tiles of 128, 102 of 256; 1024 x 1024 x 16384 125, in 8
+// parts 44).  With f32 scales and bf16 results: 128 x 4096 x 4096 rows 23.2, tiles of 128 26.1, in 4 parts 19.8; 1024 x 1024 x 4096
 // 41.7, 26.3, 24.1 in 4 parts; 4096 x 1024 x 1024 45.8, 12.8, tiles of 256 21.6; 4096^3 -, 87.4, 65.7.  Four steps' operands
 // in LDS (one workgroup a compute unit, not two) where that holds all tiles: 1024 x 4096 x 4096 34.4 -> 28.9; beyond,
 // 2048 x 4096 x 4096, 45.0 -> 53.7; alone they gain nothing (512 x 512 x 8192 45.1, 43.9), nor in f16.  Up to 16 rows the
@@ -529,7 +533,8 @@ struct Plan { int kernel, splits; int64_t split_blocks; };
 enum { kRows = 0, kTiles128 = 1, kTiles256 = 2, kTiles128Deep = 3 };
 constexpr double kCus = 256;
 
-Plan make_plan(int64_t M, int64_t N, int64_t K, bool wide) {
+Plan make_plan(int64_t M, int64_t N, int64_t K, int way) {
+    const bool wide = is_wide(way), inside = way == kWideExponents;
     const int64_t blocks = (K + kF8Block - 1) / kF8Block;
     Plan best{kRows, 1, blocks};
     if (M <= 16) return best;
@@ -537,14 +542,14 @@ Plan make_plan(int64_t M, int64_t N, int64_t K, bool wide) {
     double least = 2.5 + (wide ? 2.6 : 2.3) * ((blocks + kRowsWaves - 1) / kRowsWaves) * ceil(row_groups / kCus);
     for (int kernel = kTiles128; kernel <= (M > 128 && N > 128 ? kTiles256 : kTiles128); kernel++)
         for (int64_t want = 1; want <= 16 && want <= blocks; want *= 2) {
-            const int64_t bm = kernel == kTiles256 && !wide ? 256 : 128, bn = kernel == kTiles256 ? 256 : 128;
+            const int64_t bm = kernel == kTiles256 && way != kWide ? 256 : 128, bn = kernel == kTiles256 ? 256 : 128;
             const int64_t per = (blocks + want - 1) / want, splits = (blocks + per - 1) / per;
             const double groups = (double)((M + bm - 1) / bm) * ((N + bn - 1) / bn) * splits;
             const bool deep = kernel == kTiles128 && !wide && groups <= kCus && groups > kCus / 4;
             const double busy = fmin(1.0, groups / kCus), rounds = ceil(groups / kCus);
             double start, step;
-            if (kernel == kTiles128) start = wide ? 7.0 : 6.0, step = wide ? 1.05 + 0.1 * busy : deep ? 0.58 + 0.1 * busy : 0.6 + 0.1 * busy;
-            else start = wide ? 9.0 : 11.0, step = wide ? 1.68 + 0.35 * busy : 1.14 + 0.5 * busy;
+            if (kernel == kTiles128) start = wide ? 7.0 : 6.0, step = inside ? 0.93 + 0.07 * busy : wide ? 1.05 + 0.1 * busy : deep ? 0.58 + 0.1 * busy : 0.6 + 0.1 * busy;
+            else start = inside ? 13.0 : wide ? 9.0 : 11.0, step = inside ? 2.3 + 0.5 * busy : wide ? 1.68 + 0.35 * busy : 1.14 + 0.5 * busy;
             double t = start + step * per * rounds;
             if (splits > 1) t += 4.0 + 1e-6 * splits * M * N;  // the parts' sums written and read, 8 bytes at 8 TB/s
             if (t < least) {
@@ -564,8 +569,8 @@ int64_t split_ld(int64_t N) { return (N + 3) / 4 * 4; }
 
 size_t matmul_f8_workspace(int64_t M, int64_t N, int64_t K) {
     size_t most = 0;
-    for (int wide = 0; wide < 2; wide++) {
-        const Plan plan = make_plan(M, N, K, wide);
+    for (const int way : {kScaled, kWide, kWideExponents}) {
+        const Plan plan = make_plan(M, N, K, way);
         const size_t bytes = plan.splits > 1 ? align_up(sizeof(float) * (size_t)plan.splits * M * split_ld(N), 256) : 0;
         if (bytes > most) most = bytes;
     }
@@ -579,7 +584,7 @@ hipError_t launch_f8_matmul(const fmtc_f8& a, const fmtc_f8& b, const float* d_b
               d_bias, d_out, out_type, accumulate, 0, 0};
     const bool exponents = a.scale == FMTC_SCALE_E8M0;
     const int way = out_type == FMTC_F32 ? (exponents ? kWideExponents : kWide) : exponents ? kExponents : kScaled;
-    Plan plan = make_plan(p.M, p.N, a.depth, is_wide(way));
+    Plan plan = make_plan(p.M, p.N, a.depth, way);
     if (p.ld_a >= (1 << 23) || p.ld_b >= (1 << 23)) plan = {kRows, 1, p.blocks};  // (a tile's offsets are 32 bits)
     p.split_blocks = plan.split_blocks;
     Product inner = p;

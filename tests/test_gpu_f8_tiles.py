@@ -76,3 +76,22 @@ def test_large_products_give_the_same_bits_every_time(fmtc):  # noqa: F811
             a, b = _operands(fmtc, *shape, E4, False, 128, 150)
             first = fmtc.f8_matmul(a, b, dtype=dtype)
             assert all(torch.equal(first, fmtc.f8_matmul(a, b, dtype=dtype)) for _ in range(4))
+
+
+@pytest.mark.parametrize("shape", [(600, 520, 512), (2049, 2049, 4200)])
+@pytest.mark.parametrize("fmt", [E4, E5])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_power_of_two_scales_at_their_ends(fmtc, shape, fmt, dtype):  # noqa: F811
+    """Scales of 2^-127, 2^-126, very large ones, and one that is not a number: a row of a, a column of b."""
+    M, N, K = shape
+    a, b = _operands(fmtc, M, N, K, fmt, True, 1, 160)
+    sa, sb = a.scales.view(torch.uint8), b.scales.view(torch.uint8)
+    sa[1, 7], sb[2, 9] = 255, 255
+    sa[0, 11], sa[0, 12], sb[0, 3], sa[2, 13], sb[2, 20], sb[1, 21] = 0, 1, 200, 20, 0, 1
+    y = fmtc.f8_matmul(a, b, dtype=dtype).cpu().to(torch.float64)
+    av, bv = ref.values(a.codes, a.scales, K), ref.values(b.codes, b.scales, K)
+    want = av @ bv.t()
+    bad = torch.isnan(want)
+    assert torch.equal(torch.isnan(y), bad) and int(bad.sum()) == M + N - 1
+    av, bv = av.nan_to_num(), bv.nan_to_num()
+    assert ((y - want).abs() <= _limit(av, bv, dtype, want))[~bad].all()
