@@ -542,7 +542,8 @@ namespace {
 // all of them busy.  The numbers are fits to measured times over 17 to 4096 rows, 512 to 8192 columns and a depth of 512 to
 // 8192 (16384 for power-of-two scales and f32 results: 4096^3 133 us in tiles of 128, 102 of 256; 1024 x 1024 x 16384 125, in 8
 // parts 44).  With f32 scales and bf16 results: 128 x 4096 x 4096 rows 23.2, tiles of 128 26.1, in 4 parts 19.8; 1024 x 1024 x 4096
-// 41.7, 26.3, 24.1 in 4 parts; 4096 x 1024 x 1024 45.8, 12.8, tiles of 256 21.6; 4096^3 -, 87.4, 65.7.  Four steps' operands
+// 41.7, 26.3, 24.1 in 4 parts; 4096 x 1024 x 1024 45.8, 12.8, tiles of 256 21.6; 4096^3 -, 87.4, 65.7; 16384 x 4096 x 128
+// -, 52, 47; 5125 x 4096 x 315 -, 28.0, 29.2.  Four steps' operands
 // in LDS (one workgroup a compute unit, not two) where that holds all tiles: 1024 x 4096 x 4096 34.4 -> 28.9; beyond,
 // 2048 x 4096 x 4096, 45.0 -> 53.7; alone they gain nothing (512 x 512 x 8192 45.1, 43.9), nor in f16.  Up to 16 rows the
 // wavefronts of the first kernel waste nothing: always that one.
@@ -566,8 +567,10 @@ Plan make_plan(int64_t M, int64_t N, int64_t K, int way) {
             const double busy = fmin(1.0, groups / kCus), rounds = ceil(groups / kCus);
             double start, step;
             if (kernel == kTiles128) start = wide ? 7.0 : 6.0, step = inside ? 0.93 + 0.07 * busy : wide ? 1.05 + 0.1 * busy : deep ? 0.58 + 0.1 * busy : 0.6 + 0.1 * busy;
-            else start = inside ? 13.0 : wide ? 9.0 : 11.0, step = inside ? 2.3 + 0.5 * busy : wide ? 1.68 + 0.35 * busy : 1.14 + 0.5 * busy;
-            double t = start + step * per * rounds;
+            else start = inside ? 13.0 : wide ? 9.0 : 12.0, step = inside ? 2.3 + 0.5 * busy : wide ? 1.68 + 0.35 * busy : 1.14 + 0.5 * busy;
+            const bool apart = wide && !inside;
+            const double again = kernel == kTiles128 ? (apart ? 3.0 : 2.0) : apart ? 7.0 : 9.0;  // a further tile's start and end
+            double t = start + step * per * rounds + again * (rounds - 1);
             if (splits > 1) t += 4.0 + 1e-6 * splits * M * N;  // the parts' sums written and read, 8 bytes at 8 TB/s
             if (t < least) {
                 least = t;
