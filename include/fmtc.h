@@ -401,7 +401,8 @@ fmtc_status fmtc_block_norm(const fmtc_norm *args, void *d_h_out, int64_t ld_h_o
 /* The gradients, from dn (of n) and dh (of h', what reaches the stream from the
  * later blocks); either may be NULL (0).  args: as in the forward call, but d_h is
  * h' as it was stored; eps is not read.  Outputs, any NULL: d_dy, d_dh_in (of h; may
- * be dh itself) in `type`; d_dw_post, d_dw_pre [C] and d_dgate (as d_gate) in f32.
+ * be dh itself) in `type`; d_dw_post, d_dw_pre [C] and d_dgate (as d_gate: nothing
+ * is written to it where there are no rows) in f32.
  * Sums over rows are in a fixed order. */
 size_t fmtc_block_norm_workspace_size(int64_t rows, int C, int64_t rows_per_gate);
 fmtc_status fmtc_block_norm_backward(const fmtc_norm *args, const float *d_stats, const void *d_dn, int64_t ld_dn,

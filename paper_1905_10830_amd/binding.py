@@ -847,7 +847,7 @@ def block_norm_backward(dn, dh, y, h_out, stats, w_post, w_pre, gate=None, rows_
                         dh_in=None, workspace=None):
     """Asynchronous.  dn, dh: gradients of n and of h' (either may be None); h_out: h' as block_norm stored it, stats as it
     left them.  dy, dh_in: tensors to write to (None: new ones).  -> (dy, dh_in, dw_post, dw_pre, dgate), the last three in
-    f32, None where there is no such input."""
+    f32 (0 where there are no rows), None where there is no such input."""
     import torch
 
     a = _norm_args(y, h_out, w_post, w_pre, gate, rows_per_gate, skip, scale, 0.0)
@@ -855,6 +855,8 @@ def block_norm_backward(dn, dh, y, h_out, stats, w_post, w_pre, gate=None, rows_
     kind, device = h_out.dtype, h_out.device
     new = lambda like: torch.empty_like(like, dtype=torch.float32) if like is not None else None  # noqa: E731
     dw_post, dw_pre, dgate = new(w_post), new(w_pre), new(gate)
+    if dgate is not None and P == 0:  # (the library sees a gate of no rows then)
+        dgate.zero_()
     of = lambda t, what: _rows(t, what, C, P, kind) if t is not None else (None, 0, 0)  # noqa: E731
     (dn_p, _, dn_ld), (dh_p, _, dh_ld) = of(dn, "dn"), of(dh, "dh")
     if dy is None and y is not None:
