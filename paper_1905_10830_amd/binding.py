@@ -760,27 +760,36 @@ def f8_matmul_backward(dy, w_t, x_t, fmt=E4M3, scales=SCALE_F32, bias=False, dx=
                        workspace=None):
     """Asynchronous.  Gradients of y = x w^T + bias: dy [P, O]; w_t: the weights as F8 [K, O] in 128 x 128 blocks (None: no
     dx); x_t: x by columns as F8 [K, P] (None: no dw).  -> (dx [P, K] in dy's type, dw [O, K] f32, dbias [O] f32), None
-    where not wanted (dbias: wanted with bias=True or where given).  accumulate: dw and dbias are added to."""
+    where not wanted (dbias: wanted with bias=True or where given).  accumulate: dw and dbias are added to.  Without rows
+    (P = 0: f8_quantize gives no x by columns) x_t may be None all the same: dw is 0, as wide as the weights or as given."""
     import torch
 
     ptr, kind, ld = _rows(dy, "dy")
     P, O = dy.shape
     if accumulate and ((x_t is not None and dw is None) or (bias and dbias is None)):
         raise ValueError("accumulate needs the outputs that are added to")
+    x_c, x_rows = (None, 0) if x_t is None else (_f8(x_t), x_t.rows)
+    if P == 0 and x_t is None:
+        if dw is not None:
+            _rows(dw, "dw", dtype=torch.float32)
+            x_rows = dw.shape[1]
+        elif w_t is not None and not accumulate:
+            x_rows = w_t.rows
+        x_c = _F8(rows=x_rows) if x_rows else None
     if w_t is not None and dx is None:
         dx = _matrix(P, w_t.rows, dy.dtype, dy.device)
-    if x_t is not None and dw is None:
-        dw = _matrix(O, x_t.rows, torch.float32, dy.device)
+    if x_c is not None and dw is None:
+        dw = _matrix(O, x_rows, torch.float32, dy.device)
     if bias and dbias is None:
         dbias = torch.empty(O, dtype=torch.float32, device=dy.device)
-    if (dx is not None and w_t is None) or (dw is not None and x_t is None):
+    if (dx is not None and w_t is None) or (dw is not None and x_c is None):
         raise ValueError("dx needs w_t, dw needs x_t")
     dx_ptr, dx_kind, dx_ld = _rows(dx, "dx", w_t.rows, P) if dx is not None else (None, F32, 0)
-    dw_ptr, _, dw_ld = _rows(dw, "dw", x_t.rows, O, torch.float32) if dw is not None else (None, F32, 0)
-    K = w_t.rows if w_t is not None else x_t.rows if x_t is not None else 1
+    dw_ptr, _, dw_ld = _rows(dw, "dw", x_rows, O, torch.float32) if dw is not None else (None, F32, 0)
+    K = w_t.rows if w_t is not None else x_rows or 1
     lib = load_library()
     workspace, ws, size = _workspace(workspace, lib.fmtc_f8_matmul_backward_workspace_size(P, K, O), dy.device)
-    _check(lib.fmtc_f8_matmul_backward(ptr, kind, P, O, ld, _f8(w_t), _f8(x_t), fmt, scales, dx_ptr, dx_kind, dx_ld, dw_ptr, dw_ld,
+    _check(lib.fmtc_f8_matmul_backward(ptr, kind, P, O, ld, _f8(w_t), x_c, fmt, scales, dx_ptr, dx_kind, dx_ld, dw_ptr, dw_ld,
                                        _vector(dbias, "dbias", O, torch.float32), int(accumulate), ws, size, _stream()))
     return dx, dw, dbias
 
