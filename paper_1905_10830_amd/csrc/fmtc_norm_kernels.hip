@@ -242,7 +242,12 @@ struct Strips {
 // 129 values on.
 constexpr int lanes_of(int C) { return C <= 128 ? 16 : C <= 512 ? 64 : C <= 1024 ? 128 : C <= 2048 ? 256 : C <= 4096 ? 512 : 1024; }
 
+// A gate row for more rows than there are serves them all; callers may say any such number (the largest one for "all"), with
+// which sums of rows would pass 63 bits.
+int64_t rows_served(int64_t rows, int64_t rows_per_gate) { return rows_per_gate < rows ? rows_per_gate : rows; }
+
 Strips make_strips(int64_t rows, int C, int64_t rows_per_gate) {
+    rows_per_gate = rows_served(rows, rows_per_gate);
     // as many strips as 256 compute units walk at a time with 16 wavefronts each: the sums of a large tensor's strips are a
     // small part of the traffic, and a small tensor has every row on its way at once (500 x 960, a gate for every row: 17.7 us
     // in strips of 4 rows)
@@ -258,9 +263,8 @@ Strips make_strips(int64_t rows, int C, int64_t rows_per_gate) {
         s.rows = each / rows_per_gate * rows_per_gate;
         s.count = ceil_div(rows, s.rows);
     } else {
-        const int64_t span = rows_per_gate < rows ? rows_per_gate : rows;
-        s.per_gate = ceil_div(span, each);
-        s.rows = ceil_div(span, s.per_gate);
+        s.per_gate = ceil_div(rows_per_gate, each);
+        s.rows = ceil_div(rows_per_gate, s.per_gate);
         s.count = s.gates * s.per_gate;
     }
     return s;
@@ -548,7 +552,9 @@ hipError_t launch_block_norm_backward(const fmtc_norm& a, const float* d_stats, 
                                       const void* d_dh, int64_t ld_dh, void* d_dy, int64_t ld_dy, void* d_dh_in,
                                       int64_t ld_dh_in, float* d_dw_post, float* d_dw_pre, float* d_dgate,
                                       void* d_ws, hipStream_t s) {
-    const Strips st = make_strips(a.rows, a.C, a.d_gate ? a.rows_per_gate : 0);
+    fmtc_norm args = a;
+    args.rows_per_gate = a.d_gate ? rows_served(a.rows, a.rows_per_gate) : 0;
+    const Strips st = make_strips(a.rows, a.C, args.rows_per_gate);
     const int64_t groups = ceil_div(st.count, norm_threads(lanes_of(a.C)) / lanes_of(a.C));
     const size_t each = align_up(sizeof(float) * (size_t)groups * a.C, 256);
     char* ws = static_cast<char*>(d_ws);
@@ -560,7 +566,7 @@ hipError_t launch_block_norm_backward(const fmtc_norm& a, const float* d_stats, 
             constexpr int TPR = decltype(lanes)::value, VPT = decltype(per)::value;
             constexpr bool RAGGED = decltype(ragged)::value;
             return launch(K_BLOCK_NORM_BACKWARD, k_block_norm_backward<typename decltype(ty)::type, typename decltype(wt)::type, TPR, VPT, RAGGED>,
-                          dim3((unsigned)groups), dim3(norm_threads(TPR)), 0, s, a, q);
+                          dim3((unsigned)groups), dim3(norm_threads(TPR)), 0, s, args, q);
         });
     });
     const bool join_gate = d_dgate && st.per_gate > 1;
