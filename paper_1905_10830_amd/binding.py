@@ -667,7 +667,7 @@ class F8:
     torch.float8_e4m3fn or torch.float8_e5m2 (ld: depth rounded up to 128 or more, zeros behind the depth), and scales
     [ceil(depth / 128), ceil(rows / block_rows)] of torch.float32 or torch.float8_e8m0fnu."""
 
-    __slots__ = ("codes", "scales", "rows", "depth", "block_rows", "_c")
+    __slots__ = ("_codes", "_scales", "_rows", "_depth", "_block_rows", "_at", "_c")
 
     def __init__(self, codes, scales, depth, block_rows=1):
         if not _FORMATS:
@@ -691,9 +691,18 @@ class F8:
         self._set(codes, scales, rows, depth, block_rows, ld if rows > 1 else width, ld_scales if blocks > 1 else n_rows, fmt, kind)
 
     def _set(self, codes, scales, rows, depth, block_rows, ld, ld_scales, fmt, kind):
-        self.codes, self.scales, self.rows, self.depth, self.block_rows = codes, scales, rows, depth, block_rows
-        self._c = _F8(codes.data_ptr(), scales.data_ptr(), rows, depth, ld, ld_scales, fmt, kind, block_rows)
+        self._codes, self._scales = codes, scales
+        self._rows, self._depth, self._block_rows = rows, depth, block_rows
+        self._at = codes.data_ptr(), scales.data_ptr()
+        self._c = _F8(*self._at, rows, depth, ld, ld_scales, fmt, kind, block_rows)
         return self
+
+    # What the library reads and writes was checked when the object was made: nothing of it is assigned anew.
+    codes = property(lambda self: self._codes)
+    scales = property(lambda self: self._scales)
+    rows = property(lambda self: self._rows)
+    depth = property(lambda self: self._depth)
+    block_rows = property(lambda self: self._block_rows)
 
 
 def f8_empty(rows, depth, fmt=E4M3, scales=SCALE_F32, block_rows=1, device="cuda"):
@@ -711,7 +720,12 @@ def f8_empty(rows, depth, fmt=E4M3, scales=SCALE_F32, block_rows=1, device="cuda
 
 
 def _f8(q):
-    return None if q is None else ctypes.byref(q._c)
+    if q is None:
+        return None
+    if (q._codes.data_ptr(), q._scales.data_ptr()) != q._at:
+        which = "codes" if q._codes.data_ptr() != q._at[0] else "scales"
+        raise ValueError(f"F8: {which} are not in the memory that they had when it was made")
+    return ctypes.byref(q._c)
 
 
 def f8_quantize(x, by_rows=True, by_cols=False, fmt=E4M3, scales=SCALE_F32, block_rows=1):
