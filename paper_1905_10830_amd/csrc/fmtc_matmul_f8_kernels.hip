@@ -518,10 +518,13 @@ __global__ __launch_bounds__(256) void k_f8_join(Product p, const float* __restr
     store_out(p.out, p.out_type, p.ld_out, m, n, p.N, v, load_bias(p.bias, n, p.N), p.accumulate);
 }
 
-// rows of the large tile: half as many where operands in f16 with their sums apart, or a scale for every row of b, take the
-// registers.  (bf16 operands with their scales inside: widening is what bounds it, and twice the rows use b's tiles twice as
+// rows of the large tile: half as many where operands in f16 with their sums apart take the registers.  (bf16 operands with their scales inside: widening is what bounds it, and twice the rows use b's tiles twice as
 // often: 4096^3 135 -> 114 us, 8192^3 879 -> 770 us.)
-constexpr int kernel256_rows(int way, int b_rows) { return way == kWide || (way == kScaled && b_rows == 1) ? 128 : 256; }
+constexpr int kernel256_rows(int way) { return way == kWide ? 128 : 256; }
+// f32 scales for every row of b and bf16 or f16 results have no large tile: the scales leave registers for 128 x 256 only, which
+// is no better than 128 x 128 (4096^3 91.7 and 94.1 us, 2048 x 4096 x 2048 28.8 and 29.6, 4096 x 8192 x 1024 66.9 and 61.7,
+// 8192 x 8192 x 2048 204 and 196, 16384 x 4096 x 128 59.9 and 55.7).
+constexpr bool has_tiles256(int way, int b_rows) { return !(way == kScaled && b_rows == 1); }
 
 template <class F>
 hipError_t with_way(int way, F&& f) {
@@ -551,16 +554,16 @@ struct Plan { int kernel, splits; int64_t split_blocks; };
 enum { kRows = 0, kTiles128 = 1, kTiles256 = 2, kTiles128Deep = 3 };
 constexpr double kCus = 256;
 
-Plan make_plan(int64_t M, int64_t N, int64_t K, int way) {
+Plan make_plan(int64_t M, int64_t N, int64_t K, int way, int b_rows) {
     const bool wide = is_wide(way), inside = way == kWideExponents;
     const int64_t blocks = (K + kF8Block - 1) / kF8Block;
     Plan best{kRows, 1, blocks};
     if (M <= 16) return best;
     const double row_groups = (double)((M + 63) / 64) * ((N + 15) / 16);
     double least = 2.5 + (wide ? 2.6 : 2.3) * ((blocks + kRowsWaves - 1) / kRowsWaves) * ceil(row_groups / kCus);
-    for (int kernel = kTiles128; kernel <= (M > 128 && N > 128 ? kTiles256 : kTiles128); kernel++)
+    for (int kernel = kTiles128; kernel <= (M > 128 && N > 128 && has_tiles256(way, b_rows) ? kTiles256 : kTiles128); kernel++)
         for (int64_t want = 1; want <= 16 && want <= blocks; want *= 2) {
-            const int64_t bm = kernel == kTiles256 && way != kWide ? 256 : 128, bn = kernel == kTiles256 ? 256 : 128;
+            const int64_t bm = kernel == kTiles256 ? kernel256_rows(way) : 128, bn = kernel == kTiles256 ? 256 : 128;
             const int64_t per = (blocks + want - 1) / want, splits = (blocks + per - 1) / per;
             const double groups = (double)((M + bm - 1) / bm) * ((N + bn - 1) / bn) * splits;
             const bool deep = kernel == kTiles128 && !wide && groups <= kCus && groups > kCus / 4;
@@ -589,8 +592,10 @@ int64_t split_ld(int64_t N) { return (N + 3) / 4 * 4; }
 
 size_t matmul_f8_workspace(int64_t M, int64_t N, int64_t K) {
     size_t most = 0;
-    for (const int way : {kScaled, kWide, kWideExponents}) {
-        const Plan plan = make_plan(M, N, K, way);
+    // (all plans that there are: only kScaled asks for b's blocks, and with blocks of 128 rows its plans are those of kExponents)
+    const struct { int way, b_rows; } kinds[] = {{kScaled, kF8Block}, {kScaled, 1}, {kWide, 1}, {kWideExponents, 1}};
+    for (const auto& kind : kinds) {
+        const Plan plan = make_plan(M, N, K, kind.way, kind.b_rows);
         const size_t bytes = plan.splits > 1 ? align_up(sizeof(float) * (size_t)plan.splits * M * split_ld(N), 256) : 0;
         if (bytes > most) most = bytes;
     }
@@ -604,7 +609,7 @@ hipError_t launch_f8_matmul(const fmtc_f8& a, const fmtc_f8& b, const float* d_b
               d_bias, d_out, out_type, accumulate, 0, 0};
     const bool exponents = a.scale == FMTC_SCALE_E8M0;
     const int way = out_type == FMTC_F32 ? (exponents ? kWideExponents : kWide) : exponents ? kExponents : kScaled;
-    Plan plan = make_plan(p.M, p.N, a.depth, way);
+    Plan plan = make_plan(p.M, p.N, a.depth, way, b.block_rows);
     if (p.ld_a >= (1 << 23) || p.ld_b >= (1 << 23)) plan = {kRows, 1, p.blocks};  // (a tile's offsets are 32 bits)
     p.split_blocks = plan.split_blocks;
     Product inner = p;
@@ -627,7 +632,8 @@ hipError_t launch_f8_matmul(const fmtc_f8& a, const fmtc_f8& b, const float* d_b
                     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds);
                     return e != hipSuccess ? e : launch(K_F8_MATMUL, kernel, dim3((unsigned)(tm * tn * plan.splits)), dim3(S::kThreads), S::kLds, s, inner, (uint32_t)tm, (uint32_t)tn);
                 };
-                if (plan.kernel == kTiles256) return tiles(Tile<2, 4, kernel256_rows(W, B) / 32, 2>{});
+                if constexpr (has_tiles256(W, B))
+                    if (plan.kernel == kTiles256) return tiles(Tile<2, 4, kernel256_rows(W) / 32, 2>{});
                 if (plan.kernel == kTiles128) return tiles(Tile<2, 2, 4, 2>{});
                 if constexpr (!is_wide(W))
                     if (plan.kernel == kTiles128Deep) return tiles(Tile<2, 2, 4, 4>{});
