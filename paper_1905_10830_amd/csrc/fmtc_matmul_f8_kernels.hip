@@ -35,8 +35,8 @@ __device__ __forceinline__ v4f mfma_block_scaled(v8i b, v8i a, v4f c, int sb, in
 }
 
 // The block's product for f32 results.  The 8-bit instruction aligns the products of a group of 8 to the largest of them and
-// drops what lies below 2^-13 of it: 1.5e-5 to 2.4e-5 of a result's norm, measured, which no bf16 or f16 output shows but an
-// f32 output does.  Codes are exact in f16, and v_mfma_f32_16x16x32_f16 keeps 24 bits below the largest product, at half the
+// drops what lies below 2^-13 of it: 1.5e-5 to 2.4e-5 of the results' norm with operands of one size, 5e-5 to 7e-5 with
+// channels 100 times the others (2048 to 4096 deep), beside the 2.1e-4 of rounding to f16.  An f32 result would show it.  Codes are exact in f16, and v_mfma_f32_16x16x32_f16 keeps 24 bits below the largest product, at half the
 // rate.  Eight bytes of a lane are one step of 32 of the depth; again both operands only need the same order.
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 template <int FORMAT>
