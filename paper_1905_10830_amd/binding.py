@@ -6,6 +6,7 @@ stream.  There is no CPU path: if the library is missing or has not been
 built the first call raises.
 """
 import ctypes
+import operator
 import os
 
 NCHW, NHWC = 0, 1
@@ -667,7 +668,7 @@ class F8:
     torch.float8_e4m3fn or torch.float8_e5m2 (ld: depth rounded up to 128 or more, zeros behind the depth), and scales
     [ceil(depth / 128), ceil(rows / block_rows)] of torch.float32 or torch.float8_e8m0fnu."""
 
-    __slots__ = ("_codes", "_scales", "_rows", "_depth", "_block_rows", "_at", "_c")
+    __slots__ = ("_codes", "_scales", "_rows", "_depth", "_block_rows", "_at_codes", "_at_scales", "_ref")
 
     def __init__(self, codes, scales, depth, block_rows=1):
         if not _FORMATS:
@@ -693,16 +694,17 @@ class F8:
     def _set(self, codes, scales, rows, depth, block_rows, ld, ld_scales, fmt, kind):
         self._codes, self._scales = codes, scales
         self._rows, self._depth, self._block_rows = rows, depth, block_rows
-        self._at = codes.data_ptr(), scales.data_ptr()
-        self._c = _F8(*self._at, rows, depth, ld, ld_scales, fmt, kind, block_rows)
+        self._at_codes = at_codes = codes.data_ptr()
+        self._at_scales = at_scales = scales.data_ptr()
+        self._ref = ctypes.byref(_F8(at_codes, at_scales, rows, depth, ld, ld_scales, fmt, kind, block_rows))
         return self
 
     # What the library reads and writes was checked when the object was made: nothing of it is assigned anew.
-    codes = property(lambda self: self._codes)
-    scales = property(lambda self: self._scales)
-    rows = property(lambda self: self._rows)
-    depth = property(lambda self: self._depth)
-    block_rows = property(lambda self: self._block_rows)
+    codes = property(operator.attrgetter("_codes"))
+    scales = property(operator.attrgetter("_scales"))
+    rows = property(operator.attrgetter("_rows"))
+    depth = property(operator.attrgetter("_depth"))
+    block_rows = property(operator.attrgetter("_block_rows"))
 
 
 def f8_empty(rows, depth, fmt=E4M3, scales=SCALE_F32, block_rows=1, device="cuda"):
@@ -722,10 +724,10 @@ def f8_empty(rows, depth, fmt=E4M3, scales=SCALE_F32, block_rows=1, device="cuda
 def _f8(q):
     if q is None:
         return None
-    if (q._codes.data_ptr(), q._scales.data_ptr()) != q._at:
-        which = "codes" if q._codes.data_ptr() != q._at[0] else "scales"
+    if q._codes.data_ptr() != q._at_codes or q._scales.data_ptr() != q._at_scales:
+        which = "codes" if q._codes.data_ptr() != q._at_codes else "scales"
         raise ValueError(f"F8: {which} are not in the memory that they had when it was made")
-    return ctypes.byref(q._c)
+    return q._ref
 
 
 def f8_quantize(x, by_rows=True, by_cols=False, fmt=E4M3, scales=SCALE_F32, block_rows=1):
@@ -750,17 +752,17 @@ def f8_matmul(a, b, bias=None, out=None, dtype=None, accumulate=False, workspace
     """Asynchronous.  a: F8 [M, K], b: F8 [N, K] -> a b^T + bias [M, N] in `dtype` (bf16 unless given, or out's)."""
     import torch
 
-    M, N = a.rows, b.rows
+    M, N = a._rows, b._rows
     if out is None:
         if accumulate:
             raise ValueError("accumulate needs the output that is added to")
         kind, ld = _dtype(dtype or torch.bfloat16), N
-        out = _matrix(M, N, dtype or torch.bfloat16, a.codes.device)
+        out = _matrix(M, N, dtype or torch.bfloat16, a._codes.device)
         ptr = out.data_ptr()
     else:
         ptr, kind, ld = _rows(out, "out", N, M, dtype)
     lib = load_library()
-    workspace, ws, size = _workspace(workspace, lib.fmtc_f8_matmul_workspace_size(M, N, a.depth), out.device)
+    workspace, ws, size = _workspace(workspace, lib.fmtc_f8_matmul_workspace_size(M, N, a._depth), out.device)
     _check(lib.fmtc_f8_matmul(_f8(a), _f8(b), _vector(bias, "bias", N, torch.float32), ptr, kind, ld, int(accumulate), ws, size,
                               _stream()))
     return out
