@@ -821,8 +821,11 @@ def _norm_args(y, h, w_post, w_pre, gate, rows_per_gate, skip, scale, eps):
     if gate is None:
         rows_per_gate, gate_ptr = 0, None
     else:
-        most = max(P, 1)  # (one row for all, however many more it says)
-        rows_per_gate = min(max(int(rows_per_gate), -1) or most, most)
+        rows_per_gate = int(rows_per_gate)
+        if rows_per_gate < 0:
+            rows_per_gate = -1  # (refused)
+        elif rows_per_gate == 0 or rows_per_gate > P:
+            rows_per_gate = P or 1  # (one row for all, however many more it says)
         gate_ptr = _vector(gate, "gate", -(-P // rows_per_gate) * C if P and rows_per_gate > 0 else gate.numel())
     return _Norm(P, C, kind, F32 if like is None else _dtype(weights), 0, y_ptr, h_ptr, ld_y, ld_h, _vector(w_post, "w_post", C),
                  _vector(w_pre, "w_pre", C), gate_ptr, rows_per_gate, skip, scale, eps)
