@@ -591,6 +591,8 @@ def stream_info(header_bytes):
 
 
 # ---- a block of a network in 8-bit floating point ----
+# Like every call of this module these are not recorded by torch's autograd: what they return has no history, whatever their
+# inputs require.  The gradients are f8_matmul_backward and block_norm_backward.
 
 _KINDS = {}    # torch type -> F32, BF16, F16; filled with torch's first use
 _FORMATS = {}  # torch type -> E4M3, E5M2

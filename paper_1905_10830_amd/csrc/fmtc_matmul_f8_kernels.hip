@@ -265,9 +265,9 @@ __global__ __launch_bounds__(64 * kRowsWaves) void k_f8_matmul_rows(Product p, u
 // Rows of 128 bytes in LDS, the 16-byte pieces of a row exchanged by a key of the row, so that 16 lanes that read the same
 // piece of 16 rows touch every bank once.  The results leave through LDS too, 64 columns of a row at a time.
 //
-// bf16 results, 4096^3 / 8192^3: f32 scales 62 to 67 / 473 us (2320 TFLOP/s; an fma for each result and block), power-of-two
-// scales 64 / 420 us (2610; the matrix instructions, at the clock that their power leaves).  f32 results: f32 scales
-// 150 to 178 / 1060 us, power-of-two scales 114 / 750 us (1465; widening shares the issue slots).
+// bf16 results, 4096^3 / 8192^3, on the device: f32 scales 64 / 444 to 458 us (an fma for each result and block), power-of-two
+// scales 59 to 65 / 437 to 468 us (2350 to 2520 TFLOP/s; the matrix pipes are busy 45 / 60 % of the clocks, at 2.0 to 2.3 GHz).
+// f32 results: f32 scales 132 to 166 / 1060 us, power-of-two scales 104 to 114 / 753 to 835 us (widening shares the issue slots).
 template <int WM_, int WN_, int MT_, int STAGES_>
 struct Tile {
     static constexpr int WM = WM_, WN = WN_, MT = MT_, NT = 4, kStages = STAGES_;

@@ -8,8 +8,11 @@
 // Memory bound: 3 arrays read and 1 or 2 written (forward), 4 read and 2 written (backward), each once.  TPR lanes hold a
 // row in registers, VPT groups of 8 consecutive values each; group g of a lane starts at column 8 (g TPR + lane), so that
 // 16 lanes hold a block of 128.  A workgroup walks several rows: the weights stay in registers, and the next row's loads are
-// on their way while a row is worked on.  Forward 16384 x 4096 bf16 105 us (5.1 TB/s), 8192 x 8192 100 us, 8192 x 2048 f32 44 us;
-// backward 16384 x 4096 168 us (4.8 TB/s), 8192 x 4096 with a gate for 1024 rows 97 us; one row of 4096 3.8 us and 5.5 + 2 us.
+// on their way while a row is worked on.  Forward 16384 x 4096 bf16 105 us (5.1 TB/s), to codes 106 us, 8192 x 8192 100 us, 8192 x 2048
+// f32 44 us, 4096 x 16384 105 us; backward 16384 x 4096 168 us (4.8 TB/s), 8192 x 4096 with a gate for 1024 rows 95 us, in f32 167 + 5
+// us, 200704 x 64 29 + 5 us, 4096 x 16384 537 us; one row of 4096 4 us and 5.2 + 2 us.  Backward, 128 registers do not hold all of a row
+// where a lane has two groups (324 to 704 bytes of scratch memory a lane: 3.5 times the traffic's time); 12 to 116 bytes in f32 and
+// up to 128 channels show in no time.  (Forward, two groups: 12 to 380 bytes.)
 #include "fmtc_block.h"
 
 namespace fmtc {
