@@ -398,8 +398,8 @@ typedef struct fmtc_norm {
 } fmtc_norm;
 /* d_h_out (may be h itself, or NULL: not stored), d_n and n_codes (block_rows 1;
  * the codes of fmtc_f8_quantize for n before it is rounded): any may be NULL,
- * not all.  d_stats: f32 [2][rows], 1 / rms(y) (1 without w_post) and 1 / rms(h'),
- * what the backward pass needs; may be NULL. */
+ * not all.  d_stats: f32 [2][rows], 1 / rms(y) (1 without w_post) and 1 / rms(h')
+ * (1 without w_pre), what the backward pass needs; may be NULL. */
 fmtc_status fmtc_block_norm(const fmtc_norm *args, void *d_h_out, int64_t ld_h_out, void *d_n, int64_t ld_n,
                             const fmtc_f8 *n_codes, float *d_stats, void *hip_stream);
 /* The gradients, from dn (of n) and dh (of h', what reaches the stream from the
