@@ -414,6 +414,100 @@ fmtc_status fmtc_block_norm_backward(const fmtc_norm *args, const float *d_stats
                                      int64_t ld_dh_in, float *d_dw_post, float *d_dw_pre, float *d_dgate,
                                      void *d_workspace, size_t ws_bytes, void *hip_stream);
 
+/* ---- products in 8-bit integers ----
+ * The serving form of a layer whose weights are held as 8-bit integers: one
+ * scale for each row (token or pixel) of the activations and for each row
+ * (channel of the result) of the weights.  Sums are whole numbers in 32 bits and
+ * exact.  Conventions as above. */
+
+/* A matrix [rows][depth] of 8-bit integers: value = code * d_scales[row].  Codes:
+ * `ld` bytes from row to row, a multiple of 16 and at least depth rounded up to
+ * 128; the bytes from `depth` up to that are read and must be 0.  d_codes 16-byte
+ * aligned.  Depth up to 131071 (128 * 128 * depth has to fit 32 bits). */
+typedef struct fmtc_i8 {
+    void *d_codes;
+    float *d_scales;
+    int64_t rows, depth;
+    int64_t ld;
+} fmtc_i8;
+
+/* Quantizes d_x [rows][cols]: per row s = max(a * (1 / 127), 2^-126), a the largest
+ * magnitude, code = x * (1 / s) to the nearest whole number, ties to even (1 / 127,
+ * 1 / s and both products rounded to f32).  A row with an infinity or a NaN gets
+ * codes 0 and a scale that is not a number: so do all results of it.  The zeros
+ * behind the depth are written too. */
+fmtc_status fmtc_i8_quantize(const void *d_x, fmtc_dtype type, int64_t rows, int64_t cols, int64_t ld_x,
+                             const fmtc_i8 *out, void *hip_stream);
+
+/* out[m][n] = (sum_k a[m][k] b[n][k]) s_a[m] s_b[n] (+ d_bias[n]), the sum exact, then
+ * rounded to f32, as after each factor and the bias (f32, may be NULL); one
+ * rounding to out_type at the end.  Workspace: 256-byte aligned,
+ * fmtc_i8_matmul_workspace_size(rows of a, rows of b, depth) bytes (may be 0: then
+ * NULL is fine). */
+size_t fmtc_i8_matmul_workspace_size(int64_t M, int64_t N, int64_t K);
+fmtc_status fmtc_i8_matmul(const fmtc_i8 *a, const fmtc_i8 *b, const float *d_bias, void *d_out, fmtc_dtype out_type,
+                           int64_t ld_out, void *d_workspace, size_t ws_bytes, void *hip_stream);
+
+/* A layer: d_x [rows][w->depth] quantized by rows, times w: the same numbers as
+ * fmtc_i8_quantize and fmtc_i8_matmul.  Workspace: 256-byte aligned,
+ * fmtc_i8_linear_workspace_size(rows, w->rows, w->depth) bytes. */
+size_t fmtc_i8_linear_workspace_size(int64_t rows, int64_t N, int64_t K);
+fmtc_status fmtc_i8_linear(const void *d_x, fmtc_dtype type, int64_t rows, int64_t ld_x, const fmtc_i8 *w,
+                           const float *d_bias, void *d_out, fmtc_dtype out_type, int64_t ld_out, void *d_workspace,
+                           size_t ws_bytes, void *hip_stream);
+
+/* ---- group norm with an activation, channels last ----
+ * `samples` maps of rows_per_sample rows (pixels) of C channels in `groups` groups
+ * of C / groups neighbours, 1 <= C <= 8192.  Over the rows and channels of a
+ * sample's group: mean, variance (of all values, not one less), r = 1 / sqrt(variance + eps);
+ *     z = weight * (x - mean) * r + bias       y = act(z)
+ * act: z, max(z, 0) (NaN stays NaN), or z / (1 + e^-z).  x, y, dy and dx are `type`; weight and
+ * bias (NULL: 1 and 0) f32 or `type`.  Statistics are summed in f64. */
+typedef enum fmtc_act { FMTC_ACT_NONE = 0, FMTC_ACT_RELU = 1, FMTC_ACT_SILU = 2 } fmtc_act;
+typedef struct fmtc_gnorm {
+    int64_t samples, rows_per_sample;
+    int32_t C, groups, type, weight_type, act;
+    float eps;
+    const void *d_x;
+    int64_t ld_x;
+    const void *d_weight, *d_bias;
+} fmtc_gnorm;
+/* d_y (may be d_x itself with the same row stride) and codes ([samples * rows_per_sample][C], the codes of
+ * fmtc_i8_quantize for y before it is rounded): one of them, or neither and
+ * d_stats.  d_stats: f32 [2][samples][groups], the means and r, what the backward pass needs;
+ * may be NULL.  Workspace: 256-byte aligned. */
+size_t fmtc_group_norm_workspace_size(int64_t samples, int64_t rows_per_sample, int C, int groups);
+fmtc_status fmtc_group_norm(const fmtc_gnorm *args, void *d_y, int64_t ld_y, const fmtc_i8 *codes, float *d_stats,
+                            void *d_workspace, size_t ws_bytes, void *hip_stream);
+/* The gradients, from dy (of y), x and the statistics of the forward call (eps is not
+ * read): d_dx (may be d_dy or d_x itself with the same row stride), d_dweight and d_dbias [C] in f32,
+ * any may be NULL.  The gradient of max(z, 0) at 0 is 0.  Sums over rows are in a fixed
+ * order; without rows d_dweight and d_dbias are 0. */
+size_t fmtc_group_norm_backward_workspace_size(int64_t samples, int64_t rows_per_sample, int C, int groups);
+fmtc_status fmtc_group_norm_backward(const fmtc_gnorm *args, const float *d_stats, const void *d_dy, int64_t ld_dy,
+                                     void *d_dx, int64_t ld_dx, float *d_dweight, float *d_dbias, void *d_workspace,
+                                     size_t ws_bytes, void *hip_stream);
+
+/* ---- the norm of many tensors, and clipping ----
+ * Of `count` arrays of n contiguous values (h_list is read during the call; its device arrays must not change place in
+ * a captured graph):
+ *     norm = scale * sqrt(sum of the squares of all values)                    summed in f64
+ *     out  = in * f,  f = scale * min(1, max_norm / (norm + eps))              (f rounded to f32, then the product)
+ * d_out may be d_in itself (with out_type = type); otherwise no array that is
+ * written may overlap another one of the list.  d_out NULL in all entries: the norm only (max_norm and eps are not
+ * read).  d_norm: f32 [1], may be NULL.  An infinite norm makes f 0, a norm that is not a
+ * number makes all outputs not a number.  scale >= 0, max_norm >= 0, eps >= 0, finite (max_norm: or infinite).  Workspace:
+ * 256-byte aligned.  Results do not depend on the run. */
+typedef struct fmtc_tensor {
+    const void *d_in;
+    void *d_out;
+    int64_t n;
+    int32_t type, out_type;
+} fmtc_tensor;
+size_t fmtc_clip_workspace_size(const fmtc_tensor *h_list, int64_t count);
+fmtc_status fmtc_clip(const fmtc_tensor *h_list, int64_t count, double max_norm, double scale, double eps,
+                      float *d_norm, void *d_workspace, size_t ws_bytes, void *hip_stream);
+
 /* ---- instrumentation (not part of the method) ----
  * fmtc_profile_enable(n > 0) creates n HIP event pairs per kernel; from then on
  * every kernel launch of the library carries a pair attached to its own

@@ -16,6 +16,8 @@ F32, BF16, F16 = range(3)
 E4M3, E5M2 = range(2)
 SCALE_F32, SCALE_E8M0 = range(2)
 F8_BLOCK = 128
+ACT_NONE, ACT_RELU, ACT_SILU = range(3)
+I8_DEPTH = 131071
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libfmtc.so")
@@ -33,6 +35,9 @@ EXPORTS = [
     "fmtc_encode_u8", "fmtc_decode_u8",
     "fmtc_f8_quantize", "fmtc_f8_matmul_workspace_size", "fmtc_f8_matmul", "fmtc_f8_matmul_backward_workspace_size",
     "fmtc_f8_matmul_backward", "fmtc_block_norm", "fmtc_block_norm_workspace_size", "fmtc_block_norm_backward",
+    "fmtc_i8_quantize", "fmtc_i8_matmul_workspace_size", "fmtc_i8_matmul", "fmtc_i8_linear_workspace_size", "fmtc_i8_linear",
+    "fmtc_group_norm_workspace_size", "fmtc_group_norm", "fmtc_group_norm_backward_workspace_size",
+    "fmtc_group_norm_backward", "fmtc_clip_workspace_size", "fmtc_clip",
     "fmtc_profile_enable", "fmtc_profile_kernels", "fmtc_profile_name", "fmtc_profile_read", "fmtc_profile_copy",
     "fmtc_test_option", "fmtc_test_projection",
 ]
@@ -53,6 +58,23 @@ class _Norm(ctypes.Structure):
                 ("d_w_post", ctypes.c_void_p), ("d_w_pre", ctypes.c_void_p), ("d_gate", ctypes.c_void_p),
                 ("rows_per_gate", ctypes.c_int64), ("skip", ctypes.c_float), ("scale", ctypes.c_float),
                 ("eps", ctypes.c_float)]
+
+
+class _I8(ctypes.Structure):
+    _fields_ = [("d_codes", ctypes.c_void_p), ("d_scales", ctypes.c_void_p), ("rows", ctypes.c_int64),
+                ("depth", ctypes.c_int64), ("ld", ctypes.c_int64)]
+
+
+class _GroupNorm(ctypes.Structure):
+    _fields_ = [("samples", ctypes.c_int64), ("rows_per_sample", ctypes.c_int64), ("C", ctypes.c_int32),
+                ("groups", ctypes.c_int32), ("type", ctypes.c_int32), ("weight_type", ctypes.c_int32),
+                ("act", ctypes.c_int32), ("eps", ctypes.c_float), ("d_x", ctypes.c_void_p), ("ld_x", ctypes.c_int64),
+                ("d_weight", ctypes.c_void_p), ("d_bias", ctypes.c_void_p)]
+
+
+class _Tensor(ctypes.Structure):
+    _fields_ = [("d_in", ctypes.c_void_p), ("d_out", ctypes.c_void_p), ("n", ctypes.c_int64), ("type", ctypes.c_int32),
+                ("out_type", ctypes.c_int32)]
 
 
 class FmtcError(RuntimeError):
@@ -132,6 +154,22 @@ def load_library():
     lib.fmtc_block_norm_workspace_size.restype = sz
     lib.fmtc_block_norm_backward.argtypes = [ctypes.POINTER(_Norm), vp, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp,
                                              sz, vp]
+    i8, gnorm, f64 = ctypes.POINTER(_I8), ctypes.POINTER(_GroupNorm), ctypes.c_double
+    lib.fmtc_i8_quantize.argtypes = [vp, i32, i64, i64, i64, i8, vp]
+    lib.fmtc_i8_matmul_workspace_size.argtypes = [i64, i64, i64]
+    lib.fmtc_i8_matmul_workspace_size.restype = sz
+    lib.fmtc_i8_matmul.argtypes = [i8, i8, vp, vp, i32, i64, vp, sz, vp]
+    lib.fmtc_i8_linear_workspace_size.argtypes = [i64, i64, i64]
+    lib.fmtc_i8_linear_workspace_size.restype = sz
+    lib.fmtc_i8_linear.argtypes = [vp, i32, i64, i64, i8, vp, vp, i32, i64, vp, sz, vp]
+    for name in ("fmtc_group_norm_workspace_size", "fmtc_group_norm_backward_workspace_size"):
+        getattr(lib, name).argtypes = [i64, i64, i32, i32]
+        getattr(lib, name).restype = sz
+    lib.fmtc_group_norm.argtypes = [gnorm, vp, i64, i8, vp, vp, sz, vp]
+    lib.fmtc_group_norm_backward.argtypes = [gnorm, vp, vp, i64, vp, i64, vp, vp, vp, sz, vp]
+    lib.fmtc_clip_workspace_size.argtypes = [ctypes.POINTER(_Tensor), i64]
+    lib.fmtc_clip_workspace_size.restype = sz
+    lib.fmtc_clip.argtypes = [ctypes.POINTER(_Tensor), i64, f64, f64, f64, vp, vp, sz, vp]
     lib.fmtc_last_error.restype = ctypes.c_char_p
     lib.fmtc_profile_enable.argtypes = [i32]
     lib.fmtc_profile_name.argtypes = [i32]
@@ -906,6 +944,301 @@ def block_norm_backward(dn, dh, y, h_out, stats, w_post, w_pre, gate=None, rows_
     _check(lib.fmtc_block_norm_backward(ctypes.byref(a), _vector(stats, "stats", 2 * P, torch.float32), dn_p, dn_ld, dh_p, dh_ld,
                                         dy_p, dy_ld, di_p, di_ld, ptr(dw_post), ptr(dw_pre), ptr(dgate), ws, size, _stream()))
     return dy, dh_in, dw_post, dw_pre, dgate
+
+
+# ---- products in 8-bit integers, group norm, clipped gradients ----
+# As above: nothing of this is recorded by torch's autograd.  All tensors of a call are on the current device.
+
+def _on_current(what, *tensors):
+    """Refuses tensors of another device than the one whose stream the call goes to."""
+    import torch
+
+    try:
+        here = torch._C._cuda_getDevice()
+    except AttributeError:
+        here = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != here:
+            raise ValueError(f"{what}: a tensor on {t.device}, the current device is {here}")
+
+
+class I8:
+    """A matrix [rows, depth] of 8-bit integers with a scale for each row (fmtc_i8): codes, a tensor [rows, ld] of torch.int8
+    (ld: depth rounded up to 128 or more, a multiple of 16, zeros behind the depth), and scales [rows] of torch.float32."""
+
+    __slots__ = ("_codes", "_scales", "_rows", "_depth", "_at_codes", "_at_scales", "_ref")
+
+    def __init__(self, codes, scales, depth):
+        import torch
+
+        try:
+            (rows, width), (n_scales,), (ld, step) = codes.shape, scales.shape, codes.stride()
+            ok = codes.is_cuda and scales.is_cuda and codes.dtype == torch.int8 and scales.dtype == torch.float32
+        except (AttributeError, ValueError):
+            ok = False
+        if not ok:
+            raise ValueError("I8: expected device tensors, codes 2-d of int8 and scales 1-d of float32")
+        if not 1 <= depth <= I8_DEPTH or width < -(-depth // F8_BLOCK) * F8_BLOCK or n_scales != rows:
+            raise ValueError(f"I8: codes {tuple(codes.shape)} and {n_scales} scales do not hold {rows} x {depth} values")
+        if codes.get_device() != scales.get_device():
+            raise ValueError("I8: codes and scales are on different devices")
+        if step != 1 or (rows > 1 and scales.stride(0) != 1):
+            raise ValueError("I8: the codes of a row and the scales have to be adjacent")
+        self._set(codes, scales, rows, depth, ld if rows > 1 else width // 16 * 16)
+
+    def _set(self, codes, scales, rows, depth, ld):
+        self._codes, self._scales, self._rows, self._depth = codes, scales, rows, depth
+        self._at_codes = at_codes = codes.data_ptr()
+        self._at_scales = at_scales = scales.data_ptr()
+        self._ref = ctypes.byref(_I8(at_codes, at_scales, rows, depth, ld))
+        return self
+
+    # What the library reads and writes was checked when the object was made: nothing of it is assigned anew.
+    codes = property(operator.attrgetter("_codes"))
+    scales = property(operator.attrgetter("_scales"))
+    rows = property(operator.attrgetter("_rows"))
+    depth = property(operator.attrgetter("_depth"))
+
+
+def i8_empty(rows, depth, device="cuda"):
+    """An I8 to be written by i8_quantize or group_norm."""
+    import torch
+
+    if rows < 0 or not 1 <= depth <= I8_DEPTH:
+        raise ValueError(f"i8_empty: {rows} x {depth} values")
+    ld = -(-depth // F8_BLOCK) * F8_BLOCK
+    return I8.__new__(I8)._set(_matrix(rows, ld, torch.int8, device), torch.empty(rows, dtype=torch.float32, device=device), rows,
+                               depth, ld)
+
+
+def _i8(q):
+    if q is None:
+        return None
+    if q._codes.data_ptr() != q._at_codes or q._scales.data_ptr() != q._at_scales:
+        which = "codes" if q._codes.data_ptr() != q._at_codes else "scales"
+        raise ValueError(f"I8: {which} are not in the memory that they had when it was made")
+    return q._ref
+
+
+def i8_quantize(x, out=None):
+    """Asynchronous.  x: device matrix [rows, cols] -> I8 [rows, cols] (out, or a new one)."""
+    ptr, kind, ld = _rows(x, "x")
+    rows, cols = x.shape
+    if out is None:
+        out = i8_empty(rows, cols, x.device)
+    _on_current("i8_quantize", x, out._codes)
+    _check(load_library().fmtc_i8_quantize(ptr, kind, rows, cols, ld, _i8(out), _stream()))
+    return out
+
+
+def i8_matmul_workspace_size(M, N, K):
+    return load_library().fmtc_i8_matmul_workspace_size(M, N, K)
+
+
+def _i8_out(M, N, out, dtype, device):
+    if out is None:
+        out = _matrix(M, N, dtype, device)
+        return out, out.data_ptr(), _dtype(dtype), N
+    return (out, *_rows(out, "out", N, M, dtype))
+
+
+def i8_matmul(a, b, bias=None, out=None, dtype=None, workspace=None):
+    """Asynchronous.  a: I8 [M, K], b: I8 [N, K] -> a b^T + bias [M, N] in `dtype` (bf16 unless given, or out's)."""
+    import torch
+
+    M, N = a._rows, b._rows
+    out, ptr, kind, ld = _i8_out(M, N, out, dtype or (torch.bfloat16 if out is None else None), a._codes.device)
+    _on_current("i8_matmul", a._codes, b._codes, bias, out, workspace)
+    lib = load_library()
+    workspace, ws, size = _workspace(workspace, lib.fmtc_i8_matmul_workspace_size(M, N, a._depth), out.device)
+    _check(lib.fmtc_i8_matmul(_i8(a), _i8(b), _vector(bias, "bias", N, torch.float32), ptr, kind, ld, ws, size, _stream()))
+    return out
+
+
+def i8_linear_workspace_size(rows, N, K):
+    return load_library().fmtc_i8_linear_workspace_size(rows, N, K)
+
+
+def i8_linear(x, w, bias=None, out=None, dtype=None, workspace=None):
+    """Asynchronous.  x: device matrix [M, K], quantized by rows, times w: I8 [N, K] -> x w^T + bias [M, N] in `dtype` (x's
+    unless given, or out's).  The same numbers as i8_matmul(i8_quantize(x), w)."""
+    import torch
+
+    M, N = len(x), w._rows
+    x_ptr, x_kind, x_ld = _rows(x, "x", w._depth)
+    out, ptr, kind, ld = _i8_out(M, N, out, dtype or (x.dtype if out is None else None), x.device)
+    _on_current("i8_linear", x, w._codes, bias, out, workspace)
+    lib = load_library()
+    workspace, ws, size = _workspace(workspace, lib.fmtc_i8_linear_workspace_size(M, N, w._depth), out.device)
+    _check(lib.fmtc_i8_linear(x_ptr, x_kind, M, x_ld, _i8(w), _vector(bias, "bias", N, torch.float32), ptr, kind, ld, ws, size,
+                              _stream()))
+    return out
+
+
+def _group_norm_args(x, groups, weight, bias, rows_per_sample, act, eps):
+    x_ptr, kind, ld = _rows(x, "x")
+    P, C = x.shape
+    rows = int(rows_per_sample) or P
+    if rows < 0 or (rows and P % rows):
+        raise ValueError(f"rows_per_sample: {rows} rows a sample, {P} in all")
+    like = weight if weight is not None else bias
+    weights = x.dtype if like is None else like.dtype
+    if weight is not None and bias is not None and bias.dtype != weights:
+        raise ValueError("weight and bias have different types")
+    return _GroupNorm(P // rows if rows else 0, rows, C, groups, kind, _dtype(weights), act, eps, x_ptr, ld,
+                      _vector(weight, "weight", C), _vector(bias, "bias", C))
+
+
+def group_norm_workspace_size(P, C, groups, rows_per_sample=0):
+    rows = rows_per_sample or P
+    return load_library().fmtc_group_norm_workspace_size(P // rows if rows else 0, rows, C, groups)
+
+
+def group_norm(x, groups, weight=None, bias=None, rows_per_sample=0, act=ACT_NONE, eps=1e-5, out=None, stats=None, workspace=None):
+    """Asynchronous.  y = act(weight (x - mean) r + bias) of maps held channels last: x [P, C], rows_per_sample rows (0: all)
+    each, mean and r = 1 / sqrt(variance + eps) over the rows and the C / groups neighbouring channels of a sample's group.
+    act: ACT_NONE, ACT_RELU or ACT_SILU.  out: a tensor (may be x) or an I8 to write y to (None: a new tensor, False: not
+    stored).  stats: the f32 tensor [2, samples, groups] (means, r) that the backward pass needs, or True for a new one.
+    -> (y, stats), None where there is none."""
+    import torch
+
+    a = _group_norm_args(x, groups, weight, bias, rows_per_sample, act, eps)
+    P, C = x.shape
+    y_ptr, y_ld, codes = None, C, None
+    if out is None:
+        out = _matrix(P, C, x.dtype, x.device)
+        y_ptr = out.data_ptr()
+    elif out is False:
+        out = None
+    elif isinstance(out, I8):
+        codes = out
+    else:
+        y_ptr, _, y_ld = _rows(out, "out", C, P, x.dtype)
+    if stats is True:
+        stats = torch.empty((2, a.samples, groups), dtype=torch.float32, device=x.device)
+    elif stats is False:
+        stats = None
+    _on_current("group_norm", x, weight, bias, codes._codes if codes is not None else out, stats, workspace)
+    s_ptr = _vector(stats, "stats", 2 * a.samples * groups, torch.float32)
+    lib = load_library()
+    workspace, ws, size = _workspace(workspace, lib.fmtc_group_norm_workspace_size(a.samples, a.rows_per_sample, C, groups), x.device)
+    _check(lib.fmtc_group_norm(ctypes.byref(a), y_ptr, y_ld, _i8(codes), s_ptr, ws, size, _stream()))
+    return out, stats
+
+
+def group_norm_backward_workspace_size(P, C, groups, rows_per_sample=0):
+    rows = rows_per_sample or P
+    return load_library().fmtc_group_norm_backward_workspace_size(P // rows if rows else 0, rows, C, groups)
+
+
+def group_norm_backward(dy, x, stats, groups, weight=None, bias=None, rows_per_sample=0, act=ACT_NONE, dx=None, workspace=None):
+    """Asynchronous.  dy: gradients of y; x, weight, bias, rows_per_sample and act as in the forward call, stats as it left
+    them.  dx: the tensor to write to (may be dy or x; None: a new one, False: not wanted).  -> (dx, dweight, dbias), the last
+    two in f32, None where there is no such input."""
+    import torch
+
+    a = _group_norm_args(x, groups, weight, bias, rows_per_sample, act, 0.0)
+    P, C = x.shape
+    dy_ptr, _, dy_ld = _rows(dy, "dy", C, P, x.dtype)
+    dx_ptr, dx_ld = None, C
+    if dx is None:
+        dx = _matrix(P, C, x.dtype, x.device)
+        dx_ptr = dx.data_ptr()
+    elif dx is False:
+        dx = None
+    else:
+        dx_ptr, _, dx_ld = _rows(dx, "dx", C, P, x.dtype)
+    dweight, dbias = (None if t is None else torch.empty(C, dtype=torch.float32, device=x.device) for t in (weight, bias))
+    _on_current("group_norm_backward", dy, x, stats, weight, bias, dx, workspace)
+    s_ptr = _vector(stats, "stats", 2 * a.samples * groups, torch.float32)
+    lib = load_library()
+    workspace, ws, size = _workspace(workspace, lib.fmtc_group_norm_backward_workspace_size(a.samples, a.rows_per_sample, C, groups), x.device)
+    _check(lib.fmtc_group_norm_backward(ctypes.byref(a), s_ptr, dy_ptr, dy_ld, dx_ptr, dx_ld,
+                                        None if dweight is None else dweight.data_ptr(), None if dbias is None else dbias.data_ptr(),
+                                        ws, size, _stream()))
+    return dx, dweight, dbias
+
+
+def _overlap(spans):
+    """spans: (first byte, end, written, which tensor) -> whether a written one shares memory with one of another tensor."""
+    last_end = last_written = (0, None)  # the furthest end so far, and that of what is written: (end, which)
+    for start, end, written, which in sorted(spans):
+        for reach, other in (last_end, last_written) if written else (last_written,):
+            if reach > start and other != which:
+                return True
+        last_end = max(last_end, (end, which), key=lambda e: e[0])
+        if written:
+            last_written = max(last_written, (end, which), key=lambda e: e[0])
+    return False
+
+
+class Tensors:
+    """Tensors whose norm is taken together (fmtc_clip), with those that their scaled values are written to: themselves, or
+    `out`, as many of the same sizes (f32, bf16 or f16 each).  All contiguous, on one device; none that is written may share
+    memory with another tensor.  The object keeps them, not their values: it serves as long as they stay where they are."""
+
+    __slots__ = ("_tensors", "_out", "_at", "_list", "_norm_list", "_bytes")
+
+    def __init__(self, tensors, out=None):
+        tensors = list(tensors)
+        outs = tensors if out is None else list(out)
+        if len(outs) != len(tensors):
+            raise ValueError(f"Tensors: {len(tensors)} tensors, {len(outs)} outputs")
+        for t in tensors + outs:
+            try:
+                ok = t.is_cuda and t.is_contiguous()
+            except AttributeError:
+                ok = False
+            if not ok:
+                raise ValueError("Tensors: expected contiguous device tensors")
+            if t.get_device() != tensors[0].get_device():
+                raise ValueError("Tensors: tensors on different devices")
+        spans, n = [], len(tensors)
+        self._list, self._norm_list = (_Tensor * n)(), (_Tensor * n)()
+        for i, (t, o) in enumerate(zip(tensors, outs)):
+            if t.shape != o.shape:
+                raise ValueError(f"Tensors: an output of {tuple(o.shape)} for {tuple(t.shape)}")
+            at, at_out, size, kind, kind_out = t.data_ptr(), o.data_ptr(), t.numel(), _dtype(t.dtype), _dtype(o.dtype)
+            self._list[i] = _Tensor(at, at_out, size, kind, kind_out)
+            self._norm_list[i] = _Tensor(at, None, size, kind, kind_out)
+            if size:
+                if (at, kind) != (at_out, kind_out):
+                    spans.append((at, at + size * t.element_size(), False, (i, 0)))
+                spans.append((at_out, at_out + size * o.element_size(), True, (i, 1)))
+        if _overlap(spans):
+            raise ValueError("Tensors: an output shares memory with another tensor")
+        self._tensors, self._out = tensors, outs
+        self._at = [t.data_ptr() for t in tensors], [t.data_ptr() for t in outs]
+        self._bytes = load_library().fmtc_clip_workspace_size(self._list, n)
+
+    tensors = property(lambda self: tuple(self._tensors))
+    out = property(lambda self: tuple(self._out))
+
+    def _call(self, entries, max_norm, scale, eps, norm, workspace):
+        import torch
+
+        if [t.data_ptr() for t in self._tensors] != self._at[0] or \
+                (self._out is not self._tensors and [t.data_ptr() for t in self._out] != self._at[1]):
+            raise ValueError("Tensors: a tensor is not in the memory that it had when the object was made")
+        device = self._tensors[0].device if self._tensors else torch.device("cuda", torch.cuda.current_device())
+        if norm is None:
+            norm = torch.empty(1, dtype=torch.float32, device=device)
+        _on_current("Tensors", norm, self._tensors[0] if self._tensors else None, workspace)
+        workspace, ws, size = _workspace(workspace, self._bytes, device)
+        _check(load_library().fmtc_clip(entries, len(entries), max_norm, scale, eps, _vector(norm, "norm", 1, torch.float32), ws, size,
+                                        _stream()))
+        return norm
+
+    def workspace_size(self):
+        return self._bytes
+
+    def norm(self, scale=1.0, norm=None, workspace=None):
+        """Asynchronous.  -> f32 tensor [1] (`norm`, or a new one): scale * sqrt(sum of the squares of all values)."""
+        return self._call(self._norm_list, 0.0, scale, 0.0, norm, workspace)
+
+    def clip(self, max_norm, scale=1.0, eps=1e-6, norm=None, workspace=None):
+        """Asynchronous.  out = tensor * scale * min(1, max_norm / (norm + eps)) -> norm, as above."""
+        return self._call(self._list, max_norm, scale, eps, norm, workspace)
 
 
 TEST_STATIC_TWO_KERNELS, TEST_DECODE_ONE_ROW, TEST_SHORT_WAITS = 0, 1, 2

@@ -34,6 +34,23 @@ hipError_t launch_block_norm_backward(const fmtc_norm& a, const float* d_stats, 
                                       int64_t ld_dh_in, float* d_dw_post, float* d_dw_pre, float* d_dgate,
                                       void* d_ws, hipStream_t s);
 
+// values [rows][cols] -> codes and a scale for each row
+hipError_t launch_i8_quantize(const void* d_x, int type, int64_t rows, int64_t cols, int64_t ld_x, const fmtc_i8& out, hipStream_t s);
+size_t matmul_i8_workspace(int64_t M, int64_t N, int64_t K);
+hipError_t launch_i8_matmul(const fmtc_i8& a, const fmtc_i8& b, const float* d_bias, void* d_out, int out_type, int64_t ld_out,
+                            void* d_ws, hipStream_t s);
+
+size_t group_norm_workspace(int64_t samples, int64_t rows, int C, int groups);
+hipError_t launch_group_norm(const fmtc_gnorm& a, void* d_y, int64_t ld_y, const fmtc_i8* codes, float* d_stats, void* d_ws,
+                             hipStream_t s);
+size_t group_norm_backward_workspace(int64_t samples, int64_t rows, int C, int groups);
+hipError_t launch_group_norm_backward(const fmtc_gnorm& a, const float* d_stats, const void* d_dy, int64_t ld_dy, void* d_dx,
+                                      int64_t ld_dx, float* d_dweight, float* d_dbias, void* d_ws, hipStream_t s);
+
+size_t clip_workspace(const fmtc_tensor* list, int64_t count);
+hipError_t launch_clip(const fmtc_tensor* list, int64_t count, double max_norm, double scale, double eps, float* d_norm,
+                       void* d_ws, hipStream_t s);
+
 // ---- device helpers ----
 struct bf16 { uint16_t bits; };
 
@@ -203,6 +220,60 @@ __device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d) 
     }
     return (uint32_t)r;
 }
+// ---- 8-bit integers with a scale per row ----
+// The scale of a row from the largest of its magnitudes' bits (which compare as the magnitudes do; infinities and NaN are
+// above all numbers: then the scale is not a number and the codes are 0).  -> the factor that values are multiplied by
+__device__ __forceinline__ float i8_row_scale(uint32_t amax_bits, float* held) {
+    const bool finite = amax_bits < 0x7f800000u;
+    const float s = fmaxf(__uint_as_float(amax_bits) * (1.f / 127.f), 0x1p-126f);
+    *held = finite ? s : __uint_as_float(0x7fc00000u);
+    return finite ? 1.f / s : 0.f;
+}
+// four codes, the first in the lowest byte.  The product is rounded before the sum rounds it to a whole number (of up to
+// 127, in the sum's lowest byte); a row that is not finite has factor 0, and its NaN become 0 here.
+__device__ __forceinline__ uint32_t i8_encode4(const float* v, float inv) {
+#pragma clang fp contract(off)
+    uint32_t q[4];
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        const float t = v[i] * inv;
+        q[i] = __float_as_uint(t + 0x1.8p23f);
+    }
+    const uint32_t lo = __builtin_amdgcn_perm(q[1], q[0], 0x0c0c0400u), hi = __builtin_amdgcn_perm(q[3], q[2], 0x04000c0cu);
+    return lo | hi;
+}
+__device__ __forceinline__ uint32_t amax_bits8(const float (&v)[8]) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        const uint32_t b = __float_as_uint(v[i]) & 0x7fffffffu;
+        m = b > m ? b : m;
+    }
+    return m;
+}
+// largest of the bits over TPR lanes (16, or whole wavefronts); `part`: a word for each wavefront of the workgroup, free
+// until the next barrier behind the call
+template <int TPR>
+__device__ __forceinline__ uint32_t row_max_bits(uint32_t m, uint32_t* part) {
+    auto larger = [](uint32_t a, uint32_t b) { return a > b ? a : b; };
+    m = larger(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x128, 0xf, 0xf, true));
+    m = larger(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x124, 0xf, 0xf, true));
+    m = larger(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x122, 0xf, 0xf, true));
+    m = larger(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x121, 0xf, 0xf, true));
+    if constexpr (TPR >= 64) {
+        m = larger(m, (uint32_t)__shfl_xor((int)m, 16, 64));
+        m = larger(m, (uint32_t)__shfl_xor((int)m, 32, 64));
+    }
+    if constexpr (TPR > 64) {
+        const int first = threadIdx.x / TPR * (TPR / 64);
+        if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = m;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < TPR / 64; i++) m = larger(m, part[first + i]);
+    }
+    return m;
+}
+
 template <int SCALE>
 __device__ __forceinline__ void store_scale(void* d_scales, int64_t at, uint32_t held) {
     if constexpr (SCALE == FMTC_SCALE_F32)

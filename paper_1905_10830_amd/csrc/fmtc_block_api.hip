@@ -280,3 +280,228 @@ fmtc_status fmtc_block_norm_backward(const fmtc_norm* args, const float* d_stats
 }
 
 }  // extern "C"
+
+namespace {
+
+constexpr int64_t kMaxI8Depth = 131071;  // 128 * 128 * depth fits 32 bits
+
+fmtc_status check_i8(const char* who, const char* what, const fmtc_i8* q) {
+    if (!q) return set_error(FMTC_EINVAL, "%s: %s is NULL", who, what);
+    if (!side_ok(q->rows, 0) || q->depth < 1 || q->depth > kMaxI8Depth)
+        return set_error(FMTC_EINVAL, "%s: %s is %lld x %lld (depth 1 to %lld)", who, what, (long long)q->rows, (long long)q->depth, (long long)kMaxI8Depth);
+    if (q->rows == 0) return FMTC_OK;
+    if (!q->d_codes || !q->d_scales) return set_error(FMTC_EINVAL, "%s: codes or scales of %s are NULL", who, what);
+    if (!aligned(q->d_codes, 16) || !aligned(q->d_scales, 4))
+        return set_error(FMTC_EINVAL, "%s: codes of %s need 16-byte alignment, scales 4-byte", who, what);
+    if (q->ld % 16 != 0 || q->ld < blocks_of(q->depth) * kF8Block || q->ld > kMaxLd)
+        return set_error(FMTC_EINVAL, "%s: row stride %lld of %s: a multiple of 16, at least the depth rounded up to 128", who, (long long)q->ld, what);
+    return FMTC_OK;
+}
+
+fmtc_status check_i8_product(const char* who, int64_t M, int64_t N, const float* d_bias, const void* d_out, fmtc_dtype out_type, int64_t ld_out) {
+    if (!dtype_ok(out_type)) return set_error(FMTC_EINVAL, "%s: type %d", who, (int)out_type);
+    if (!aligned(d_bias, 4)) return set_error(FMTC_EINVAL, "%s: bias is not aligned to its type", who);
+    if (M == 0 || N == 0) return FMTC_OK;
+    CHECK(check_values(who, "out", d_out, out_type, M, N, ld_out));
+    if (((M + 15) / 16) * ((N + 15) / 16) > kMaxGroups) return set_error(FMTC_EINVAL, "%s: the output is too large", who);
+    return FMTC_OK;
+}
+
+// Workspace of fmtc_i8_linear: x as codes, its scales, and what the product needs
+struct LinearSpace { size_t codes, scales, product, product_bytes, total; };
+LinearSpace linear_space(int64_t M, int64_t N, int64_t K) {
+    LinearSpace w;
+    w.codes = 0;
+    w.scales = align_up((size_t)M * blocks_of(K) * kF8Block, 256);
+    w.product = align_up(w.scales + sizeof(float) * (size_t)M, 256);
+    w.product_bytes = matmul_i8_workspace(M, N, K);
+    w.total = w.product + w.product_bytes;
+    return w;
+}
+bool i8_depth_ok(int64_t K) { return K >= 1 && K <= kMaxI8Depth; }
+
+fmtc_status check_gnorm(const char* who, const fmtc_gnorm* a) {
+    if (!a) return set_error(FMTC_EINVAL, "%s: args is NULL", who);
+    if (!side_ok(a->samples, 0) || !side_ok(a->rows_per_sample, 0) || !side_ok(a->samples * a->rows_per_sample, 0))
+        return set_error(FMTC_EINVAL, "%s: %lld samples of %lld rows", who, (long long)a->samples, (long long)a->rows_per_sample);
+    if (a->C < 1 || a->C > 8192 || a->groups < 1 || a->C % a->groups != 0)
+        return set_error(FMTC_EINVAL, "%s: %d channels (1 to 8192) in %d groups", who, a->C, a->groups);
+    if (!dtype_ok(a->type) || (a->weight_type != FMTC_F32 && a->weight_type != a->type))
+        return set_error(FMTC_EINVAL, "%s: type %d, weights of type %d (f32 or the same)", who, a->type, a->weight_type);
+    if (a->act != FMTC_ACT_NONE && a->act != FMTC_ACT_RELU && a->act != FMTC_ACT_SILU) return set_error(FMTC_EINVAL, "%s: activation %d", who, a->act);
+    if (!aligned(a->d_weight, dtype_size(a->weight_type)) || !aligned(a->d_bias, dtype_size(a->weight_type)))
+        return set_error(FMTC_EINVAL, "%s: weight or bias are not aligned to their type", who);
+    return check_values(who, "x", a->d_x, a->type, a->samples * a->rows_per_sample, a->C, a->ld_x);
+}
+bool gnorm_size_ok(int64_t samples, int64_t rows, int C, int groups) {
+    return side_ok(samples, 1) && side_ok(rows, 1) && side_ok(samples * rows, 1) && C >= 1 && C <= 8192 && groups >= 1 && C % groups == 0;
+}
+// an array of a call that may be another one of it only as it is
+fmtc_status check_in_place(const char* who, const char* what, const void* out, int64_t ld_out, const char* of, const void* in, int64_t ld_in) {
+    if (out && out == in && ld_out != ld_in) return set_error(FMTC_EINVAL, "%s: %s is %s with another row stride", who, what, of);
+    return FMTC_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+fmtc_status fmtc_i8_quantize(const void* d_x, fmtc_dtype type, int64_t rows, int64_t cols, int64_t ld_x, const fmtc_i8* out, void* hip_stream) {
+    const char* who = "fmtc_i8_quantize";
+    if (!dtype_ok(type)) return set_error(FMTC_EINVAL, "%s: type %d", who, (int)type);
+    if (!side_ok(rows, 0) || !i8_depth_ok(cols)) return set_error(FMTC_EINVAL, "%s: %lld x %lld values", who, (long long)rows, (long long)cols);
+    CHECK(check_i8(who, "out", out));
+    if (out->rows != rows || out->depth != cols) return set_error(FMTC_EINVAL, "%s: out has another shape", who);
+    CHECK(check_values(who, "x", d_x, type, rows, cols, ld_x));
+    if (rows == 0) return FMTC_OK;
+    return hip_status(launch_i8_quantize(d_x, type, rows, cols, ld_x, *out, (hipStream_t)hip_stream), who);
+}
+
+size_t fmtc_i8_matmul_workspace_size(int64_t M, int64_t N, int64_t K) {
+    return side_ok(M, 1) && side_ok(N, 1) && i8_depth_ok(K) ? matmul_i8_workspace(M, N, K) : 0;
+}
+
+fmtc_status fmtc_i8_matmul(const fmtc_i8* a, const fmtc_i8* b, const float* d_bias, void* d_out, fmtc_dtype out_type,
+                           int64_t ld_out, void* d_workspace, size_t ws_bytes, void* hip_stream) {
+    const char* who = "fmtc_i8_matmul";
+    CHECK(check_i8(who, "a", a));
+    CHECK(check_i8(who, "b", b));
+    if (a->depth != b->depth) return set_error(FMTC_EINVAL, "%s: depths %lld and %lld", who, (long long)a->depth, (long long)b->depth);
+    CHECK(check_i8_product(who, a->rows, b->rows, d_bias, d_out, out_type, ld_out));
+    if (a->rows == 0 || b->rows == 0) return FMTC_OK;
+    CHECK(check_workspace(who, d_workspace, ws_bytes, matmul_i8_workspace(a->rows, b->rows, a->depth)));
+    return hip_status(launch_i8_matmul(*a, *b, d_bias, d_out, out_type, ld_out, d_workspace, (hipStream_t)hip_stream), who);
+}
+
+size_t fmtc_i8_linear_workspace_size(int64_t rows, int64_t N, int64_t K) {
+    return side_ok(rows, 1) && side_ok(N, 1) && i8_depth_ok(K) ? linear_space(rows, N, K).total : 0;
+}
+
+fmtc_status fmtc_i8_linear(const void* d_x, fmtc_dtype type, int64_t rows, int64_t ld_x, const fmtc_i8* w, const float* d_bias,
+                           void* d_out, fmtc_dtype out_type, int64_t ld_out, void* d_workspace, size_t ws_bytes, void* hip_stream) {
+    const char* who = "fmtc_i8_linear";
+    hipStream_t s = (hipStream_t)hip_stream;
+    if (!dtype_ok(type)) return set_error(FMTC_EINVAL, "%s: type %d", who, (int)type);
+    CHECK(check_i8(who, "w", w));
+    if (!side_ok(rows, 0)) return set_error(FMTC_EINVAL, "%s: %lld rows", who, (long long)rows);
+    CHECK(check_values(who, "x", d_x, type, rows, w->depth, ld_x));
+    CHECK(check_i8_product(who, rows, w->rows, d_bias, d_out, out_type, ld_out));
+    if (rows == 0 || w->rows == 0) return FMTC_OK;
+    const LinearSpace at = linear_space(rows, w->rows, w->depth);
+    CHECK(check_workspace(who, d_workspace, ws_bytes, at.total));
+    char* ws = static_cast<char*>(d_workspace);
+    const fmtc_i8 x{ws + at.codes, reinterpret_cast<float*>(ws + at.scales), rows, w->depth, blocks_of(w->depth) * kF8Block};
+    hipError_t e = launch_i8_quantize(d_x, type, rows, w->depth, ld_x, x, s);
+    if (e == hipSuccess) e = launch_i8_matmul(x, *w, d_bias, d_out, out_type, ld_out, ws + at.product, s);
+    return hip_status(e, who);
+}
+
+size_t fmtc_group_norm_workspace_size(int64_t samples, int64_t rows_per_sample, int C, int groups) {
+    return gnorm_size_ok(samples, rows_per_sample, C, groups) ? group_norm_workspace(samples, rows_per_sample, C, groups) : 0;
+}
+
+fmtc_status fmtc_group_norm(const fmtc_gnorm* args, void* d_y, int64_t ld_y, const fmtc_i8* codes, float* d_stats, void* d_workspace,
+                            size_t ws_bytes, void* hip_stream) {
+    const char* who = "fmtc_group_norm";
+    CHECK(check_gnorm(who, args));
+    if (!(args->eps >= 0.f)) return set_error(FMTC_EINVAL, "%s: eps is negative or not a number", who);
+    const int64_t rows = args->samples * args->rows_per_sample;
+    if (codes) {
+        CHECK(check_i8(who, "codes", codes));
+        if (codes->rows != rows || codes->depth != args->C) return set_error(FMTC_EINVAL, "%s: codes has to be [%lld][%d]", who, (long long)rows, args->C);
+    }
+    if (!aligned(d_stats, 4)) return set_error(FMTC_EINVAL, "%s: stats is not aligned to its type", who);
+    if (rows == 0) return FMTC_OK;
+    if (!d_y && !codes && !d_stats) return set_error(FMTC_EINVAL, "%s: no output", who);
+    if (d_y) {
+        CHECK(check_values(who, "y", d_y, args->type, rows, args->C, ld_y));
+        CHECK(check_in_place(who, "y", d_y, ld_y, "x", args->d_x, args->ld_x));
+    }
+    CHECK(check_workspace(who, d_workspace, ws_bytes, group_norm_workspace(args->samples, args->rows_per_sample, args->C, args->groups)));
+    return hip_status(launch_group_norm(*args, d_y, ld_y, codes, d_stats, d_workspace, (hipStream_t)hip_stream), who);
+}
+
+size_t fmtc_group_norm_backward_workspace_size(int64_t samples, int64_t rows_per_sample, int C, int groups) {
+    return gnorm_size_ok(samples, rows_per_sample, C, groups) ? group_norm_backward_workspace(samples, rows_per_sample, C, groups) : 0;
+}
+
+fmtc_status fmtc_group_norm_backward(const fmtc_gnorm* args, const float* d_stats, const void* d_dy, int64_t ld_dy, void* d_dx,
+                                     int64_t ld_dx, float* d_dweight, float* d_dbias, void* d_workspace, size_t ws_bytes,
+                                     void* hip_stream) {
+    const char* who = "fmtc_group_norm_backward";
+    hipStream_t s = (hipStream_t)hip_stream;
+    CHECK(check_gnorm(who, args));
+    if (!aligned(d_stats, 4) || !aligned(d_dweight, 4) || !aligned(d_dbias, 4))
+        return set_error(FMTC_EINVAL, "%s: stats, dweight or dbias are not aligned to their type", who);
+    const int64_t rows = args->samples * args->rows_per_sample;
+    if (rows == 0) {
+        hipError_t e = hipSuccess;
+        if (d_dweight) e = launch_fill_rows(d_dweight, 1, args->C, args->C, s);
+        if (e == hipSuccess && d_dbias) e = launch_fill_rows(d_dbias, 1, args->C, args->C, s);
+        return hip_status(e, who);
+    }
+    if (!d_dx && !d_dweight && !d_dbias) return set_error(FMTC_EINVAL, "%s: no output", who);
+    if (!d_stats) return set_error(FMTC_EINVAL, "%s: stats is NULL", who);
+    CHECK(check_values(who, "dy", d_dy, args->type, rows, args->C, ld_dy));
+    if (d_dx) {
+        CHECK(check_values(who, "dx", d_dx, args->type, rows, args->C, ld_dx));
+        CHECK(check_in_place(who, "dx", d_dx, ld_dx, "x", args->d_x, args->ld_x));
+        CHECK(check_in_place(who, "dx", d_dx, ld_dx, "dy", d_dy, ld_dy));
+    }
+    CHECK(check_workspace(who, d_workspace, ws_bytes, group_norm_backward_workspace(args->samples, args->rows_per_sample, args->C, args->groups)));
+    return hip_status(launch_group_norm_backward(*args, d_stats, d_dy, ld_dy, d_dx, ld_dx, d_dweight, d_dbias, d_workspace, s), who);
+}
+
+}  // extern "C"
+
+namespace {
+
+constexpr int64_t kMaxValues = (int64_t)1 << 40;  // of a list together
+
+fmtc_status check_list(const char* who, const fmtc_tensor* list, int64_t count) {
+    if (count < 0 || (count > 0 && !list)) return set_error(FMTC_EINVAL, "%s: list of %lld arrays is NULL or has no such length", who, (long long)count);
+    int64_t total = 0, written = 0, full = 0;
+    for (int64_t i = 0; i < count; i++) {
+        const fmtc_tensor& t = list[i];
+        if (t.n < 0 || t.n > kMaxValues || (total += t.n) > kMaxValues) return set_error(FMTC_EINVAL, "%s: array %lld has %lld values", who, (long long)i, (long long)t.n);
+        if (!dtype_ok(t.type) || (t.d_out && !dtype_ok(t.out_type)))
+            return set_error(FMTC_EINVAL, "%s: array %lld has type %d, out_type %d", who, (long long)i, t.type, t.out_type);
+        if (t.n == 0) continue;
+        full++;
+        written += t.d_out != nullptr;
+        if (!t.d_in) return set_error(FMTC_EINVAL, "%s: array %lld is NULL", who, (long long)i);
+        if (!aligned(t.d_in, dtype_size(t.type)) || (t.d_out && !aligned(t.d_out, dtype_size(t.out_type))))
+            return set_error(FMTC_EINVAL, "%s: array %lld is not aligned to its type", who, (long long)i);
+        if (t.d_out == t.d_in && t.out_type != t.type) return set_error(FMTC_EINVAL, "%s: array %lld is written in place in another type", who, (long long)i);
+    }
+    if (written != 0 && written != full) return set_error(FMTC_EINVAL, "%s: %lld of %lld arrays have an output", who, (long long)written, (long long)full);
+    return FMTC_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t fmtc_clip_workspace_size(const fmtc_tensor* h_list, int64_t count) {
+    return check_list("fmtc_clip_workspace_size", h_list, count) == FMTC_OK ? clip_workspace(h_list, count) : 0;
+}
+
+fmtc_status fmtc_clip(const fmtc_tensor* h_list, int64_t count, double max_norm, double scale, double eps, float* d_norm,
+                      void* d_workspace, size_t ws_bytes, void* hip_stream) {
+    const char* who = "fmtc_clip";
+    CHECK(check_list(who, h_list, count));
+    if (!(max_norm >= 0.0)) return set_error(FMTC_EINVAL, "%s: max_norm is negative or not a number", who);
+    if (!(scale >= 0.0 && scale <= 3.402823466385288e38) || !(eps >= 0.0 && eps <= 3.402823466385288e38))
+        return set_error(FMTC_EINVAL, "%s: scale or eps are negative or not finite", who);
+    if (!aligned(d_norm, 4)) return set_error(FMTC_EINVAL, "%s: norm is not aligned to its type", who);
+    bool write = false, any = false;
+    for (int64_t i = 0; i < count; i++) {
+        any = any || h_list[i].n > 0;
+        write = write || (h_list[i].d_out && h_list[i].n > 0);
+    }
+    if (!write && !d_norm) return any ? set_error(FMTC_EINVAL, "%s: no output", who) : FMTC_OK;
+    CHECK(check_workspace(who, d_workspace, ws_bytes, clip_workspace(h_list, count)));
+    return hip_status(launch_clip(h_list, count, max_norm, scale, eps, d_norm, d_workspace, (hipStream_t)hip_stream), who);
+}
+
+}  // extern "C"

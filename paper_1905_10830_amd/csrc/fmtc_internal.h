@@ -136,7 +136,8 @@ int test_option(int which);  // current value (0 unless a test set it)
 // When enabled, a launch carries a pair of events that the runtime attaches to the kernel's own dispatch, so
 // the elapsed time is the kernel's start-to-end time on the GPU (no bracket of separate marker commands).
 enum KernelId { K_PROJECT = 0, K_HISTOGRAM, K_TABLE, K_PACK, K_DECODE, K_COPY, K_QUANTIZE_U8, K_RECONSTRUCT_U8,
-                K_F8_QUANTIZE, K_F8_MATMUL, K_BLOCK_NORM, K_BLOCK_NORM_BACKWARD, K_COUNT };
+                K_F8_QUANTIZE, K_F8_MATMUL, K_BLOCK_NORM, K_BLOCK_NORM_BACKWARD, K_I8_QUANTIZE, K_I8_MATMUL, K_GROUP_NORM,
+                K_GROUP_NORM_BACKWARD, K_CLIP, K_COUNT };
 bool prof_next(int id, hipEvent_t* start, hipEvent_t* stop);
 
 template <class T>

@@ -21,7 +21,9 @@ Profiler g_prof;
 const char* const kNames[K_COUNT] = {"k_project_quantize", "k_histogram", "k_huffman_table",
                                      "k_pack",             "k_decode",    "k_copy",
                                      "k_quantize_u8",      "k_reconstruct_u8", "k_f8_quantize",
-                                     "k_f8_matmul",        "k_block_norm",     "k_block_norm_backward"};
+                                     "k_f8_matmul",        "k_block_norm",     "k_block_norm_backward",
+                                     "k_i8_quantize",      "k_i8_matmul",      "k_group_norm",
+                                     "k_group_norm_backward", "k_clip"};
 
 void release() {
     for (int k = 0; k < K_COUNT; k++) {
