@@ -475,8 +475,10 @@ typedef struct fmtc_gnorm {
 /* d_y (may be d_x itself with the same row stride) and codes ([samples * rows_per_sample][C], the codes of
  * fmtc_i8_quantize for y before it is rounded): one of them, or neither and
  * d_stats.  d_stats: f32 [2][samples][groups], the means and r, what the backward pass needs;
- * may be NULL.  Workspace: 256-byte aligned. */
-size_t fmtc_group_norm_workspace_size(int64_t samples, int64_t rows_per_sample, int C, int groups);
+ * may be NULL.  Workspace: 256-byte aligned, fmtc_group_norm_workspace_size bytes (to_codes: with `codes`; may be
+ * 0: then NULL is fine). */
+size_t fmtc_group_norm_workspace_size(int64_t samples, int64_t rows_per_sample, int C, int groups, fmtc_dtype type,
+                                      int to_codes);
 fmtc_status fmtc_group_norm(const fmtc_gnorm *args, void *d_y, int64_t ld_y, const fmtc_i8 *codes, float *d_stats,
                             void *d_workspace, size_t ws_bytes, void *hip_stream);
 /* The gradients, from dy (of y), x and the statistics of the forward call (eps is not

@@ -162,9 +162,10 @@ def load_library():
     lib.fmtc_i8_linear_workspace_size.argtypes = [i64, i64, i64]
     lib.fmtc_i8_linear_workspace_size.restype = sz
     lib.fmtc_i8_linear.argtypes = [vp, i32, i64, i64, i8, vp, vp, i32, i64, vp, sz, vp]
-    for name in ("fmtc_group_norm_workspace_size", "fmtc_group_norm_backward_workspace_size"):
-        getattr(lib, name).argtypes = [i64, i64, i32, i32]
-        getattr(lib, name).restype = sz
+    lib.fmtc_group_norm_workspace_size.argtypes = [i64, i64, i32, i32, i32, i32]
+    lib.fmtc_group_norm_workspace_size.restype = sz
+    lib.fmtc_group_norm_backward_workspace_size.argtypes = [i64, i64, i32, i32]
+    lib.fmtc_group_norm_backward_workspace_size.restype = sz
     lib.fmtc_group_norm.argtypes = [gnorm, vp, i64, i8, vp, vp, sz, vp]
     lib.fmtc_group_norm_backward.argtypes = [gnorm, vp, vp, i64, vp, i64, vp, vp, vp, sz, vp]
     lib.fmtc_clip_workspace_size.argtypes = [ctypes.POINTER(_Tensor), i64]
@@ -1089,9 +1090,12 @@ def _group_norm_args(x, groups, weight, bias, rows_per_sample, act, eps):
                       _vector(weight, "weight", C), _vector(bias, "bias", C))
 
 
-def group_norm_workspace_size(P, C, groups, rows_per_sample=0):
+def group_norm_workspace_size(P, C, groups, rows_per_sample=0, dtype=None, to_codes=False):
+    """Bytes for group_norm of values of `dtype` (bf16 unless given); to_codes: into an I8."""
+    import torch
+
     rows = rows_per_sample or P
-    return load_library().fmtc_group_norm_workspace_size(P // rows if rows else 0, rows, C, groups)
+    return load_library().fmtc_group_norm_workspace_size(P // rows if rows else 0, rows, C, groups, _dtype(dtype or torch.bfloat16), to_codes)
 
 
 def group_norm(x, groups, weight=None, bias=None, rows_per_sample=0, act=ACT_NONE, eps=1e-5, out=None, stats=None, workspace=None):
@@ -1121,7 +1125,7 @@ def group_norm(x, groups, weight=None, bias=None, rows_per_sample=0, act=ACT_NON
     _on_current("group_norm", x, weight, bias, codes._codes if codes is not None else out, stats, workspace)
     s_ptr = _vector(stats, "stats", 2 * a.samples * groups, torch.float32)
     lib = load_library()
-    workspace, ws, size = _workspace(workspace, lib.fmtc_group_norm_workspace_size(a.samples, a.rows_per_sample, C, groups), x.device)
+    workspace, ws, size = _workspace(workspace, lib.fmtc_group_norm_workspace_size(a.samples, a.rows_per_sample, C, groups, a.type, codes is not None), x.device)
     _check(lib.fmtc_group_norm(ctypes.byref(a), y_ptr, y_ld, _i8(codes), s_ptr, ws, size, _stream()))
     return out, stats
 
@@ -1217,8 +1221,9 @@ class Tensors:
     def _call(self, entries, max_norm, scale, eps, norm, workspace):
         import torch
 
-        if [t.data_ptr() for t in self._tensors] != self._at[0] or \
-                (self._out is not self._tensors and [t.data_ptr() for t in self._out] != self._at[1]):
+        address = torch.Tensor.data_ptr
+        if list(map(address, self._tensors)) != self._at[0] or \
+                (self._out is not self._tensors and list(map(address, self._out)) != self._at[1]):
             raise ValueError("Tensors: a tensor is not in the memory that it had when the object was made")
         device = self._tensors[0].device if self._tensors else torch.device("cuda", torch.cuda.current_device())
         if norm is None:

@@ -396,8 +396,8 @@ fmtc_status fmtc_i8_linear(const void* d_x, fmtc_dtype type, int64_t rows, int64
     return hip_status(e, who);
 }
 
-size_t fmtc_group_norm_workspace_size(int64_t samples, int64_t rows_per_sample, int C, int groups) {
-    return gnorm_size_ok(samples, rows_per_sample, C, groups) ? group_norm_workspace(samples, rows_per_sample, C, groups) : 0;
+size_t fmtc_group_norm_workspace_size(int64_t samples, int64_t rows_per_sample, int C, int groups, fmtc_dtype type, int to_codes) {
+    return gnorm_size_ok(samples, rows_per_sample, C, groups) && dtype_ok(type) ? group_norm_workspace(samples, rows_per_sample, C, groups, type, to_codes) : 0;
 }
 
 fmtc_status fmtc_group_norm(const fmtc_gnorm* args, void* d_y, int64_t ld_y, const fmtc_i8* codes, float* d_stats, void* d_workspace,
@@ -417,7 +417,7 @@ fmtc_status fmtc_group_norm(const fmtc_gnorm* args, void* d_y, int64_t ld_y, con
         CHECK(check_values(who, "y", d_y, args->type, rows, args->C, ld_y));
         CHECK(check_in_place(who, "y", d_y, ld_y, "x", args->d_x, args->ld_x));
     }
-    CHECK(check_workspace(who, d_workspace, ws_bytes, group_norm_workspace(args->samples, args->rows_per_sample, args->C, args->groups)));
+    CHECK(check_workspace(who, d_workspace, ws_bytes, group_norm_workspace(args->samples, args->rows_per_sample, args->C, args->groups, args->type, codes)));
     return hip_status(launch_group_norm(*args, d_y, ld_y, codes, d_stats, d_workspace, (hipStream_t)hip_stream), who);
 }
 

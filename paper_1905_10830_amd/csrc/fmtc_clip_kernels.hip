@@ -43,11 +43,24 @@ __device__ __forceinline__ double block_sum(double v, double* part) {
     return v;
 }
 
-// values [c0, c1) of an array of n: f(index, values) for 8 at a time, U loads on their way together
-template <class T, int U, class F>
-__device__ __forceinline__ void walk(const T* in, int64_t c0, int64_t c1, int64_t n, F&& f) {
-    int64_t c = c0 + 8 * threadIdx.x;
-    for (; c - 8 * threadIdx.x + U * kStep <= c1; c += U * kStep) {
+// How many values lie before the first one at a multiple of 128 bytes.  Pieces begin at such places: views into one buffer
+// begin anywhere, and wide accesses across the lines of the cache cost a third of the rate.
+template <class T>
+__device__ __forceinline__ int64_t values_before_line(const void* p) {
+    return (int64_t)((0 - (uintptr_t)p) % 128 / sizeof(T));
+}
+// The values of a piece: f(index, values) for 8 at a time from `lead` on, U loads on their way together, and one(index) for
+// each of the few before the first line and behind the last 8.
+template <class T, int U, class F, class G>
+__device__ __forceinline__ void walk(const T* in, int64_t index, int64_t piece, int64_t n, int64_t lead, F&& f, G&& one) {
+    const int64_t c1 = lead + (index + 1) * piece < n ? lead + (index + 1) * piece : n;
+    int64_t c = lead + index * piece;
+    if (index == 0)
+        for (int64_t i = threadIdx.x; i < (lead < n ? lead : n); i += kThreads) one(i);
+    const int64_t whole = c < c1 ? c + (c1 - c) / 8 * 8 : c;
+    for (int64_t i = whole + threadIdx.x; i < c1; i += kThreads) one(i);
+    c += 8 * threadIdx.x;
+    for (; c + (U - 1) * kStep < whole; c += U * kStep) {
         Raw<T> raw[U];
 #pragma unroll
         for (int u = 0; u < U; u++) raw[u].template load<false>(in, c + u * kStep, n);
@@ -59,10 +72,25 @@ __device__ __forceinline__ void walk(const T* in, int64_t c0, int64_t c1, int64_
             f(c + u * kStep, v);
         }
     }
-    for (; c < c1; c += kStep) {
+    for (; c < whole; c += kStep) {
         float v[8];
-        load8<true>(in, c, n, v);
+        load8<false>(in, c, n, v);
         f(c, v);
+    }
+}
+
+// 8 values, at a multiple of 16 bytes, past the caches, which keep what the first pass read
+template <class O>
+__device__ __forceinline__ void stream8(O* p, const float (&v)[8]) {
+    typedef uint32_t words __attribute__((ext_vector_type(4)));
+    O t[8];
+#pragma unroll
+    for (int i = 0; i < 8; i++) t[i] = from_f32<O>(v[i]);
+#pragma unroll
+    for (int i = 0; i < (int)sizeof t / 16; i++) {
+        words w;
+        __builtin_memcpy(&w, reinterpret_cast<const char*>(t) + 16 * i, 16);
+        __builtin_nontemporal_store(w, reinterpret_cast<words*>(reinterpret_cast<char*>(p) + 16 * i));
     }
 }
 
@@ -77,17 +105,22 @@ __global__ __launch_bounds__(kThreads) void k_clip_squares(List a, double* __res
     __shared__ double part[kThreads / 64];
     const uint32_t piece = blockIdx.x;
     const int k = find(a, piece);
-    const int64_t n = a.n[k], c0 = (int64_t)(piece - a.first[k]) * a.piece, c1 = c0 + a.piece < n ? c0 + a.piece : n;
     double s0 = 0.0, s1 = 0.0;
     with_kind(a.type[k], [&](auto ty) {
         using T = typename decltype(ty)::type;
-        walk<T, 4>(static_cast<const T*>(a.in[k]), c0, c1, n, [&](int64_t, const float (&v)[8]) {
+        const T* const in = static_cast<const T*>(a.in[k]);
+        walk<T, 4>(in, piece - a.first[k], a.piece, a.n[k], values_before_line<T>(in),
+                   [&](int64_t, const float (&v)[8]) {
 #pragma unroll
-            for (int i = 0; i < 8; i += 2) {
-                s0 = fma((double)v[i], (double)v[i], s0);
-                s1 = fma((double)v[i + 1], (double)v[i + 1], s1);
-            }
-        });
+                       for (int i = 0; i < 8; i += 2) {
+                           s0 = fma((double)v[i], (double)v[i], s0);
+                           s1 = fma((double)v[i + 1], (double)v[i + 1], s1);
+                       }
+                   },
+                   [&](int64_t c) {
+                       const double v = to_f32(in[c]);
+                       s0 = fma(v, v, s0);
+                   });
     });
     const double s = block_sum(s0 + s1, part);
     if (threadIdx.x == 0) sums[a.base + piece] = s;
@@ -107,18 +140,20 @@ __global__ __launch_bounds__(kThreads) void k_clip_scale(List a, const double* _
     const uint32_t piece = a.pieces - 1 - blockIdx.x;
     const int k = find(a, piece);
     if (f == 1.f && a.in[k] == a.out[k]) return;  // (in place, and nothing changes)
-    const int64_t n = a.n[k], c0 = (int64_t)(piece - a.first[k]) * a.piece, c1 = c0 + a.piece < n ? c0 + a.piece : n;
     with_kind(a.type[k], [&](auto ty) {
         with_kind(a.out_type[k], [&](auto to) {
             using T = typename decltype(ty)::type;
             using O = typename decltype(to)::type;
             O* const out = static_cast<O*>(a.out[k]);
-            walk<T, 4>(static_cast<const T*>(a.in[k]), c0, c1, n, [&](int64_t c, const float (&v)[8]) {
-                float w[8];
+            const T* const in = static_cast<const T*>(a.in[k]);
+            walk<T, 4>(in, piece - a.first[k], a.piece, a.n[k], values_before_line<O>(out),
+                       [&](int64_t c, const float (&v)[8]) {
+                           float w[8];
 #pragma unroll
-                for (int i = 0; i < 8; i++) w[i] = v[i] * f;
-                store8(out + c, n - c, w);
-            });
+                           for (int i = 0; i < 8; i++) w[i] = v[i] * f;
+                           stream8(out + c, w);
+                       },
+                       [&](int64_t c) { out[c] = from_f32<O>(to_f32(in[c]) * f); });
         });
     });
 }
@@ -131,22 +166,28 @@ int64_t piece_values(const fmtc_tensor* list, int64_t count) {
 }
 int64_t pieces_of(int64_t n, int64_t piece) { return (n + piece - 1) / piece; }
 
-// The arrays from *at on that fit a launch
-List take(const fmtc_tensor* list, int64_t count, int64_t piece, int64_t* at, uint32_t base) {
+// The arrays of launch `which`, kMost of those that have values; base: the pieces of the launches before it
+List take(const fmtc_tensor* list, int64_t count, int64_t piece, int64_t which) {
     List a{};
     a.piece = piece;
-    a.base = base;
+    int64_t before = which * kMost;
     int k = 0;
-    for (; *at < count && k < kMost; ++*at) {
-        const fmtc_tensor& t = list[*at];
+    for (int64_t i = 0; i < count && k < kMost; i++) {
+        const fmtc_tensor& t = list[i];
         if (t.n == 0) continue;
+        const uint32_t pieces = (uint32_t)pieces_of(t.n, piece);
+        if (before > 0) {
+            before--;
+            a.base += pieces;
+            continue;
+        }
         a.in[k] = t.d_in;
         a.out[k] = t.d_out;
         a.n[k] = t.n;
         a.first[k] = a.pieces;
         a.type[k] = (uint8_t)t.type;
         a.out_type[k] = (uint8_t)t.out_type;
-        a.pieces += (uint32_t)pieces_of(t.n, piece);
+        a.pieces += pieces;
         k++;
     }
     for (; k < kMost; k++) a.first[k] = ~0u;
@@ -165,23 +206,28 @@ size_t clip_workspace(const fmtc_tensor* list, int64_t count) {
 hipError_t launch_clip(const fmtc_tensor* list, int64_t count, double max_norm, double scale, double eps, float* d_norm, void* d_ws, hipStream_t s) {
     const int64_t piece = piece_values(list, count);
     double* const sums = static_cast<double*>(d_ws);
+    int64_t full = 0;
     uint32_t n_sums = 0;
-    hipError_t e = hipSuccess;
-    for (int64_t at = 0; at < count && e == hipSuccess;) {
-        const List a = take(list, count, piece, &at, n_sums);
-        if (a.pieces) e = launch(K_CLIP, k_clip_squares, dim3(a.pieces), dim3(kThreads), 0, s, a, sums);
-        n_sums += a.pieces;
-    }
     bool write = false;
-    for (int64_t i = 0; i < count; i++) write = write || (list[i].d_out && list[i].n);
+    for (int64_t i = 0; i < count; i++)
+        if (list[i].n) {
+            full++;
+            n_sums += (uint32_t)pieces_of(list[i].n, piece);
+            write = write || list[i].d_out;
+        }
+    const int64_t launches = (full + kMost - 1) / kMost;
+    hipError_t e = hipSuccess;
+    List a{};
+    for (int64_t k = 0; k < launches && e == hipSuccess; k++) {
+        a = take(list, count, piece, k);
+        e = launch(K_CLIP, k_clip_squares, dim3(a.pieces), dim3(kThreads), 0, s, a, sums);
+    }
     if (e == hipSuccess && d_norm && !write) {
-        List none{};
+        const List none{};
         return launch(K_CLIP, k_clip_scale, dim3(1), dim3(kThreads), 0, s, none, sums, n_sums, max_norm, scale, eps, d_norm);
     }
-    if (!write) return e;
-    for (int64_t at = 0; at < count && e == hipSuccess;) {
-        const List a = take(list, count, piece, &at, 0);
-        if (!a.pieces) continue;
+    for (int64_t k = launches - 1; k >= 0 && write && e == hipSuccess; k--) {
+        if (k < launches - 1) a = take(list, count, piece, k);
         e = launch(K_CLIP, k_clip_scale, dim3(a.pieces), dim3(kThreads), 0, s, a, sums, n_sums, max_norm, scale, eps, d_norm);
         d_norm = nullptr;
     }

@@ -3,8 +3,11 @@
 //   forward:   z = w x^ + b,  y = act(z)
 //   backward:  dz = dy act'(z);  db = sum dz,  dw = sum dz x^  (over all rows);
 //              dx = r (w dz - A - x^ B),  A = sum of w dz / (S D),  B = sum of w dz x^ / (S D)  (over the sample's group)
-// Memory bound.  A thread takes 8 neighbouring channels (a lane of the row's LX) of every LY-th row, so that whole rows are
-// read whatever the groups are; the sums meet in LDS by channel and are added up by group there.
+// Memory bound.  A workgroup works on a slab of a sample's rows: W neighbouring channels, whole groups.  A thread takes 8
+// neighbouring ones of them (a lane of the LX of a row) of every LY-th row; the sums meet in LDS and are added up by group
+// there.  Where a slab fits the registers of one workgroup, all is done with one read of the values (k_group_norm_once,
+// k_group_norm_backward_once); else the rows are cut in chunks, whose sums one kernel leaves in the workspace and the next one
+// adds up before it reads the values again.
 #include "fmtc_block.h"
 
 namespace fmtc {
@@ -13,221 +16,170 @@ namespace {
 
 struct Maps {
     int64_t samples, S, ld;
-    int C, G, D, LX, LY;     // LX lanes a row, LY rows at a time; D channels a group
+    int C, G, D;          // D channels a group
+    int W, groups, slabs, LX, LY; // channels and groups of a slab (the last one may have fewer), slabs of a row; lanes of a row, rows at a time
+    int pre;                      // sums by group: a thread's 8 channels leave 1 << pre values (see fold)
     const void *x, *w, *b;
     int weight_type;
-    int64_t chunks, per;     // parts of a sample's rows, rows of a part
+    int64_t chunks, per;  // parts of a sample's rows, rows of a part
 };
 
-template <class F>
-__device__ __forceinline__ void with_weights(int type, F&& f) {
-    if (type == FMTC_F32) f(Type<float>{});
-    else if (type == FMTC_BF16) f(Type<bf16>{});
-    else f(Type<_Float16>{});
-}
-// channels c .. c + 7 of the weight (1 where there is none) or of the bias (0)
+// What a workgroup works on.  Workgroups go to the 8 XCDs in turn: each XCD gets a range of them, so that slabs that share
+// lines of memory run on one and find them in its cache.
+struct Place {
+    int64_t n, k;
+    int slab, c0, width, g0, groups;  // the slab's first channel, its channels, its first group, its groups
+    __device__ __forceinline__ Place(const Maps& p, int64_t parts, uint32_t first) {
+        const uint32_t total = gridDim.x - first, b = blockIdx.x - first, each = total / 8, more = total % 8, xcd = b % 8;
+        const uint32_t at = xcd * each + (xcd < more ? xcd : more) + b / 8, row = at / (uint32_t)p.slabs;
+        slab = (int)(at - row * p.slabs);
+        n = row / (uint32_t)parts;
+        k = row - n * parts;
+        c0 = slab * p.W;
+        width = p.C - c0 < p.W ? p.C - c0 : p.W;
+        g0 = slab * p.groups;
+        groups = p.G - g0 < p.groups ? p.G - g0 : p.groups;
+    }
+};
+
+// i / d for i up to 2^20, r = 1 / d: what is added keeps the product further from the next whole number than its roundings go
+__device__ __forceinline__ int quotient(int i, float r) { return (int)(((float)i + 0.5f) * r); }
+
+// channels c .. c + 7 of the weight (1 where there is none) or of the bias (0); f32, or the type of the values
+template <class T, bool RAGGED>
 __device__ __forceinline__ void load_param(const void* p, int type, int c, int C, float without, float (&v)[8]) {
 #pragma unroll
     for (int i = 0; i < 8; i++) v[i] = without;
-    if (p)
-        with_weights(type, [&](auto ty) {
-            using W = typename decltype(ty)::type;
-            load8<true>(static_cast<const W*>(p), c, C, v);
-        });
+    if (p) {
+        if (type == FMTC_F32) load8<RAGGED>(static_cast<const float*>(p), c, C, v);
+        else load8<RAGGED>(static_cast<const T*>(p), c, C, v);
+    }
+}
+// f(i, group) for each of 8 channels from c on (of a slab of `width`; those past it: the last one's group)
+template <class F>
+__device__ __forceinline__ void each_group(int c, int width, int D, F&& f) {
+    int g = quotient(c, 1.f / (float)D), left = D - (c - g * D);
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        f(i, g);
+        left--;
+        const bool next = left == 0 && c + i + 1 < width;
+        g = next ? g + 1 : g;
+        left = next ? D : left;
+    }
 }
 
-// e = exp(-|z|) keeps both the sigmoid and what it lacks to 1 exact to a few roundings
 template <int ACT>
 __device__ __forceinline__ float act(float z) {
     if constexpr (ACT == FMTC_ACT_RELU) return z < 0.f ? 0.f : z;
     if constexpr (ACT == FMTC_ACT_SILU) return z * __builtin_amdgcn_rcpf(1.f + __expf(-z));
     return z;
 }
+// (silu: p (1 + z (1 - p)); from z = 17 on p is 1 and z (1 - p) is lost, which is less than 17 half steps of it)
 template <int ACT>
 __device__ __forceinline__ float act_gradient(float z) {
     if constexpr (ACT == FMTC_ACT_RELU) return z > 0.f ? 1.f : z <= 0.f ? 0.f : z;
     if constexpr (ACT == FMTC_ACT_SILU) {
-        const float e = __expf(-fabsf(z)), r = __builtin_amdgcn_rcpf(1.f + e), er = e * r;
-        const float p = z >= 0.f ? r : er, q = z >= 0.f ? er : r;
-        return p * fmaf(z, q, 1.f);
+        const float p = __builtin_amdgcn_rcpf(1.f + __expf(-z));
+        return p * fmaf(z, 1.f - p, 1.f);
     }
     return 1.f;
 }
 
-// Sums over the rows and channels of each group of what is in `red` ([LY][8 LX]): f(group, sum) by one thread each.  lanes:
-// how many work on a group, a power of two up to 64.
-template <class V, class F>
-__device__ __forceinline__ void group_sums(const V* red, const Maps& p, int lanes, F&& f) {
-    const int l = threadIdx.x & (lanes - 1), step = blockDim.x / lanes, n = p.LY * p.D;
-    for (int g = threadIdx.x / lanes; g < p.G; g += step) {
-        V sum = 0;
-        for (int i = l; i < n; i += lanes) {
-            const int y = i / p.D, c = i - y * p.D;
-            sum += red[y * 8 * p.LX + g * p.D + c];
-        }
-        for (int o = lanes >> 1; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
-        if (l == 0) f(g, sum);
-    }
-}
-__device__ __forceinline__ int group_lanes(int G) {
+// f(group, lane, lanes) on `lanes` neighbouring threads for each of n things: a power of two up to 64 of them, such that all
+// threads have work.
+template <class F>
+__device__ __forceinline__ void spread(int n, F&& f) {
     int lanes = 64;
-    while (lanes > 1 && lanes * G > (int)blockDim.x) lanes >>= 1;
-    return lanes;
+    while (lanes > 1 && lanes * n > (int)blockDim.x) lanes >>= 1;
+    for (int i = threadIdx.x / lanes; i < n; i += blockDim.x / lanes) f(i, (int)threadIdx.x & (lanes - 1), lanes);
+}
+template <class V>
+__device__ __forceinline__ V lanes_sum(V v, int lanes) {
+    for (int o = lanes >> 1; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+    return v;
 }
 
-constexpr int kUnroll = 4;  // rows of a thread on their way together
-
-// The sums of the values and of their squares, of each part of a sample's rows and each group: part[sample][chunk][group].
-// In f64, so that the variance is right however far the mean is from 0 (f64 runs at the rate of f32 here).
-template <class T, bool RAGGED>
-__global__ __launch_bounds__(1024) void k_group_norm_sums(Maps p, double2* __restrict__ part) {
-    extern __shared__ __attribute__((aligned(16))) double red[];
-    const int t = threadIdx.x, ly = t / p.LX, lx = t - ly * p.LX, c = 8 * lx;
-    const int64_t n = blockIdx.x / p.chunks, k = blockIdx.x - n * p.chunks;
-    const int64_t r0 = k * p.per, r1 = r0 + p.per < p.S ? r0 + p.per : p.S;
-    const bool live = ly < p.LY;
-    double s[8] = {}, q[8] = {};
-    if (live) {
-        const T* const x = static_cast<const T*>(p.x) + n * p.S * p.ld;
-        for (int64_t r = r0 + ly; r < r1; r += (int64_t)kUnroll * p.LY) {
-            Raw<T> raw[kUnroll];
+// A thread's sums by channel to 1 << pre sums of neighbours of one group: 1 where a group has a multiple of 8 channels, 8 / D
+// for 2 and 4 of them, else 8 as they are.
+constexpr int fold_of(int D) { return D % 8 == 0 ? 0 : D == 4 ? 1 : D == 2 ? 2 : 3; }
+__device__ __forceinline__ void fold(double (&s)[8], int pre) {
+    if (pre < 3)
 #pragma unroll
-            for (int u = 0; u < kUnroll; u++) {
-                const int64_t at = r + (int64_t)u * p.LY;
-                raw[u].template load<RAGGED>(x + (at < r1 ? at : r) * p.ld, c, p.C);
-            }
-#pragma unroll
-            for (int u = 0; u < kUnroll; u++) {
-                if constexpr (RAGGED) raw[u].settle(c, p.C);
-                raw[u].zero_unless(r + (int64_t)u * p.LY < r1);
-#pragma unroll
-                for (int i = 0; i < 8; i++) {
-                    const double v = raw[u][i];
-                    s[i] += v;
-                    q[i] = fma(v, v, q[i]);
-                }
-            }
-        }
-    }
-    const int lanes = group_lanes(p.G);
-    double2* const to = part + (n * p.chunks + k) * p.G;
-    double* const mine = red + (ly * p.LX + lx) * 8;
-    if (live)
-#pragma unroll
-        for (int i = 0; i < 8; i++) mine[i] = s[i];
-    __syncthreads();
-    group_sums(red, p, lanes, [&](int g, double v) { to[g].x = v; });
-    __syncthreads();
-    if (live)
-#pragma unroll
-        for (int i = 0; i < 8; i++) mine[i] = q[i];
-    __syncthreads();
-    group_sums(red, p, lanes, [&](int g, double v) { to[g].y = v; });
+        for (int i = 0; i < 4; i++) s[i] = s[2 * i] + s[2 * i + 1];
+    if (pre < 2) s[0] += s[1], s[1] = s[2] + s[3];
+    if (pre < 1) s[0] += s[1];
 }
 
-// mean and r of each group of sample n into LDS, and, by the sample's first workgroup, where the caller wants them
-__device__ __forceinline__ void finish_stats(const Maps& p, const double2* part, int64_t n, float eps, float* mean_r, float* stats, bool first) {
-    const int lanes = group_lanes(p.G), l = threadIdx.x & (lanes - 1), step = blockDim.x / lanes;
-    const double count = (double)p.S * (double)p.D;
-    for (int g = threadIdx.x / lanes; g < p.G; g += step) {
-        double s = 0.0, q = 0.0;
-        for (int64_t k = l; k < p.chunks; k += lanes) {
-            const double2 v = part[(n * p.chunks + k) * p.G + g];
-            s += v.x;
-            q += v.y;
+// The sums s of the values and q of their squares of all threads, by group: f(group of the slab, sum, sum of squares) on one
+// thread each.  red: 2 << pre doubles a thread (a thread's values apart by the number of threads, so that neighbours write to
+// neighbouring banks).
+template <class F>
+__device__ __forceinline__ void sums_by_group(const Maps& p, const Place& at, bool live, double (&s)[8], double (&q)[8], double* red, F&& f) {
+    const int T = blockDim.x, pre = p.pre, D = p.D << pre >> 3, n = 1 << pre;  // values of a group in a row
+    const float rD = 1.f / (float)D;
+    fold(s, pre);
+    fold(q, pre);
+#pragma unroll
+    for (int i = 0; i < 8; i++)
+        if (i < n) {
+            red[i * T + threadIdx.x] = live ? s[i] : 0.0;
+            red[(n + i) * T + threadIdx.x] = live ? q[i] : 0.0;
         }
-        for (int o = lanes >> 1; o > 0; o >>= 1) {
-            s += __shfl_xor(s, o, 64);
-            q += __shfl_xor(q, o, 64);
-        }
-        if (l == 0) {
-            const double mean = s / count, var = q / count - mean * mean;
-            const float m = (float)mean, r = (float)(1.0 / sqrt((var < 0.0 ? 0.0 : var) + (double)eps));
-            mean_r[g] = m;
-            mean_r[p.G + g] = r;
-            if (stats && first) {
-                stats[n * p.G + g] = m;
-                stats[(p.samples + n) * p.G + g] = r;
-            }
-        }
-    }
     __syncthreads();
+    spread(at.groups, [&](int g, int l, int lanes) {
+        double a = 0.0, b = 0.0;
+        for (int i = l; i < p.LY * D; i += lanes) {
+            const int y = quotient(i, rD), v = g * D + i - y * D, from = (v & (n - 1)) * T + y * p.LX + (v >> pre);
+            a += red[from];
+            b += red[n * T + from];
+        }
+        a = lanes_sum(a, lanes);
+        b = lanes_sum(b, lanes);
+        if (l == 0) f(g, a, b);
+    });
 }
-
-template <class T, bool RAGGED, int ACT>
-__global__ __launch_bounds__(1024) void k_group_norm_apply(Maps p, const double2* __restrict__ part, int64_t parts, int64_t rows, float eps,
-                                                           T* y, int64_t ld_y, float* __restrict__ stats) {
-    extern __shared__ __attribute__((aligned(16))) float mean_r[];
-    const int64_t n = blockIdx.x / parts, k = blockIdx.x - n * parts;
-    finish_stats(p, part, n, eps, mean_r, stats, k == 0);
-    if (!y) return;
-    const int t = threadIdx.x, ly = t / p.LX, lx = t - ly * p.LX, c = 8 * lx;
-    if (ly >= p.LY) return;
-    float w[8], b[8], m[8];
-    load_param(p.w, p.weight_type, c, p.C, 1.f, w);
-    load_param(p.b, p.weight_type, c, p.C, 0.f, b);
+template <class T>
+__device__ __forceinline__ void add(const Raw<T>& raw, double (&s)[8], double (&q)[8]) {
 #pragma unroll
     for (int i = 0; i < 8; i++) {
-        const int g = (c + i < p.C ? c + i : p.C - 1) / p.D;
-        m[i] = mean_r[g];
-        w[i] *= mean_r[p.G + g];
+        const double v = raw[i];
+        s[i] += v;
+        q[i] = fma(v, v, q[i]);
     }
-    const int64_t r0 = k * rows, r1 = r0 + rows < p.S ? r0 + rows : p.S;
-    const T* const x = static_cast<const T*>(p.x) + n * p.S * p.ld;
-    T* const out = y + n * p.S * ld_y;
-    for (int64_t r = r0 + ly; r < r1; r += (int64_t)kUnroll * p.LY) {
-        Raw<T> raw[kUnroll];
-#pragma unroll
-        for (int u = 0; u < kUnroll; u++) {
-            const int64_t at = r + (int64_t)u * p.LY;
-            raw[u].template load<RAGGED>(x + (at < r1 ? at : r) * p.ld, c, p.C);
-        }
-#pragma unroll
-        for (int u = 0; u < kUnroll; u++) {
-            const int64_t at = r + (int64_t)u * p.LY;
-            if (at >= r1) break;
-            if constexpr (RAGGED) raw[u].settle(c, p.C);
-            float v[8];
-#pragma unroll
-            for (int i = 0; i < 8; i++) v[i] = act<ACT>(fmaf(raw[u][i] - m[i], w[i], b[i]));
-            store8(out + at * ld_y + c, RAGGED ? p.C - c : 8, v);
-        }
+}
+// From sums in f64, so that the variance is right however far the mean is from 0 (reading 100 MB takes the same time with f64
+// sums as with f32 ones, 5.1 TB/s).  stats: the caller's, or NULL
+__device__ __forceinline__ void finish(const Maps& p, const Place& at, int g, double s, double q, float eps, float* mean_r, float* stats) {
+    const double count = (double)p.S * (double)p.D, mean = s / count, var = q / count - mean * mean;
+    // (a variance that is not a number stays that)
+    const float m = (float)mean, r = (float)(1.0 / sqrt((var < 0.0 ? 0.0 : var) + (double)eps));
+    mean_r[g] = m;
+    mean_r[at.groups + g] = r;
+    if (stats) {
+        stats[at.n * p.G + at.g0 + g] = m;
+        stats[(p.samples + at.n) * p.G + at.g0 + g] = r;
     }
 }
 
-// To codes with a scale for each row: TPR lanes hold a row; mean, weight and bias of each channel in LDS.
-constexpr int codes_threads(int TPR) { return TPR < 256 ? 256 : TPR; }
-template <class T, bool RAGGED, int TPR>
-__global__ __launch_bounds__(codes_threads(TPR)) void k_group_norm_codes(Maps p, const double2* __restrict__ part, int64_t parts, int64_t rows,
-                                                                         float eps, int act_kind, fmtc_i8 out, T* y, int64_t ld_y,
-                                                                         float* __restrict__ stats) {
-    extern __shared__ __attribute__((aligned(16))) float mean_r[];
-    __shared__ uint32_t turns[2][codes_threads(TPR) / 64];
-    constexpr int kRows = codes_threads(TPR) / TPR;
-    const int64_t n = blockIdx.x / parts, k = blockIdx.x - n * parts;
-    finish_stats(p, part, n, eps, mean_r, stats, k == 0);
-    const int lane = threadIdx.x % TPR, c = 8 * lane, width = (p.C + kF8Block - 1) / kF8Block * kF8Block;
-    float w[8], b[8], m[8];
-    load_param(p.w, p.weight_type, c, p.C, 1.f, w);
-    load_param(p.b, p.weight_type, c, p.C, 0.f, b);
-#pragma unroll
-    for (int i = 0; i < 8; i++) {
-        const bool there = c + i < p.C;
-        const int g = (there ? c + i : p.C - 1) / p.D;
-        m[i] = there ? mean_r[g] : 0.f;
-        w[i] = there ? w[i] * mean_r[p.G + g] : 0.f;
-        b[i] = there ? b[i] : 0.f;
+// y = act((x - m) w + b) of a thread's 8 channels (c: of the slab's).  The parameters set out before the statistics are there.
+struct Scale {
+    float m[8], w[8], b[8];
+    template <class T, bool RAGGED>
+    __device__ __forceinline__ void load(const Maps& p, const Place& at, int c) {
+        load_param<T, RAGGED>(p.w, p.weight_type, at.c0 + c, p.C, 1.f, w);
+        load_param<T, RAGGED>(p.b, p.weight_type, at.c0 + c, p.C, 0.f, b);
     }
-    const int64_t r0 = k * rows, r1 = r0 + rows < p.S ? r0 + rows : p.S;
-    const T* const x = static_cast<const T*>(p.x) + n * p.S * p.ld;
-    int turn = 0;
-    for (int64_t r = r0; r < r1; r += kRows, turn ^= 1) {  // (all threads take every round: there are barriers in it)
-        const int64_t mine = r + threadIdx.x / TPR, at = mine < r1 ? mine : r1 - 1;
-        Raw<T> raw;
-        raw.template load<RAGGED>(x + at * p.ld, c, p.C);
-        if constexpr (RAGGED) raw.settle(c, p.C);
-        raw.zero_unless(c < p.C);
-        float v[8];
+    __device__ __forceinline__ void settle(const Maps& p, const Place& at, int c, const float* mean_r) {
+        each_group(c < at.width ? c : at.width - 1, at.width, p.D, [&](int i, int g) {
+            const bool there = c + i < at.width;
+            m[i] = there ? mean_r[g] : 0.f;
+            w[i] = there ? w[i] * mean_r[at.groups + g] : 0.f;
+            b[i] = there ? b[i] : 0.f;
+        });
+    }
+    template <class T>
+    __device__ __forceinline__ void apply(const Raw<T>& raw, int act_kind, float (&v)[8]) const {
 #pragma unroll
         for (int i = 0; i < 8; i++) v[i] = fmaf(raw[i] - m[i], w[i], b[i]);
         if (act_kind == FMTC_ACT_RELU) {
@@ -237,35 +189,337 @@ __global__ __launch_bounds__(codes_threads(TPR)) void k_group_norm_codes(Maps p,
 #pragma unroll
             for (int i = 0; i < 8; i++) v[i] = act<FMTC_ACT_SILU>(v[i]);
         }
-        float held;
-        const float inv = i8_row_scale(row_max_bits<TPR>(amax_bits8(v), turns[turn]), &held);
-        if (mine >= r1) continue;
-        const int64_t row = n * p.S + at;
-        if (c < width)
-            *reinterpret_cast<uint2*>(static_cast<uint8_t*>(out.d_codes) + row * out.ld + c) = make_uint2(i8_encode4(v, inv), i8_encode4(v + 4, inv));
-        if (lane == 0) out.d_scales[row] = held;
-        if (y && c < p.C) store8(y + row * ld_y + c, p.C - c, v);
+    }
+};
+
+struct Lane { int ly, lx, c; bool live; };
+__device__ __forceinline__ Lane lane_of(const Maps& p, const Place& at) {
+    const int t = threadIdx.x, ly = quotient(t, 1.f / (float)p.LX), lx = t - ly * p.LX;
+    return {ly, lx, 8 * lx, ly < p.LY && 8 * lx < at.width};
+}
+template <class T>
+__device__ __forceinline__ T* slab_of(void* base, int64_t ld, const Maps& p, const Place& at) {
+    return static_cast<T*>(base) + at.n * p.S * ld + at.c0;
+}
+template <class T>
+__device__ __forceinline__ const T* slab_of(const void* base, int64_t ld, const Maps& p, const Place& at) {
+    return static_cast<const T*>(base) + at.n * p.S * ld + at.c0;
+}
+
+constexpr int kUnroll = 4;  // rows of a thread on their way together
+
+// A slab in the registers of a workgroup, R rows a thread.
+template <class T, bool RAGGED, int R>
+__global__ __launch_bounds__(1024) void k_group_norm_once(Maps p, float eps, int act_kind, T* y, int64_t ld_y, float* __restrict__ stats) {
+    extern __shared__ __attribute__((aligned(16))) double red[];
+    const Place at(p, 1, 0);
+    const Lane me = lane_of(p, at);
+    float* const mean_r = reinterpret_cast<float*>(red + (2 << p.pre) * blockDim.x);
+    const T* const x = slab_of<T>(p.x, p.ld, p, at);
+    Raw<T> raw[R];
+    Scale scale;
+    double s[8] = {}, q[8] = {};
+    if (me.live) {
+#pragma unroll
+        for (int u = 0; u < R; u++) {
+            const int64_t r = me.ly + (int64_t)u * p.LY;
+            raw[u].template load<RAGGED>(x + (r < p.S ? r : 0) * p.ld, me.c, at.width);
+        }
+        scale.load<T, RAGGED>(p, at, me.c);
+#pragma unroll
+        for (int u = 0; u < R; u++) {
+            if constexpr (RAGGED) raw[u].settle(me.c, at.width);
+            raw[u].zero_unless(me.ly + (int64_t)u * p.LY < p.S);
+            add(raw[u], s, q);
+        }
+    }
+    sums_by_group(p, at, me.live, s, q, red, [&](int g, double a, double b) { finish(p, at, g, a, b, eps, mean_r, stats); });
+    __syncthreads();
+    if (!me.live || !y) return;
+    scale.settle(p, at, me.c, mean_r);
+    T* const out = slab_of<T>(y, ld_y, p, at);
+#pragma unroll
+    for (int u = 0; u < R; u++) {
+        const int64_t r = me.ly + (int64_t)u * p.LY;
+        if (r >= p.S) break;
+        float v[8];
+        scale.apply(raw[u], act_kind, v);
+        store8(out + r * ld_y + me.c, RAGGED ? at.width - me.c : 8, v);
     }
 }
 
-// What a thread needs of its 8 channels for the gradients
-struct Channels {
-    float m[8], r[8], w[8], b[8];
-    __device__ __forceinline__ void load(const Maps& p, const float* stats, int64_t n, int c) {
-        load_param(p.w, p.weight_type, c, p.C, 1.f, w);
-        load_param(p.b, p.weight_type, c, p.C, 0.f, b);
+// The sums of the values and of their squares, of each part of a sample's rows and each group: part[sample][chunk][group].
+template <class T, bool RAGGED>
+__global__ __launch_bounds__(1024) void k_group_norm_sums(Maps p, double2* __restrict__ part) {
+    extern __shared__ __attribute__((aligned(16))) double red[];
+    const Place at(p, p.chunks, 0);
+    const Lane me = lane_of(p, at);
+    const int64_t r0 = at.k * p.per, r1 = r0 + p.per < p.S ? r0 + p.per : p.S;
+    double s[8] = {}, q[8] = {};
+    if (me.live) {
+        const T* const x = slab_of<T>(p.x, p.ld, p, at);
+        for (int64_t r = r0 + me.ly; r < r1; r += (int64_t)kUnroll * p.LY) {
+            Raw<T> raw[kUnroll];
 #pragma unroll
-        for (int i = 0; i < 8; i++) {
-            const int g = (c + i < p.C ? c + i : p.C - 1) / p.D;
-            m[i] = stats[n * p.G + g];
-            r[i] = stats[(p.samples + n) * p.G + g];
+            for (int u = 0; u < kUnroll; u++) {
+                const int64_t from = r + (int64_t)u * p.LY;
+                raw[u].template load<RAGGED>(x + (from < r1 ? from : r) * p.ld, me.c, at.width);
+            }
+#pragma unroll
+            for (int u = 0; u < kUnroll; u++) {
+                if constexpr (RAGGED) raw[u].settle(me.c, at.width);
+                raw[u].zero_unless(r + (int64_t)u * p.LY < r1);
+                add(raw[u], s, q);
+            }
         }
     }
+    double2* const to = part + (at.n * p.chunks + at.k) * p.G + at.g0;
+    sums_by_group(p, at, me.live, s, q, red, [&](int g, double a, double b) { to[g] = make_double2(a, b); });
+}
+
+// mean and r of each group of a slab into LDS, and, by the first workgroup of a slab, where the caller wants them
+__device__ __forceinline__ void finish_parts(const Maps& p, const Place& at, const double2* part, float eps, float* mean_r, float* stats) {
+    spread(at.groups, [&](int g, int l, int lanes) {
+        double s = 0.0, q = 0.0;
+        for (int64_t k = l; k < p.chunks; k += lanes) {
+            const double2 v = part[(at.n * p.chunks + k) * p.G + at.g0 + g];
+            s += v.x;
+            q += v.y;
+        }
+        s = lanes_sum(s, lanes);
+        q = lanes_sum(q, lanes);
+        if (l == 0) finish(p, at, g, s, q, eps, mean_r, at.k == 0 ? stats : nullptr);
+    });
+    __syncthreads();
+}
+
+template <class T, bool RAGGED>
+__global__ __launch_bounds__(1024) void k_group_norm_apply(Maps p, const double2* __restrict__ part, int64_t parts, int64_t rows, float eps,
+                                                           int act_kind, T* y, int64_t ld_y, float* __restrict__ stats) {
+    extern __shared__ __attribute__((aligned(16))) float mean_r[];
+    const Place at(p, parts, 0);
+    const Lane me = lane_of(p, at);
+    Scale scale;
+    scale.load<T, RAGGED>(p, at, me.c);
+    finish_parts(p, at, part, eps, mean_r, stats);
+    if (!y || !me.live) return;
+    scale.settle(p, at, me.c, mean_r);
+    const int64_t r0 = at.k * rows, r1 = r0 + rows < p.S ? r0 + rows : p.S;
+    const T* const x = slab_of<T>(p.x, p.ld, p, at);
+    T* const out = slab_of<T>(y, ld_y, p, at);
+    for (int64_t r = r0 + me.ly; r < r1; r += (int64_t)kUnroll * p.LY) {
+        Raw<T> raw[kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; u++) {
+            const int64_t from = r + (int64_t)u * p.LY;
+            raw[u].template load<RAGGED>(x + (from < r1 ? from : r) * p.ld, me.c, at.width);
+        }
+#pragma unroll
+        for (int u = 0; u < kUnroll; u++) {
+            const int64_t to = r + (int64_t)u * p.LY;
+            if (to >= r1) break;
+            if constexpr (RAGGED) raw[u].settle(me.c, at.width);
+            float v[8];
+            scale.apply(raw[u], act_kind, v);
+            store8(out + to * ld_y + me.c, RAGGED ? at.width - me.c : 8, v);
+        }
+    }
+}
+
+// To codes with a scale for each row: TPR lanes hold a row, VPT groups of 8 consecutive channels each.
+constexpr int codes_threads(int TPR) { return TPR < 256 ? 256 : TPR; }
+template <class T, bool RAGGED, int TPR, int VPT>
+__global__ __launch_bounds__(codes_threads(TPR)) void k_group_norm_codes(Maps p, const double2* __restrict__ part, int64_t parts, int64_t rows,
+                                                                         float eps, int act_kind, fmtc_i8 out, T* y, int64_t ld_y,
+                                                                         float* __restrict__ stats) {
+    extern __shared__ __attribute__((aligned(16))) float mean_r[];
+    __shared__ uint32_t turns[2][codes_threads(TPR) / 64];
+    constexpr int kRows = codes_threads(TPR) / TPR;
+    const Place at(p, parts, 0);
+    const int lane = threadIdx.x % TPR, width = (p.C + kF8Block - 1) / kF8Block * kF8Block;
+    const int64_t r0 = at.k * rows, r1 = r0 + rows < p.S ? r0 + rows : p.S;
+    const T* const x = slab_of<T>(p.x, p.ld, p, at);
+    Raw<T> next[VPT];
+    auto fetch = [&](int64_t r) {
+        const int64_t mine = r + threadIdx.x / TPR, from = mine < r1 ? mine : r1 - 1;
+#pragma unroll
+        for (int j = 0; j < VPT; j++) next[j].template load<RAGGED>(x + from * p.ld, 8 * (j * TPR + lane), p.C);
+    };
+    fetch(r0);
+    Scale scale[VPT];
+#pragma unroll
+    for (int j = 0; j < VPT; j++) scale[j].template load<T, RAGGED>(p, at, 8 * (j * TPR + lane));
+    finish_parts(p, at, part, eps, mean_r, stats);
+#pragma unroll
+    for (int j = 0; j < VPT; j++) scale[j].settle(p, at, 8 * (j * TPR + lane), mean_r);
+    int turn = 0;
+    for (int64_t r = r0; r < r1; r += kRows, turn ^= 1) {  // (all threads take every round: there may be barriers in it)
+        const int64_t mine = r + threadIdx.x / TPR, from = mine < r1 ? mine : r1 - 1;
+        Raw<T> raw[VPT];
+        float v[VPT][8];
+        uint32_t m = 0;
+#pragma unroll
+        for (int j = 0; j < VPT; j++) raw[j] = next[j];
+        if (r + kRows < r1) fetch(r + kRows);
+#pragma unroll
+        for (int j = 0; j < VPT; j++) {
+            const int c = 8 * (j * TPR + lane);
+            if constexpr (RAGGED) raw[j].settle(c, p.C);
+            raw[j].zero_unless(c < p.C);
+            scale[j].apply(raw[j], act_kind, v[j]);
+            const uint32_t b = amax_bits8(v[j]);
+            m = b > m ? b : m;
+        }
+        float held;
+        const float inv = i8_row_scale(row_max_bits<TPR>(m, turns[turn]), &held);
+        if (mine >= r1) continue;
+        const int64_t row = at.n * p.S + from;
+#pragma unroll
+        for (int j = 0; j < VPT; j++) {
+            const int c = 8 * (j * TPR + lane);
+            if (c < width)
+                *reinterpret_cast<uint2*>(static_cast<uint8_t*>(out.d_codes) + row * out.ld + c) = make_uint2(i8_encode4(v[j], inv), i8_encode4(v[j] + 4, inv));
+            if (y && c < p.C) store8(y + row * ld_y + c, p.C - c, v[j]);
+        }
+        if (lane == 0) out.d_scales[row] = held;
+    }
+}
+
+// ---- gradients ----
+// What a thread needs of its 8 channels: d = x - m, z = d a + b; x^ = d r only enters sums, to which r is a factor
+struct Channels {
+    float m[8], a[8], b[8];
+    template <class T, bool RAGGED>
+    __device__ __forceinline__ void load(const Maps& p, const Place& at, const float* stats, int c) {
+        load_param<T, RAGGED>(p.w, p.weight_type, at.c0 + c, p.C, 1.f, a);
+        load_param<T, RAGGED>(p.b, p.weight_type, at.c0 + c, p.C, 0.f, b);
+        const float *const mean = stats + at.n * p.G + at.g0, *const r = mean + p.samples * p.G;
+        each_group(c, at.width, p.D, [&](int i, int g) {
+            m[i] = mean[g];
+            a[i] *= r[g];
+        });
+    }
+    template <int ACT>
+    __device__ __forceinline__ float dz(int i, float x, float dy) const {
+        return ACT == FMTC_ACT_NONE ? dy : dy * act_gradient<ACT>(fmaf(x - m[i], a[i], b[i]));
+    }
 };
-template <int ACT>
-__device__ __forceinline__ void gradient(const Channels& ch, int i, float x, float dy, float* xh, float* dz) {
-    *xh = (x - ch.m[i]) * ch.r[i];
-    *dz = ACT == FMTC_ACT_NONE ? dy : dy * act_gradient<ACT>(fmaf(*xh, ch.w[i], ch.b[i]));
+
+// The sums of dz (s) and of dz d (q) of all threads, by channel of the slab, those of dz d times r: f(0 or 1, channel, sum) on
+// one thread each.  red: 16 floats a thread.
+template <class F>
+__device__ __forceinline__ void sums_by_channel(const Maps& p, const Place& at, const float* stats, bool live, const float (&s)[8],
+                                                const float (&q)[8], float* red, F&& f) {
+    const int T = blockDim.x;
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        red[i * T + threadIdx.x] = live ? s[i] : 0.f;
+        red[(8 + i) * T + threadIdx.x] = live ? q[i] : 0.f;
+    }
+    __syncthreads();
+    spread(2 * at.width, [&](int i, int l, int lanes) {
+        const int which = i >= at.width, c = i - which * at.width;
+        const float* const from = red + (8 * which + c % 8) * T + c / 8;
+        float sum = 0.f;
+        for (int y = l; y < p.LY; y += lanes) sum += from[y * p.LX];
+        sum = lanes_sum(sum, lanes);
+        if (l == 0) f(which, c, which ? sum * stats[(p.samples + at.n) * p.G + at.g0 + quotient(c, 1.f / (float)p.D)] : sum);
+    });
+}
+
+template <class T>
+__device__ __forceinline__ float weight_at(const Maps& p, int c) {
+    return !p.w ? 1.f : p.weight_type == FMTC_F32 ? static_cast<const float*>(p.w)[c] : to_f32(static_cast<const T*>(p.w)[c]);
+}
+// A and B of each group of the slab from the sums by channel, [2][width] with the weights in them, both in LDS
+__device__ __forceinline__ void group_terms(const Maps& p, const Place& at, const float* by_channel, float* ab) {
+    const float rcount = 1.f / ((float)p.S * (float)p.D);
+    spread(2 * at.groups, [&](int i, int l, int lanes) {
+        const int which = i >= at.groups, g = i - which * at.groups;
+        float sum = 0.f;
+        for (int c = l; c < p.D; c += lanes) sum += by_channel[which * at.width + g * p.D + c];
+        sum = lanes_sum(sum, lanes);
+        if (l == 0) ab[i] = sum * rcount;
+    });
+    __syncthreads();
+}
+// dx = r (w dz - A - x^ B) = a dz + (d D + E):  D = -r r B, E = -r A
+struct Terms {
+    float D[8], E[8];
+    __device__ __forceinline__ void load(const Maps& p, const Place& at, const float* stats, int c, const float* ab) {
+        const float* const rs = stats + (p.samples + at.n) * p.G + at.g0;
+        each_group(c, at.width, p.D, [&](int i, int g) {
+            const float r = rs[g];
+            E[i] = -r * ab[g];
+            D[i] = -r * (r * ab[at.groups + g]);
+        });
+    }
+    __device__ __forceinline__ float dx(const Channels& ch, int i, float x, float dz) const {
+        return fmaf(dz, ch.a[i], fmaf(x - ch.m[i], D[i], E[i]));
+    }
+};
+
+// A slab in the registers of a workgroup, R rows a thread: x as it is and dz in f32 (an activation's gradient is computed
+// once: it costs as much as all the rest).  part[sample][2][C]: the sums by channel
+template <class T, bool RAGGED, int ACT, int R>
+__global__ __launch_bounds__(512) void k_group_norm_backward_once(Maps p, const float* __restrict__ stats, const T* dy, int64_t ld_dy, T* dx,
+                                                                  int64_t ld_dx, float* __restrict__ part) {
+    extern __shared__ __attribute__((aligned(16))) float red_f[];
+    const Place at(p, 1, 0);
+    const Lane me = lane_of(p, at);
+    float *const by_channel = red_f + 16 * blockDim.x, *const ab = by_channel + 2 * at.width;
+    const T *const x = slab_of<T>(p.x, p.ld, p, at), *const g = slab_of<T>(dy, ld_dy, p, at);
+    Raw<T> raw[R];
+    float dz[R][8], s[8] = {}, q[8] = {};
+    Channels ch;
+    if (me.live) {
+        Raw<T> raw_g[R];
+#pragma unroll
+        for (int u = 0; u < R; u++) {
+            const int64_t r = me.ly + (int64_t)u * p.LY, from = r < p.S ? r : 0;
+            raw[u].template load<RAGGED>(x + from * p.ld, me.c, at.width);
+            raw_g[u].template load<RAGGED>(g + from * ld_dy, me.c, at.width);
+        }
+        ch.load<T, RAGGED>(p, at, stats, me.c);
+#pragma unroll
+        for (int u = 0; u < R; u++) {
+            if constexpr (RAGGED) raw[u].settle(me.c, at.width), raw_g[u].settle(me.c, at.width);
+            raw[u].zero_unless(me.ly + (int64_t)u * p.LY < p.S);
+            raw_g[u].zero_unless(me.ly + (int64_t)u * p.LY < p.S);
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                dz[u][i] = ch.dz<ACT>(i, raw[u][i], raw_g[u][i]);
+                s[i] += dz[u][i];
+                q[i] = fmaf(dz[u][i], raw[u][i] - ch.m[i], q[i]);
+            }
+            __builtin_amdgcn_sched_barrier(0);  // (row by row: all rows widened at a time are more than the registers hold)
+        }
+    }
+    float* const to = part + at.n * 2 * p.C + at.c0;
+    sums_by_channel(p, at, stats, me.live, s, q, red_f, [&](int which, int c, float sum) {
+        to[which * p.C + c] = sum;
+        by_channel[which * at.width + c] = sum * weight_at<T>(p, at.c0 + c);
+    });
+    __syncthreads();
+    group_terms(p, at, by_channel, ab);
+    if (!me.live || !dx) return;
+    // (x stays as it is: without this it would be kept widened, and there are no registers for that)
+#pragma unroll
+    for (int u = 0; u < R; u++)
+#pragma unroll
+        for (int i = 0; i < Raw<T>::kWords; i++) asm volatile("" : "+v"(raw[u].w[i]));
+    Terms terms;
+    terms.load(p, at, stats, me.c, ab);
+    T* const out = slab_of<T>(dx, ld_dx, p, at);
+#pragma unroll
+    for (int u = 0; u < R; u++) {
+        const int64_t r = me.ly + (int64_t)u * p.LY;
+        if (r >= p.S) break;
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; i++) v[i] = terms.dx(ch, i, raw[u][i], dz[u][i]);
+        store8(out + r * ld_dx + me.c, RAGGED ? at.width - me.c : 8, v);
+    }
 }
 
 // The sums of dz and of dz x^ of each part of a sample's rows and each channel: part[sample][chunk][2][C].
@@ -273,244 +527,300 @@ template <class T, bool RAGGED, int ACT>
 __global__ __launch_bounds__(1024) void k_group_norm_gradient_sums(Maps p, const float* __restrict__ stats, const T* __restrict__ dy,
                                                                    int64_t ld_dy, float* __restrict__ part) {
     extern __shared__ __attribute__((aligned(16))) float red_f[];
-    const int t = threadIdx.x, ly = t / p.LX, lx = t - ly * p.LX, c = 8 * lx;
-    const int64_t n = blockIdx.x / p.chunks, k = blockIdx.x - n * p.chunks;
-    const int64_t r0 = k * p.per, r1 = r0 + p.per < p.S ? r0 + p.per : p.S;
+    const Place at(p, p.chunks, 0);
+    const Lane me = lane_of(p, at);
+    const int64_t r0 = at.k * p.per, r1 = r0 + p.per < p.S ? r0 + p.per : p.S;
     float s[8] = {}, q[8] = {};
-    if (ly < p.LY) {
+    if (me.live) {
         Channels ch;
-        ch.load(p, stats, n, c);
-        const T *const x = static_cast<const T*>(p.x) + n * p.S * p.ld, *const g = dy + n * p.S * ld_dy;
+        ch.load<T, RAGGED>(p, at, stats, me.c);
+        const T *const x = slab_of<T>(p.x, p.ld, p, at), *const g = slab_of<T>(dy, ld_dy, p, at);
         constexpr int U = kUnroll / 2;
-        for (int64_t r = r0 + ly; r < r1; r += (int64_t)U * p.LY) {
+        for (int64_t r = r0 + me.ly; r < r1; r += (int64_t)U * p.LY) {
             Raw<T> raw[U], raw_g[U];
 #pragma unroll
             for (int u = 0; u < U; u++) {
-                const int64_t at = r + (int64_t)u * p.LY, from = at < r1 ? at : r;
-                raw[u].template load<RAGGED>(x + from * p.ld, c, p.C);
-                raw_g[u].template load<RAGGED>(g + from * ld_dy, c, p.C);
+                const int64_t row = r + (int64_t)u * p.LY, from = row < r1 ? row : r;
+                raw[u].template load<RAGGED>(x + from * p.ld, me.c, at.width);
+                raw_g[u].template load<RAGGED>(g + from * ld_dy, me.c, at.width);
             }
 #pragma unroll
             for (int u = 0; u < U; u++) {
                 if (r + (int64_t)u * p.LY >= r1) break;
-                if constexpr (RAGGED) raw[u].settle(c, p.C), raw_g[u].settle(c, p.C);
+                if constexpr (RAGGED) raw[u].settle(me.c, at.width), raw_g[u].settle(me.c, at.width);
 #pragma unroll
                 for (int i = 0; i < 8; i++) {
-                    float xh, dz;
-                    gradient<ACT>(ch, i, raw[u][i], raw_g[u][i], &xh, &dz);
+                    const float dz = ch.dz<ACT>(i, raw[u][i], raw_g[u][i]);
                     s[i] += dz;
-                    q[i] = fmaf(dz, xh, q[i]);
+                    q[i] = fmaf(dz, raw[u][i] - ch.m[i], q[i]);
                 }
             }
         }
-#pragma unroll
-        for (int i = 0; i < 8; i++) {
-            red_f[(ly * p.LX + lx) * 8 + i] = s[i];
-            red_f[((p.LY + ly) * p.LX + lx) * 8 + i] = q[i];
-        }
     }
-    __syncthreads();
-    const int64_t base = (n * p.chunks + k) * 2 * p.C;
-    for (int i = t; i < 2 * p.C; i += blockDim.x) {
-        const int which = i >= p.C, col = i - which * p.C;
-        float sum = 0.f;
-        for (int y = 0; y < p.LY; y++) sum += red_f[(which * p.LY + y) * 8 * p.LX + col];
-        part[base + i] = sum;
-    }
+    float* const to = part + (at.n * p.chunks + at.k) * 2 * p.C + at.c0;
+    sums_by_channel(p, at, stats, me.live, s, q, red_f, [&](int which, int c, float sum) { to[which * p.C + c] = sum; });
 }
 
-template <class T, bool RAGGED, int ACT>
-__global__ __launch_bounds__(1024) void k_group_norm_dx(Maps p, const float* __restrict__ stats, const float* __restrict__ part, int64_t parts,
-                                                        int64_t rows, const T* dy, int64_t ld_dy, T* dx, int64_t ld_dx) {
-    extern __shared__ __attribute__((aligned(16))) float red_f[];  // [2][C]: sums by channel, then [2][G]: A and B
-    const int t = threadIdx.x, ly = t / p.LX, lx = t - ly * p.LX, c = 8 * lx;
-    const int64_t n = blockIdx.x / parts, k = blockIdx.x - n * parts;
-    float* const ab = red_f + 2 * p.C;
-    for (int i = t; i < 2 * p.C; i += blockDim.x) {
-        float sum = 0.f;
-        for (int64_t j = 0; j < p.chunks; j++) sum += part[(n * p.chunks + j) * 2 * p.C + i];
-        const int col = i < p.C ? i : i - p.C;
-        float w = 1.f;
-        if (p.w) with_weights(p.weight_type, [&](auto ty) {
-            using W = typename decltype(ty)::type;
-            w = to_f32(static_cast<const W*>(p.w)[col]);
-        });
-        red_f[i] = w * sum;
-    }
-    __syncthreads();
-    const float rcount = 1.f / ((float)p.S * (float)p.D);
-    for (int i = t; i < 2 * p.G; i += blockDim.x) {
-        const int which = i >= p.G, g = i - which * p.G;
-        float sum = 0.f;
-        for (int j = 0; j < p.D; j++) sum += red_f[which * p.C + g * p.D + j];
-        ab[i] = sum * rcount;
-    }
-    __syncthreads();
-    if (ly >= p.LY) return;
-    Channels ch;
-    ch.load(p, stats, n, c);
-    float A[8], B[8];
-#pragma unroll
-    for (int i = 0; i < 8; i++) {
-        const int g = (c + i < p.C ? c + i : p.C - 1) / p.D;
-        A[i] = ab[g];
-        B[i] = ab[p.G + g];
-    }
-    const int64_t r0 = k * rows, r1 = r0 + rows < p.S ? r0 + rows : p.S;
-    const T *const x = static_cast<const T*>(p.x) + n * p.S * p.ld, *const g = dy + n * p.S * ld_dy;
-    T* const out = dx + n * p.S * ld_dx;
-    constexpr int U = kUnroll / 2;
-    for (int64_t r = r0 + ly; r < r1; r += (int64_t)U * p.LY) {
-        Raw<T> raw[U], raw_g[U];
-#pragma unroll
-        for (int u = 0; u < U; u++) {
-            const int64_t at = r + (int64_t)u * p.LY, from = at < r1 ? at : r;
-            raw[u].template load<RAGGED>(x + from * p.ld, c, p.C);
-            raw_g[u].template load<RAGGED>(g + from * ld_dy, c, p.C);
-        }
-#pragma unroll
-        for (int u = 0; u < U; u++) {
-            const int64_t at = r + (int64_t)u * p.LY;
-            if (at >= r1) break;
-            if constexpr (RAGGED) raw[u].settle(c, p.C), raw_g[u].settle(c, p.C);
-            float v[8];
-#pragma unroll
-            for (int i = 0; i < 8; i++) {
-                float xh, dz;
-                gradient<ACT>(ch, i, raw[u][i], raw_g[u][i], &xh, &dz);
-                v[i] = ch.r[i] * (fmaf(ch.w[i], dz, -A[i]) - xh * B[i]);
-            }
-            store8(out + at * ld_dx + c, RAGGED ? p.C - c : 8, v);
-        }
-    }
-}
-
-// dbias and dweight: sums over the parts, 32 columns a workgroup, 32 slices of the parts, added up in order
-__global__ __launch_bounds__(1024) void k_group_norm_params(const float* __restrict__ part, int64_t n, int C, float* __restrict__ dweight,
-                                                            float* __restrict__ dbias) {
-    __shared__ float slice[32][33];
-    const int col = threadIdx.x & 31, k = threadIdx.x >> 5, c = blockIdx.x * 32 + col;
+// dbias and dweight: sums over n rows of part, 32 columns a workgroup, slices of the rows, added up in order
+__device__ __forceinline__ void param_sums(const float* part, int64_t n, int C, float* dweight, float* dbias, float* slice) {
+    const int col = threadIdx.x & 31, k = threadIdx.x >> 5, slices = blockDim.x >> 5, c = blockIdx.x * 32 + col;
     float sum = 0.f;
     if (c < 2 * C)
 #pragma unroll 4
-        for (int64_t i = k; i < n; i += 32) sum += part[i * 2 * C + c];
-    slice[k][col] = sum;
+        for (int64_t i = k; i < n; i += slices) sum += part[i * 2 * C + c];
+    slice[k * 33 + col] = sum;
     __syncthreads();
     if (k == 0 && c < 2 * C) {
-#pragma unroll
-        for (int i = 1; i < 32; i++) sum += slice[i][col];
+        for (int i = 1; i < slices; i++) sum += slice[i * 33 + col];
         float* const to = c < C ? dbias : dweight;
         if (to) to[c < C ? c : c - C] = sum;
     }
 }
+__global__ __launch_bounds__(1024) void k_group_norm_params(const float* __restrict__ part, int64_t n, int C, float* __restrict__ dweight,
+                                                            float* __restrict__ dbias) {
+    __shared__ float slice[32 * 33];
+    param_sums(part, n, C, dweight, dbias, slice);
+}
 
+// dx from the sums of the parts.  The first `before` workgroups do the sums for dbias and dweight.
+template <class T, bool RAGGED, int ACT>
+__global__ __launch_bounds__(1024) void k_group_norm_dx(Maps p, const float* __restrict__ stats, const float* __restrict__ part, int64_t parts,
+                                                        int64_t rows, uint32_t before, const T* dy, int64_t ld_dy, T* dx, int64_t ld_dx,
+                                                        float* __restrict__ dweight, float* __restrict__ dbias) {
+    extern __shared__ __attribute__((aligned(16))) float red_f[];  // [slices][2][width] (or the other sums' slices), then [2][groups]: A and B
+    if (blockIdx.x < before) return param_sums(part, p.samples * p.chunks, p.C, dweight, dbias, red_f);
+    const Place at(p, parts, before);
+    const int wide = 2 * at.width, t = threadIdx.x, slices = (int)blockDim.x / wide < p.chunks ? (int)blockDim.x / wide : (int)p.chunks;
+    float* const ab = red_f + (slices > 1 ? slices : 1) * wide;
+    // sums over the chunks: neighbouring threads on neighbouring channels, several slices of the chunks where threads are left
+    for (int i = t; i < (slices > 1 ? slices : 1) * wide; i += blockDim.x) {
+        const int slice = i / wide, j = i - slice * wide, which = j >= at.width, c = at.c0 + j - which * at.width;
+        float sum = 0.f;
+#pragma unroll 4
+        for (int64_t k = slice; k < p.chunks; k += slices > 1 ? slices : 1) sum += part[(at.n * p.chunks + k) * 2 * p.C + which * p.C + c];
+        red_f[i] = sum * weight_at<T>(p, c);
+    }
+    __syncthreads();
+    if (slices > 1) {
+        for (int i = t; i < wide; i += blockDim.x)
+            for (int k = 1; k < slices; k++) red_f[i] += red_f[k * wide + i];
+        __syncthreads();
+    }
+    group_terms(p, at, red_f, ab);
+    const Lane me = lane_of(p, at);
+    if (!me.live) return;
+    Channels ch;
+    ch.load<T, RAGGED>(p, at, stats, me.c);
+    Terms terms;
+    terms.load(p, at, stats, me.c, ab);
+    const int64_t r0 = at.k * rows, r1 = r0 + rows < p.S ? r0 + rows : p.S;
+    const T *const x = slab_of<T>(p.x, p.ld, p, at), *const g = slab_of<T>(dy, ld_dy, p, at);
+    T* const out = slab_of<T>(dx, ld_dx, p, at);
+    constexpr int U = kUnroll / 2;
+    for (int64_t r = r0 + me.ly; r < r1; r += (int64_t)U * p.LY) {
+        Raw<T> raw[U], raw_g[U];
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            const int64_t row = r + (int64_t)u * p.LY, from = row < r1 ? row : r;
+            raw[u].template load<RAGGED>(x + from * p.ld, me.c, at.width);
+            raw_g[u].template load<RAGGED>(g + from * ld_dy, me.c, at.width);
+        }
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            const int64_t to = r + (int64_t)u * p.LY;
+            if (to >= r1) break;
+            if constexpr (RAGGED) raw[u].settle(me.c, at.width), raw_g[u].settle(me.c, at.width);
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; i++) v[i] = terms.dx(ch, i, raw[u][i], ch.dz<ACT>(i, raw[u][i], raw_g[u][i]));
+            store8(out + to * ld_dx + me.c, RAGGED ? at.width - me.c : 8, v);
+        }
+    }
+}
+
+// ---- which way ----
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-struct Shape { int threads, LX, LY; };
-Shape shape_of(int C) {
-    const int LX = (C + 7) / 8, threads = LX <= 64 ? 256 : LX <= 128 ? 512 : 1024;
-    return {threads, LX, threads / LX};
-}
-// parts of a sample's rows: `want` workgroups in all, some rows for every thread, and not more than `most`
-int64_t parts_of(int64_t samples, int64_t S, int LY, int64_t want, int64_t most) {
-    int64_t parts = ceil_div(want, samples), fit = ceil_div(S, (int64_t)kUnroll * LY);
-    parts = parts < fit ? parts : fit;
-    parts = parts < most ? parts : most;
-    return ceil_div(S, ceil_div(S, parts));
-}
-constexpr int64_t kWorkgroups = 2048;  // of 256 threads: what runs at a time
-constexpr int64_t kMostChunks = 256;
+struct Plan {
+    int threads, W, rows;     // rows: of a thread, in its registers (0: in two passes)
+    int64_t chunks;           // two passes: parts of a sample's rows
+};
+constexpr double kCus = 256;
 
-Maps maps_of(const fmtc_gnorm& a, const Shape& sh) {
-    Maps p{a.samples, a.rows_per_sample, a.ld_x, a.C, a.groups, a.C / a.groups, sh.LX, sh.LY, a.d_x, a.d_weight, a.d_bias, a.weight_type, 0, 0};
-    p.chunks = parts_of(p.samples, p.S, sh.LY, kWorkgroups * 256 / sh.threads, kMostChunks);
-    p.per = ceil_div(p.S, p.chunks);
-    return p;
+int lanes_of(int W) { return (W + 7) / 8; }
+// registers of a thread for a slab: its rows go up in these steps
+constexpr int kRowSteps16[] = {1, 2, 4, 8, 13}, kRowSteps32[] = {1, 2, 4, 6};
+int row_step(int64_t rows, int size) {
+    if (size == 2) {
+        for (int r : kRowSteps16) if (rows <= r) return r;
+    } else {
+        for (int r : kRowSteps32) if (rows <= r) return r;
+    }
+    return 0;
 }
-int64_t chunks_of(int64_t samples, int64_t S, int C) {
-    const Shape sh = shape_of(C);
-    return parts_of(samples, S, sh.LY, kWorkgroups * 256 / sh.threads, kMostChunks);
+
+// The least of the times that are expected, in us.  arrays: read (1 forward, 2 backward)
+Plan make_plan(int64_t samples, int64_t S, int C, int groups, int size, int arrays, bool may_be_once) {
+    const int D = C / groups;
+    const double values = (double)samples * S * C, bytes = values * size * (arrays + 1);
+    Plan best{};
+    // two passes: whole rows, cut in slabs where a few samples would need many chunks, whose sums are read again and again
+    int W = C;
+    auto threads_of = [](int W) { return W > 4096 ? 1024 : 512; };
+    auto want = [&](int W) { return ceil_div(512 * 1024 / threads_of(W), samples * ceil_div(C, W)); };
+    while (want(W) > 32 && W % 2 == 0 && (W / 2) % D == 0 && (W / 2) * size >= 128 && (W / 2) % 8 == 0) W /= 2;
+    best.threads = threads_of(W);
+    best.W = W;
+    const int64_t rows = ceil_div(S, (int64_t)(kUnroll / arrays) * (best.threads / lanes_of(W)));
+    best.chunks = want(W) < rows ? want(W) : rows;
+    best.chunks = ceil_div(S, ceil_div(S, best.chunks < 256 ? best.chunks : 256));
+    if (!may_be_once) return best;
+    double least = 8.0 + (bytes + values * size * arrays * (values * size * arrays > 2e8 ? 1.0 : 0.6)) / 5e6;
+    for (int gs = 1;; gs = gs * 2 < groups ? gs * 2 : groups) {
+        const int W = gs * D, LX = lanes_of(W);
+        for (int threads = 256; threads <= (arrays == 1 ? 1024 : 512); threads *= 2) {
+            if (LX > threads || (W < 8 && W != C) || (double)samples * ceil_div(groups, gs) > 2e9) continue;
+            const size_t lds = arrays == 1 ? sizeof(double) * (2 << fold_of(D)) * threads + sizeof(float) * 2 * gs : 0;
+            if (lds > 160 * 1024) continue;
+            const int R = row_step(ceil_div(S, threads / LX), size);
+            if (!R) continue;
+            const double wgs = (double)samples * ceil_div(groups, gs), at_once = kCus * 1024 / threads;
+            const double rounds = ceil(wgs / at_once), segment = W * size;
+            const double slow = (W == C || segment >= 128 ? 1.0 : segment >= 64 ? 1.05 : segment >= 32 ? 1.2 : 1.6) * (W % 8 && W != C ? 1.5 : 1.0);
+            const double mine = bytes / wgs * (wgs > kCus ? 1024.0 / threads : 1.0) * rounds / 30e3;  // one compute unit's part
+            const double t = 4.0 + 1.5 * rounds + fmax(bytes * slow / 5e6, mine);
+            if (t < least) {
+                least = t;
+                best.threads = threads;
+                best.W = W;
+                best.rows = R;
+            }
+        }
+        if (gs == groups) break;
+    }
+    return best;
+}
+
+Maps maps_of(const fmtc_gnorm& a, const Plan& plan) {
+    const int LX = lanes_of(plan.W), D = a.C / a.groups;
+    return {a.samples, a.rows_per_sample, a.ld_x, a.C, a.groups, D, plan.W, plan.W / D, (int)ceil_div(a.C, plan.W), LX, plan.threads / LX, fold_of(D),
+            a.d_x, a.d_weight, a.d_bias, a.weight_type, plan.chunks, plan.chunks ? ceil_div(a.rows_per_sample, plan.chunks) : 0};
+}
+// parts of a sample's rows for the second pass: some rows for every thread, about `want` workgroups in all
+int64_t parts_of(const Maps& p, int rows_at_a_time, int unroll, int64_t want) {
+    const int64_t fit = ceil_div(p.S, (int64_t)unroll * rows_at_a_time), parts = ceil_div(want, p.samples * p.slabs);
+    return ceil_div(p.S, ceil_div(p.S, parts < fit ? parts : fit));
 }
 template <class F>
 hipError_t with_act(int act, F&& f) {
     return act == FMTC_ACT_NONE ? f(Int<FMTC_ACT_NONE>{}) : act == FMTC_ACT_RELU ? f(Int<FMTC_ACT_RELU>{}) : f(Int<FMTC_ACT_SILU>{});
 }
-template <class K>
-hipError_t allow_lds(K kernel, size_t bytes) {
-    return bytes <= 65536 ? hipSuccess : hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+template <class T, class F>
+hipError_t with_rows(int rows, F&& f) {
+    if (rows == 1) return f(Int<1>{});
+    if (rows == 2) return f(Int<2>{});
+    if (rows == 4) return f(Int<4>{});
+    if constexpr (sizeof(T) == 2) return rows == 8 ? f(Int<8>{}) : f(Int<13>{});
+    else return f(Int<6>{});
 }
+template <class... A, class... B>
+hipError_t go(int id, void (*kernel)(A...), int64_t grid, int threads, size_t lds, hipStream_t s, B... args) {
+    if (lds > 65536) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        if (e != hipSuccess) return e;
+    }
+    return launch(id, kernel, dim3((unsigned)grid), dim3(threads), lds, s, args...);
+}
+int type_size(int type) { return type == FMTC_F32 ? 4 : 2; }
 
 }  // namespace
 
-size_t group_norm_workspace(int64_t samples, int64_t S, int C, int groups) {
-    return align_up(sizeof(double2) * (size_t)(samples * chunks_of(samples, S, C)) * groups, 256);
+size_t group_norm_workspace(int64_t samples, int64_t S, int C, int groups, int type, bool to_codes) {
+    const Plan plan = make_plan(samples, S, C, groups, type_size(type), 1, !to_codes);
+    return plan.rows ? 0 : align_up(sizeof(double2) * (size_t)(samples * plan.chunks) * groups, 256);
 }
-size_t group_norm_backward_workspace(int64_t samples, int64_t S, int C, int) {
-    return align_up(sizeof(float) * (size_t)(samples * chunks_of(samples, S, C)) * 2 * C, 256);
+size_t group_norm_backward_workspace(int64_t samples, int64_t S, int C, int groups) {
+    size_t most = 0;
+    for (int size = 2; size <= 4; size += 2) {  // (in one pass there is one part of a sample, no more)
+        const size_t bytes = sizeof(float) * (size_t)(samples * make_plan(samples, S, C, groups, size, 2, false).chunks) * 2 * C;
+        most = bytes > most ? bytes : most;
+    }
+    return align_up(most, 256);
 }
 
 hipError_t launch_group_norm(const fmtc_gnorm& a, void* d_y, int64_t ld_y, const fmtc_i8* codes, float* d_stats, void* d_ws, hipStream_t s) {
-    const Shape sh = shape_of(a.C);
-    const Maps p = maps_of(a, sh);
+    const Plan plan = make_plan(a.samples, a.rows_per_sample, a.C, a.groups, type_size(a.type), 1, !codes);
+    Maps p = maps_of(a, plan);
     double2* const part = static_cast<double2*>(d_ws);
     return with_type(a.type, [&](auto ty) {
         using T = typename decltype(ty)::type;
-        return with_bit(a.C % 8 != 0, [&](auto rg) {
+        return with_bit(p.C % 8 != 0 || p.W % 8 != 0, [&](auto rg) {
             constexpr bool R = decltype(rg)::value;
-            auto sums = k_group_norm_sums<T, R>;
-            const size_t lds = sizeof(double) * 8 * sh.LX * sh.LY;
-            hipError_t e = allow_lds(sums, lds);
-            if (e == hipSuccess) e = launch(K_GROUP_NORM, sums, dim3((unsigned)(p.samples * p.chunks)), dim3(sh.threads), lds, s, p, part);
+            const size_t lds = sizeof(double) * (2 << p.pre) * plan.threads, lds_stats = sizeof(float) * 2 * p.groups;
+            if (plan.rows)
+                return with_rows<T>(plan.rows, [&](auto rows) {
+                    return go(K_GROUP_NORM, k_group_norm_once<T, R, decltype(rows)::value>, p.samples * p.slabs, plan.threads, lds + lds_stats, s,
+                              p, a.eps, a.act, static_cast<T*>(d_y), ld_y, d_stats);
+                });
+            const hipError_t e = go(K_GROUP_NORM, k_group_norm_sums<T, R>, p.samples * p.slabs * p.chunks, plan.threads, lds, s, p, part);
             if (e != hipSuccess) return e;
-            const size_t lds_stats = sizeof(float) * 2 * p.G;
             if (codes) {
-                auto go = [&](auto tpr) {
-                    constexpr int TPR = decltype(tpr)::value, kRows = codes_threads(TPR) / TPR;
-                    const int64_t parts = parts_of(p.samples, p.S, kRows, kWorkgroups, p.S), rows = ceil_div(p.S, parts);
-                    auto kernel = k_group_norm_codes<T, R, TPR>;
-                    const hipError_t e = allow_lds(kernel, lds_stats);
-                    return e != hipSuccess ? e : launch(K_GROUP_NORM, kernel, dim3((unsigned)(p.samples * parts)), dim3(codes_threads(TPR)), lds_stats, s, p,
-                                                        (const double2*)part, parts, rows, a.eps, a.act, *codes, static_cast<T*>(d_y), ld_y, d_stats);
+                p.W = p.C;  // (rows as a whole)
+                p.groups = p.G;
+                p.slabs = 1;
+                auto with = [&](auto tpr, auto vpt) {
+                    constexpr int TPR = decltype(tpr)::value, VPT = decltype(vpt)::value;
+                    const int64_t parts = parts_of(p, codes_threads(TPR) / TPR, 1, 2048), rows = ceil_div(p.S, parts);
+                    return go(K_GROUP_NORM, k_group_norm_codes<T, R, TPR, VPT>, p.samples * parts, codes_threads(TPR), sizeof(float) * 2 * p.G, s,
+                              p, part, parts, rows, a.eps, a.act, *codes, static_cast<T*>(d_y), ld_y, d_stats);
                 };
-                return p.C <= 128 ? go(Int<16>{}) : p.C <= 512 ? go(Int<64>{}) : p.C <= 2048 ? go(Int<256>{}) : go(Int<1024>{});
+                if (p.C <= 128) return with(Int<16>{}, Int<1>{});
+                if (p.C <= 512) return with(Int<64>{}, Int<1>{});
+                if (p.C <= 1024) return with(Int<64>{}, Int<2>{});
+                if (p.C <= 2048) return with(Int<256>{}, Int<1>{});
+                return with(Int<1024>{}, Int<1>{});
             }
-            const int64_t parts = d_y ? parts_of(p.samples, p.S, sh.LY, kWorkgroups * 256 / sh.threads, p.S) : 1, rows = ceil_div(p.S, parts);
-            return with_act(a.act, [&](auto ac) {
-                auto kernel = k_group_norm_apply<T, R, decltype(ac)::value>;
-                const hipError_t e = allow_lds(kernel, lds_stats);
-                return e != hipSuccess ? e : launch(K_GROUP_NORM, kernel, dim3((unsigned)(p.samples * parts)), dim3(sh.threads), lds_stats, s, p, (const double2*)part,
-                                                    parts, rows, a.eps, static_cast<T*>(d_y), ld_y, d_stats);
-            });
+            const int64_t parts = d_y ? parts_of(p, p.LY, kUnroll, 1024 * 512 / plan.threads) : 1, rows = ceil_div(p.S, parts);
+            return go(K_GROUP_NORM, k_group_norm_apply<T, R>, p.samples * p.slabs * parts, plan.threads, lds_stats, s, p, part, parts, rows, a.eps,
+                      a.act, static_cast<T*>(d_y), ld_y, d_stats);
         });
     });
 }
 
 hipError_t launch_group_norm_backward(const fmtc_gnorm& a, const float* d_stats, const void* d_dy, int64_t ld_dy, void* d_dx, int64_t ld_dx,
                                       float* d_dweight, float* d_dbias, void* d_ws, hipStream_t s) {
-    const Shape sh = shape_of(a.C);
-    const Maps p = maps_of(a, sh);
+    const Plan plan = make_plan(a.samples, a.rows_per_sample, a.C, a.groups, type_size(a.type), 2, true);
+    const Maps p = maps_of(a, plan);
     float* const part = static_cast<float*>(d_ws);
     return with_type(a.type, [&](auto ty) {
         using T = typename decltype(ty)::type;
-        return with_bit(a.C % 8 != 0, [&](auto rg) {
+        return with_bit(p.C % 8 != 0 || p.W % 8 != 0, [&](auto rg) {
             return with_act(a.act, [&](auto ac) {
                 constexpr bool R = decltype(rg)::value;
                 constexpr int A = decltype(ac)::value;
                 const T* dy = static_cast<const T*>(d_dy);
-                auto sums = k_group_norm_gradient_sums<T, R, A>;
-                const size_t lds = sizeof(float) * 16 * sh.LX * sh.LY, lds_dx = sizeof(float) * 2 * (p.C + p.G);
-                hipError_t e = allow_lds(sums, lds);
-                if (e == hipSuccess)
-                    e = launch(K_GROUP_NORM_BACKWARD, sums, dim3((unsigned)(p.samples * p.chunks)), dim3(sh.threads), lds, s, p, d_stats, dy, ld_dy, part);
-                if (e == hipSuccess && (d_dweight || d_dbias))
-                    e = launch(K_GROUP_NORM_BACKWARD, k_group_norm_params, dim3((unsigned)ceil_div(2 * p.C, 32)), dim3(1024), 0, s, (const float*)part,
-                               p.samples * p.chunks, p.C, d_dweight, d_dbias);
-                if (e != hipSuccess || !d_dx) return e;
-                const int64_t parts = parts_of(p.samples, p.S, sh.LY, kWorkgroups * 256 / sh.threads, p.S), rows = ceil_div(p.S, parts);
-                auto kernel = k_group_norm_dx<T, R, A>;
-                e = allow_lds(kernel, lds_dx);
-                return e != hipSuccess ? e : launch(K_GROUP_NORM_BACKWARD, kernel, dim3((unsigned)(p.samples * parts)), dim3(sh.threads), lds_dx, s, p, d_stats,
-                                                    (const float*)part, parts, rows, dy, ld_dy, static_cast<T*>(d_dx), ld_dx);
+                const bool params = d_dweight || d_dbias;
+                const int64_t param_groups = params ? ceil_div(2 * p.C, 32) : 0;
+                const size_t lds = sizeof(float) * 16 * plan.threads, lds_ab = sizeof(float) * 2 * p.groups;
+                auto sum_params = [&](int64_t n) {
+                    return params ? go(K_GROUP_NORM_BACKWARD, k_group_norm_params, param_groups, 1024, 0, s, part, n, p.C, d_dweight, d_dbias) : hipSuccess;
+                };
+                if (plan.rows) {
+                    const hipError_t e = with_rows<T>(plan.rows, [&](auto rows) {
+                        return go(K_GROUP_NORM_BACKWARD, k_group_norm_backward_once<T, R, A, decltype(rows)::value>, p.samples * p.slabs, plan.threads,
+                                  lds + sizeof(float) * 2 * p.W + lds_ab, s, p, d_stats, dy, ld_dy, static_cast<T*>(d_dx), ld_dx, part);
+                    });
+                    return e != hipSuccess ? e : sum_params(p.samples);
+                }
+                const hipError_t e = go(K_GROUP_NORM_BACKWARD, k_group_norm_gradient_sums<T, R, A>, p.samples * p.slabs * p.chunks, plan.threads, lds, s, p,
+                                        d_stats, dy, ld_dy, part);
+                if (e != hipSuccess) return e;
+                if (!d_dx) return sum_params(p.samples * p.chunks);
+                const int64_t parts = parts_of(p, p.LY, kUnroll / 2, 1024 * 512 / plan.threads), rows = ceil_div(p.S, parts);
+                size_t lds_dx = sizeof(float) * (2 * p.W > plan.threads ? 2 * p.W : plan.threads) + lds_ab;
+                if (lds_dx < sizeof(float) * 33 * (plan.threads / 32)) lds_dx = sizeof(float) * 33 * (plan.threads / 32);
+                return go(K_GROUP_NORM_BACKWARD, k_group_norm_dx<T, R, A>, param_groups + p.samples * p.slabs * parts, plan.threads, lds_dx, s, p, d_stats, part,
+                          parts, rows, (uint32_t)param_groups, dy, ld_dy, static_cast<T*>(d_dx), ld_dx, d_dweight, d_dbias);
             });
         });
     });
