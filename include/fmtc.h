@@ -450,7 +450,7 @@ fmtc_status fmtc_i8_matmul(const fmtc_i8 *a, const fmtc_i8 *b, const float *d_bi
 
 /* A layer: d_x [rows][w->depth] quantized by rows, times w: the same numbers as
  * fmtc_i8_quantize and fmtc_i8_matmul.  Workspace: 256-byte aligned,
- * fmtc_i8_linear_workspace_size(rows, w->rows, w->depth) bytes. */
+ * fmtc_i8_linear_workspace_size(rows, w->rows, w->depth) bytes (may be 0: then NULL is fine). */
 size_t fmtc_i8_linear_workspace_size(int64_t rows, int64_t N, int64_t K);
 fmtc_status fmtc_i8_linear(const void *d_x, fmtc_dtype type, int64_t rows, int64_t ld_x, const fmtc_i8 *w,
                            const float *d_bias, void *d_out, fmtc_dtype out_type, int64_t ld_out, void *d_workspace,

@@ -39,6 +39,10 @@ hipError_t launch_i8_quantize(const void* d_x, int type, int64_t rows, int64_t c
 size_t matmul_i8_workspace(int64_t M, int64_t N, int64_t K);
 hipError_t launch_i8_matmul(const fmtc_i8& a, const fmtc_i8& b, const float* d_bias, void* d_out, int out_type, int64_t ld_out,
                             void* d_ws, hipStream_t s);
+// quantizer and product of very few rows in one launch, without a workspace
+bool i8_linear_is_one(int64_t M, int64_t K);
+hipError_t launch_i8_linear_one(const void* d_x, int type, int64_t rows, int64_t ld_x, const fmtc_i8& w, const float* d_bias, void* d_out,
+                                int out_type, int64_t ld_out, hipStream_t s);
 
 size_t group_norm_workspace(int64_t samples, int64_t rows, int C, int groups, int type, bool to_codes);
 hipError_t launch_group_norm(const fmtc_gnorm& a, void* d_y, int64_t ld_y, const fmtc_i8* codes, float* d_stats, void* d_ws,

@@ -310,6 +310,7 @@ fmtc_status check_i8_product(const char* who, int64_t M, int64_t N, const float*
 // Workspace of fmtc_i8_linear: x as codes, its scales, and what the product needs
 struct LinearSpace { size_t codes, scales, product, product_bytes, total; };
 LinearSpace linear_space(int64_t M, int64_t N, int64_t K) {
+    if (i8_linear_is_one(M, K)) return {0, 0, 0, 0, 0};
     LinearSpace w;
     w.codes = 0;
     w.scales = align_up((size_t)M * blocks_of(K) * kF8Block, 256);
@@ -389,6 +390,7 @@ fmtc_status fmtc_i8_linear(const void* d_x, fmtc_dtype type, int64_t rows, int64
     if (rows == 0 || w->rows == 0) return FMTC_OK;
     const LinearSpace at = linear_space(rows, w->rows, w->depth);
     CHECK(check_workspace(who, d_workspace, ws_bytes, at.total));
+    if (i8_linear_is_one(rows, w->depth)) return hip_status(launch_i8_linear_one(d_x, type, rows, ld_x, *w, d_bias, d_out, out_type, ld_out, s), who);
     char* ws = static_cast<char*>(d_workspace);
     const fmtc_i8 x{ws + at.codes, reinterpret_cast<float*>(ws + at.scales), rows, w->depth, blocks_of(w->depth) * kF8Block};
     hipError_t e = launch_i8_quantize(d_x, type, rows, w->depth, ld_x, x, s);

@@ -3,6 +3,8 @@
 // The sum is exact in 32 bits, whatever its order, so that the depth can be taken by several wavefronts or workgroups
 // without a result depending on it.  b's rows are the matrix instruction's first operand and a's its second: a lane then
 // holds four consecutive columns n of one row m of the result, and the results leave in vectors.
+#include <type_traits>
+
 #include "fmtc_block.h"
 #include "fmtc_device.h"
 
@@ -91,38 +93,45 @@ struct Product {
     int* part;
 };
 
-// n .. n + 3 of a vector of N, `without` where there is none (columns past the last: the last one's, not stored)
-__device__ __forceinline__ v4f load_four(const float* p, int64_t n, int64_t N, float without) {
-    v4f v = {without, without, without, without};
+// n .. n + 3 of a vector of N, 0 where there is none (columns past the last: the last one's, not stored)
+__device__ __forceinline__ v4f load_four(const float* p, int64_t n, int64_t N) {
+    v4f v = {};
     if (p)
 #pragma unroll
         for (int i = 0; i < 4; i++) v[i] = p[n + i < N ? n + i : N - 1];
     return v;
 }
 
-// out[m][n .. n + 3].  The factors one after the other: their product alone could leave f32's range.
-__device__ __forceinline__ void store_out(const Product& p, int64_t m, int64_t n, v4i sum, float sa, v4f sb, v4f bias) {
-    const int64_t at = m * p.ld_out + n;
-    const int k = p.N - n < 4 ? (int)(p.N - n) : 4;
+// The factors one after the other: their product alone could leave f32's range.
+__device__ __forceinline__ v4f scaled(v4i sum, float sa, v4f sb, v4f bias) {
     v4f v;
 #pragma unroll
-    for (int i = 0; i < 4; i++) v[i] = (float)sum[i] * sa * sb[i];
-    if (p.bias) v += bias;
-    if (p.out_type == FMTC_F32) {
-        float* to = static_cast<float*>(p.out) + at;
-        if (k == 4) __builtin_memcpy(to, &v, 16);
-        else
-            for (int i = 0; i < k; i++) to[i] = v[i];
-    } else {
-        uint16_t r[4];
+    for (int i = 0; i < 4; i++) v[i] = (float)sum[i] * sa * sb[i] + bias[i];
+    return v;
+}
+// k of four consecutive results
+template <class O>
+__device__ __forceinline__ void store_four(O* to, v4f v, int64_t k) {
+    O r[4];
+#pragma unroll
+    for (int i = 0; i < 4; i++) r[i] = from_f32<O>(v[i]);
+    if (k >= 4) __builtin_memcpy(to, r, sizeof r);
+    else
 #pragma unroll
         for (int i = 0; i < 4; i++)
-            r[i] = p.out_type == FMTC_BF16 ? from_f32<bf16>(v[i]).bits : __builtin_bit_cast(uint16_t, from_f32<_Float16>(v[i]));
-        uint16_t* to = static_cast<uint16_t*>(p.out) + at;
-        if (k == 4) __builtin_memcpy(to, r, 8);
-        else
-            for (int i = 0; i < k; i++) to[i] = r[i];
-    }
+            if (i < k) to[i] = r[i];
+}
+// f(the outputs as what they are)
+template <class F>
+__device__ __forceinline__ void with_out(const Product& p, F&& f) {
+    if (p.out_type == FMTC_BF16) f(static_cast<bf16*>(p.out));
+    else if (p.out_type == FMTC_F16) f(static_cast<_Float16*>(p.out));
+    else f(static_cast<float*>(p.out));
+}
+// out[m][n .. n + 3]
+__device__ __forceinline__ void store_out(const Product& p, int64_t m, int64_t n, v4i sum) {
+    const v4f v = scaled(sum, p.sa[m], load_four(p.sb, n, p.N), load_four(p.bias, n, p.N));
+    with_out(p, [&](auto* out) { store_four(out + m * p.ld_out + n, v, p.N - n); });
 }
 
 // 128 bytes of a row for 16 x 16 results: lanes 16 g .. 16 g + 15 hold the bytes 16 g .. and 64 + 16 g .. (the same order of
@@ -178,8 +187,90 @@ __global__ __launch_bounds__(64 * kRowsWaves) void k_i8_matmul_rows(Product p, u
 #pragma unroll
         for (int w = 1; w < kRowsWaves; w++) v += sums[w][k][lane];
         const int64_t m = (mt * MT + k / NT) * 16 + i16, n4 = (nt * NT + k % NT) * 16 + g * 4;
-        if (m < p.M && n4 < p.N) store_out(p, m, n4, v, p.sa[m], load_four(p.sb, n4, p.N, 0.f), load_four(p.bias, n4, p.N, 0.f));
+        if (m < p.M && n4 < p.N) store_out(p, m, n4, v);
     }
+}
+
+// A layer of very few rows in one launch: every workgroup quantizes the rows itself, into LDS, while its first weights are on
+// their way.  TPR lanes (whole wavefronts) take a row, up to 4 groups of 8 values each.
+constexpr int kLinearRows = 8, kLinearGroups = 4, kLinearThreads = 64 * kRowsWaves;
+constexpr int kLinearCodes = 8 * kLinearGroups * kLinearThreads;  // bytes of codes: of all rows together
+bool linear_fits(int64_t M, int64_t K) {
+    int64_t lanes = kLinearThreads;
+    for (int64_t rows = 1; rows < M; rows *= 2) lanes /= 2;
+    return M <= kLinearRows && (K + kBlock - 1) / kBlock * kBlock <= 8 * kLinearGroups * lanes;
+}
+template <class T, bool RAGGED>
+__global__ __launch_bounds__(kLinearThreads) void k_i8_linear_rows(Product p, const T* __restrict__ x, int64_t K, int64_t ld_x, int tpr) {
+    __shared__ v4i sums[kRowsWaves][64];
+    __shared__ uint32_t part[kRowsWaves];
+    __shared__ float scales[kLinearRows];
+    __shared__ __attribute__((aligned(16))) uint8_t codes[kLinearCodes + 16 * kLinearRows];  // (rows apart by 16 bytes more: other banks)
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6, g = lane >> 4, i16 = lane & 15;
+    const int row = t / tpr, at = t - row * tpr, M = (int)p.M, width = (int)p.blocks * kBlock, pitch = width + 16;
+    const int64_t n0 = (int64_t)blockIdx.x * 16, n = n0 + i16;
+    const T* const from = x + (row < M ? row : M - 1) * ld_x;
+    Raw<T> raw[kLinearGroups];
+#pragma unroll
+    for (int j = 0; j < kLinearGroups; j++) raw[j].template load<RAGGED>(from, 8 * (j * tpr + at), K);
+    // the weights' blocks wave, wave + 8, ..: the first four now (past the last: that one again, not used)
+    const uint8_t* const b_row = p.b + (n < p.N ? n : p.N - 1) * p.ld_b;
+    const int blocks = (int)p.blocks;
+    constexpr int kAhead = 4;
+    Operand b[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; i++) {
+        const int kb = wave + i * kRowsWaves;
+        b[i] = load_operand(b_row + (int64_t)(kb < blocks ? kb : blocks - 1) * kBlock, g);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    uint32_t m = 0;
+    float v[kLinearGroups][8];
+#pragma unroll
+    for (int j = 0; j < kLinearGroups; j++) {
+        const int c = 8 * (j * tpr + at);
+        if constexpr (RAGGED) raw[j].settle(c, K);
+        raw[j].zero_unless(c < K);
+#pragma unroll
+        for (int i = 0; i < 8; i++) v[j][i] = raw[j][i];
+        const uint32_t bits = amax_bits8(v[j]);
+        m = bits > m ? bits : m;
+    }
+    m = row_max_bits<64>(m, part);
+    if (lane == 0) part[wave] = m;
+    __syncthreads();
+    for (int w = row * (tpr / 64); w < (row + 1) * (tpr / 64); w++) m = part[w] > m ? part[w] : m;
+    float held;
+    const float inv = i8_row_scale(m, &held);
+    if (row < M) {
+        if (at == 0) scales[row] = held;
+#pragma unroll
+        for (int j = 0; j < kLinearGroups; j++) {
+            const int c = 8 * (j * tpr + at);
+            if (c < width) *reinterpret_cast<uint2*>(codes + row * pitch + c) = make_uint2(i8_encode4(v[j], inv), i8_encode4(v[j] + 4, inv));
+        }
+    }
+    __syncthreads();
+    const uint8_t* const a_row = codes + (i16 < M ? i16 : M - 1) * pitch;  // (rows that do not exist: the last one, never stored)
+    v4i acc = {};
+    for (int kb = wave; kb < blocks; kb += kAhead * kRowsWaves) {
+#pragma unroll
+        for (int i = 0; i < kAhead; i++) {
+            const int k = kb + i * kRowsWaves;
+            if (k < blocks) acc = mfma_block(b[i], load_operand(a_row + k * kBlock, g), acc);
+            const int next = k + kAhead * kRowsWaves;
+            b[i] = load_operand(b_row + (int64_t)(next < blocks ? next : blocks - 1) * kBlock, g);
+        }
+    }
+    sums[wave][lane] = acc;
+    __syncthreads();
+    if (wave != 0 || i16 >= M) return;
+#pragma unroll
+    for (int w = 1; w < kRowsWaves; w++) acc += sums[w][lane];
+    const int64_t n4 = n0 + g * 4;
+    if (n4 >= p.N) return;
+    const v4f out = scaled(acc, scales[i16], load_four(p.sb, n4, p.N), load_four(p.bias, n4, p.N));
+    with_out(p, [&](auto* to) { store_four(to + i16 * p.ld_out + n4, out, p.N - n4); });
 }
 
 // Many rows: a tile of BM x BN results per workgroup, operands through LDS, one block of the depth (128 bytes of a row) a
@@ -189,18 +280,17 @@ __global__ __launch_bounds__(64 * kRowsWaves) void k_i8_matmul_rows(Product p, u
 // read and those of the step after it set out into the place that came free, all under the last tiles' products.
 //
 // Rows of 128 bytes in LDS, the 16-byte pieces of a row exchanged by a key of the row, so that 16 lanes that read the same
-// piece of 16 rows touch every bank once.  The results leave through LDS too, 64 columns of a row at a time.
+// piece of 16 rows touch every bank once.
 template <int WM_, int WN_, int MT_, int NT_, int STAGES_>
 struct Tile {
     static constexpr int WM = WM_, WN = WN_, MT = MT_, NT = NT_, kStages = STAGES_;
     static constexpr int kThreads = 64 * WM * WN, BM = WM * MT * 16, BN = WN * NT * 16;
     static constexpr int kStage = (BM + BN) * kBlock;
     static constexpr int kLoads = (BM + BN) / 8 / (WM * WN);  // loads of 8 rows a wavefront, a's and b's in one range
-    static constexpr int kPitch = 68, kOutRows = 64;          // results in LDS: a wavefront's 64 rows x 64 columns at a time
-    static constexpr int kLoop = kStages * kStage, kOut = WM * WN * kOutRows * kPitch * 4;
-    static constexpr int kLds = kLoop > kOut ? kLoop : kOut;
-    static_assert((BM + BN) % (8 * WM * WN) == 0 && kLoads % 4 == 0 && BM % 64 == 0 && MT % 4 == 0 && NT % 4 == 0);
+    static constexpr int kLds = kStages * kStage + 4 * (BM + 2 * BN);  // the operands, the scales and the bias
+    static_assert((BM + BN) % (8 * WM * WN) == 0 && kLoads % 2 == 0 && BM % 64 == 0 && MT % 4 == 0 && NT % 4 == 0);
     static_assert((kStages & (kStages - 1)) == 0 && kStages >= 2);
+    static_assert(WM * WN * MT * 16 * 128 <= kStages * kStage);  // results on their way out
 };
 __device__ __forceinline__ int row_key(int row) { return (row >> 1) & 7; }
 
@@ -212,7 +302,7 @@ __device__ __forceinline__ void load16_to_lds(const void* base, uint32_t off, ui
 }
 
 template <class S>
-__global__ __launch_bounds__(S::kThreads, S::kThreads == 256 && S::NT == 8 ? 1 : 2) void k_i8_matmul_tiles(Product p, uint32_t tiles_m, uint32_t tiles_n) {
+__global__ __launch_bounds__(S::kThreads, 2) void k_i8_matmul_tiles(Product p, uint32_t tiles_m, uint32_t tiles_n) {
     extern __shared__ __attribute__((aligned(128))) uint8_t lds[];
     constexpr int MT = S::MT, NT = S::NT, kStages = S::kStages;
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), g = lane >> 4, i16 = lane & 15;
@@ -256,6 +346,17 @@ __global__ __launch_bounds__(S::kThreads, S::kThreads == 256 && S::NT == 8 ? 1 :
         return Operand{*reinterpret_cast<const v4i*>(at + 16 * (g ^ key)), *reinterpret_cast<const v4i*>(at + 16 * ((4 + g) ^ key))};
     };
 
+    // scales and bias in LDS for the end (those past the last: the last one's, not stored)
+    float* const vectors = reinterpret_cast<float*>(lds + kStages * S::kStage);
+    if (!p.part) {
+        for (int i = t; i < S::BM; i += S::kThreads) vectors[i] = p.sa[m0 + (i < rows_a ? i : rows_a - 1)];
+        for (int i = t; i < S::BN; i += S::kThreads) {
+            const int64_t n = n0 + (i < rows_b ? i : rows_b - 1);
+            vectors[S::BM + i] = p.sb[n];
+            vectors[S::BM + S::BN + i] = p.bias ? p.bias[n] : 0.f;
+        }
+    }
+
     v4i acc[MT][NT] = {};
     // all blocks' loads that fit, and the first half of those of the last place's; the rest of them in the first step
 #pragma unroll
@@ -291,39 +392,66 @@ __global__ __launch_bounds__(S::kThreads, S::kThreads == 256 && S::NT == 8 ? 1 :
             __builtin_amdgcn_sched_barrier(0);
         }
     }
-    // 4 tiles of a at a time: 64 rows of 64 columns in the wavefront's own part of LDS, then whole rows to memory
+    // The results leave through LDS, 128 bytes of each of a wavefront's rows at a time, as what they are in memory: then 8 lanes
+    // write a line.  (4096^2 results of 2 bytes: 8.6 us, a fill of such an array 7.2; 8 bytes a lane from sums in LDS 13; straight from
+    // the registers, 32 bytes of a row at a time, 24.)
     wait_loads<0>();
     __syncthreads();
-    int* const out = reinterpret_cast<int*>(lds) + wave * S::kOutRows * S::kPitch;
+    uint8_t* const mine = lds + wave * MT * 16 * 128;
+    const float *const sa = vectors + wm * MT * 16 + i16, *const sb = vectors + S::BM + wn * NT * 16 + 4 * g, *const bias = sb + S::BN;
+    auto leave = [&](auto* out, int64_t ld, auto&& value) {
+        using O = typename std::remove_pointer<decltype(out)>::type;
+        constexpr int kCols = 128 / sizeof(O), kTiles = kCols / 16, kPiece = 16 / sizeof(O);
+        O* const to = out + (m0 + wm * MT * 16 + (lane >> 3)) * ld + n0 + wn * NT * 16 + (lane & 7) * kPiece;
+        const int row = wm * MT * 16 + (lane >> 3), col = wn * NT * 16 + (lane & 7) * kPiece;
 #pragma unroll
-    for (int j0 = 0; j0 < NT; j0 += 4) {
-        const int64_t n = n0 + wn * NT * 16 + 16 * j0 + 4 * i16;
-        v4f bias = load_four(p.bias, n, p.N, 0.f), sb = load_four(p.sb, n, p.N, 0.f);
-        asm volatile("" : "+v"(bias), "+v"(sb));  // (waited for here: in the loop a wait for them is one for the stores, too)
+        for (int j0 = 0; j0 < NT; j0 += kTiles) {
 #pragma unroll
-        for (int i0 = 0; i0 < MT; i0 += 4) {
-            const int64_t m1 = m0 + wm * MT * 16 + i0 * 16;
+            for (int j = 0; j < kTiles; j++)
 #pragma unroll
-            for (int i = 0; i < 4; i++)
+                for (int i = 0; i < MT; i++) {
+                    O r[4];
+                    value(i, j0 + j, r);
+                    const int at = (16 * j + 4 * g) * (int)sizeof(O);
+                    __builtin_memcpy(mine + (16 * i + i16) * 128 + ((at / 16 ^ key) * 16 | at % 16), r, sizeof r);
+                }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            const int left = rows_b - col - j0 * 16;
 #pragma unroll
-                for (int j = 0; j < 4; j++) *reinterpret_cast<v4i*>(out + (16 * i + i16) * S::kPitch + 16 * j + 4 * g) = acc[i0 + i][j0 + j];
-            float sa = 0.f;  // lane l: the scale of row l of these 64
-            if (!p.part) sa = p.sa[m1 + lane < p.M ? m1 + lane : p.M - 1];
-            asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(sa) : : "memory");
-#pragma unroll 4
-            for (int r0 = 0; r0 < 64; r0 += 4) {
-                const int r = r0 + g;
-                const int64_t m = m1 + r;
-                const v4i v = *reinterpret_cast<const v4i*>(out + r * S::kPitch + 4 * i16);
-                const float mine = __shfl(sa, r, 64);
-                if (m < p.M && n < p.N) {
-                    if (p.part) *reinterpret_cast<v4i*>(p.part + z * p.split_out + m * p.ld_part + n) = v;
-                    else store_out(p, m, n, v, mine, sb, bias);
+            for (int r = 0; r < MT * 16; r += 8) {
+                const int at = r + (lane >> 3);
+                const v4i v = *reinterpret_cast<const v4i*>(mine + at * 128 + 16 * ((lane & 7) ^ row_key(at)));
+                if (row + r < rows_a) {
+                    O* const here = to + r * ld + j0 * 16;
+                    if (left >= kPiece) {
+                        __builtin_memcpy(here, &v, 16);
+                    } else {
+                        O one[kPiece];
+                        __builtin_memcpy(one, &v, 16);
+#pragma unroll
+                        for (int k = 0; k < kPiece; k++)
+                            if (k < left) here[k] = one[k];
+                    }
                 }
             }
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         }
+    };
+    if (p.part) {
+        leave(p.part + z * p.split_out, p.ld_part, [&](int i, int j, int (&r)[4]) {
+#pragma unroll
+            for (int k = 0; k < 4; k++) r[k] = acc[i][j][k];
+        });
+        return;
     }
+    with_out(p, [&](auto* out) {
+        using O = typename std::remove_pointer<decltype(out)>::type;
+        leave(out, p.ld_out, [&](int i, int j, O (&r)[4]) {
+            const v4f v = scaled(acc[i][j], sa[16 * i], *reinterpret_cast<const v4f*>(sb + 16 * j), *reinterpret_cast<const v4f*>(bias + 16 * j));
+#pragma unroll
+            for (int k = 0; k < 4; k++) r[k] = from_f32<O>(v[k]);
+        });
+    });
 }
 
 // out from the sums of the splits: four columns of a row a thread
@@ -333,11 +461,18 @@ __global__ __launch_bounds__(256) void k_i8_join(Product p, int splits, uint32_t
     v4i v = *reinterpret_cast<const v4i*>(p.part + m * p.ld_part + n);
 #pragma unroll 4
     for (int z = 1; z < splits; z++) v += *reinterpret_cast<const v4i*>(p.part + z * p.split_out + m * p.ld_part + n);
-    store_out(p, m, n, v, p.sa[m], load_four(p.sb, n, p.N, 0.f), load_four(p.bias, n, p.N, 0.f));
+    store_out(p, m, n, v);
 }
 
+// Which kernel, and in how many parts of the depth: the least of the times that a product of these sizes is expected to take,
+// in us: fits to 22 sizes of 32 to 16384 rows, 512 to 8192 columns and a depth of 128 to 8192.  bf16 results, in us, few
+// rows / 128 x 128 / 128 x 128 with four steps in LDS / 256 x 256: 64 x 8192 x 2048 12.7 / 15.4 / 11.7 / -; 1024 x 1024 x 1024
+// 12.5 / 8.9 / 8.5 / 15.3; 1024 x 4096 x 4096 146 / 28.6 / 23.4 / 42.6; 2048 x 4096 x 2048 - / 23.1 / 26.8 / 28.7; 4096 x 8192 x 2048
+// - / 85.6 / 102 / 68.4; 16384 x 4096 x 128 - / 51.6 / 77.2 / 47.7.  In parts: 64 x 1024 x 8192 128 x 128 46.6, in 8 parts 13.1; 128 x
+// 4096 x 4096 18.7, in 2 parts 15.5.  Four steps' operands in LDS leave room for one workgroup a compute unit, not two: only where
+// there are no more.  Up to 16 rows the wavefronts of the first kernel waste nothing: always that one.
 struct Plan { int kernel, splits; int64_t split_blocks; };
-enum { kRows = 0, kTiles128 = 1, kTiles256 = 2 };
+enum { kRows = 0, kTiles128 = 1, kTiles256 = 2, kTiles128Deep = 3 };
 constexpr double kCus = 256;
 
 Plan make_plan(int64_t M, int64_t N, int64_t K) {
@@ -346,18 +481,21 @@ Plan make_plan(int64_t M, int64_t N, int64_t K) {
     if (M <= 16) return best;
     const double row_groups = (double)((M + 63) / 64) * ((N + 15) / 16);
     double least = 2.5 + 2.3 * ((blocks + kRowsWaves - 1) / kRowsWaves) * ceil(row_groups / kCus);
-    for (int kernel = kTiles128; kernel <= (M > 128 && N > 128 ? kTiles256 : kTiles128); kernel++)
+    for (int kernel = kTiles128; kernel <= kTiles256; kernel++)
         for (int64_t want = 1; want <= 16 && want <= blocks; want *= 2) {
             const int64_t side = kernel == kTiles256 ? 256 : 128;
             const int64_t per = (blocks + want - 1) / want, splits = (blocks + per - 1) / per;
             const double groups = (double)((M + side - 1) / side) * ((N + side - 1) / side) * splits;
-            const double busy = fmin(1.0, groups / kCus), rounds = ceil(groups / kCus);
-            const double start = kernel == kTiles128 ? 6.0 : 12.0, step = kernel == kTiles128 ? 0.6 + 0.1 * busy : 1.14 + 0.5 * busy;
-            double t = start + step * per * rounds + (kernel == kTiles128 ? 2.0 : 9.0) * (rounds - 1);
-            if (splits > 1) t += 4.0 + 1e-6 * splits * M * N;
+            const bool deep = kernel == kTiles128 && groups <= kCus;
+            const double busy = fmin(1.0, groups / kCus), rounds = ceil(groups / (kernel == kTiles128 ? 2 * kCus : kCus));
+            double t;
+            if (deep) t = 5.6 + (0.41 + 0.14 * busy) * per;
+            else if (kernel == kTiles128) t = 5.4 + 1.05 * per * rounds + 5.0 * (rounds - 1);
+            else t = 7.5 + 4.0 * busy + (1.07 + 0.4 * busy) * per * rounds + 6.0 * (rounds - 1);
+            if (splits > 1) t += 3.0 + 1.3e-6 * splits * M * N;
             if (t < least) {
                 least = t;
-                best = {kernel, (int)splits, per};
+                best = {deep ? (int)kTiles128Deep : kernel, (int)splits, per};
             }
         }
     return best;
@@ -400,10 +538,27 @@ hipError_t launch_i8_matmul(const fmtc_i8& a, const fmtc_i8& b, const float* d_b
     hipError_t e;
     if (plan.kernel == kTiles256) e = tiles(Tile<2, 4, 8, 4, 2>{});
     else if (plan.kernel == kTiles128) e = tiles(Tile<2, 2, 4, 4, 2>{});
+    else if (plan.kernel == kTiles128Deep) e = tiles(Tile<2, 2, 4, 4, 4>{});
     else e = p.M <= 16 ? rows(Int<1>{}) : rows(Int<4>{});
     if (e != hipSuccess || plan.splits == 1) return e;
     const int64_t quads = (p.N + 3) / 4;
     return launch(K_I8_MATMUL, k_i8_join, dim3((unsigned)((p.M * quads + 255) / 256)), dim3(256), 0, s, p, plan.splits, (uint32_t)quads);
+}
+
+bool i8_linear_is_one(int64_t M, int64_t K) { return linear_fits(M, K); }
+hipError_t launch_i8_linear_one(const void* d_x, int type, int64_t rows, int64_t ld_x, const fmtc_i8& w, const float* d_bias, void* d_out,
+                                int out_type, int64_t ld_out, hipStream_t s) {
+    Product p{nullptr, static_cast<const uint8_t*>(w.d_codes), nullptr, w.d_scales, d_bias, d_out, rows, w.rows,
+              (w.depth + kBlock - 1) / kBlock, 0, w.ld, ld_out, out_type, 0, 0, 0, nullptr};
+    int tpr = kLinearThreads;
+    for (int64_t r = 1; r < rows; r *= 2) tpr /= 2;
+    return with_type(type, [&](auto ty) {
+        using T = typename decltype(ty)::type;
+        return with_bit(w.depth % 8 != 0, [&](auto rg) {
+            return launch(K_I8_MATMUL, k_i8_linear_rows<T, decltype(rg)::value>, dim3((unsigned)((p.N + 15) / 16)), dim3(kLinearThreads), 0, s, p,
+                          static_cast<const T*>(d_x), w.depth, ld_x, tpr);
+        });
+    });
 }
 
 hipError_t launch_i8_quantize(const void* d_x, int type, int64_t rows, int64_t cols, int64_t ld_x, const fmtc_i8& out, hipStream_t s) {
