@@ -1,6 +1,7 @@
 """A residual network of pointwise blocks in 8-bit floating point, with its stream stored by the codec.
 
     python -m paper_1905_10830_amd.blocks [--channels 256] [--hidden 1024] [--blocks 3] [--steps 20] [--bits 6]
+                                          [--inputs 0] [--groups 8] [--max-norm 0]
 
 Every pixel of a map is a row of the stream h.  A block multiplies the normalised row by two weight matrices with a ReLU
 between them; its output is normalised, gated and added to the stream:
@@ -8,8 +9,11 @@ between them; its output is normalised, gated and added to the stream:
     y = W2 relu(W1 n + b1),   u = w_post y / rms(y),   h' = h + gate u,   n' = w_pre' h' / rms(h')
 
 The products take 8-bit codes with a scale per block of 128 (f8_quantize, f8_matmul, f8_matmul_backward), what lies
-between them is one call (block_norm, block_norm_backward).  The command trains such a network for a few steps on a
-synthetic map, then runs it forward only, one row at a time and as a whole, and stores the last stream with the
+between them is one call (block_norm, block_norm_backward).  With `inputs` channels a stem comes first: the maps' group norm
+with an activation and a product to the stream, h = Ws silu(group_norm(x)) + bs (group_norm, group_norm_backward).  A step
+normalises each gradient, or clips all of them together (Tensors).  To serve, the weights can be held as 8-bit integers with a
+scale for each row instead (i8_quantize, i8_linear, i8_matmul).  The command trains such a network for a few steps on a
+synthetic map, then runs it forward only, one row at a time and as a whole, in both forms, and stores the last stream with the
 feature-map codec (fit_basis, encode, decode).
 """
 import argparse
@@ -23,9 +27,10 @@ EPS = 1e-6
 
 
 class Blocks:
-    """Parameters (f32) of the blocks and the passes through them.  `scales`: fmtc.SCALE_F32 or fmtc.SCALE_E8M0."""
+    """Parameters (f32) of the blocks and the passes through them.  `scales`: fmtc.SCALE_F32 or fmtc.SCALE_E8M0.  inputs: the
+    channels of the maps that a stem makes the stream of (0: no stem, what comes in is the stream), in `groups` groups."""
 
-    def __init__(self, channels, hidden, blocks, scales=fmtc.SCALE_E8M0, seed=0, device="cuda"):
+    def __init__(self, channels, hidden, blocks, scales=fmtc.SCALE_E8M0, seed=0, device="cuda", inputs=0, groups=8):
         g = torch.Generator(device=device).manual_seed(seed)
         normal = lambda *s: torch.randn(s, generator=g, device=device)  # noqa: E731
         self.channels, self.scales = channels, scales
@@ -36,20 +41,37 @@ class Blocks:
                             f"w_post.{i}": torch.ones(channels, device=device),
                             f"gate.{i}": torch.full((1, channels), 0.5, device=device),
                             f"w_pre.{i + 1}": torch.ones(channels, device=device)}
-        self.blocks = blocks
-        self.codes = {}
+        self.blocks, self.inputs, self.groups = blocks, inputs, groups
+        self.products = [f"{w}.{i}" for i in range(blocks) for w in ("w1", "w2")]
+        if inputs:
+            self.params |= {"stem.weight": torch.ones(inputs, device=device), "stem.bias": torch.zeros(inputs, device=device),
+                            "ws": normal(channels, inputs) / inputs ** 0.5, "bs": torch.zeros(channels, device=device)}
+            self.products.append("ws")
+        self.codes, self.integers = {}, {}
         self.quantize_weights()
 
     def quantize_weights(self):
         """Weights as codes, for the products and (transposed) for their gradients: once after every change."""
-        for i in range(self.blocks):
-            for w in ("w1", "w2"):
-                self.codes[f"{w}.{i}"] = fmtc.f8_quantize(self.params[f"{w}.{i}"], by_cols=True, block_rows=fmtc.F8_BLOCK, scales=self.scales)
+        for w in self.products:
+            self.codes[w] = fmtc.f8_quantize(self.params[w], by_cols=True, block_rows=fmtc.F8_BLOCK, scales=self.scales)
 
-    def forward(self, h):
+    def quantize_integers(self):
+        """Weights as 8-bit integers for forward_integers: once the parameters stay as they are."""
+        for w in self.products:
+            self.integers[w] = fmtc.i8_quantize(self.params[w])
+
+    def _stem(self, x, rows_per_sample, **more):
+        p = self.params
+        return fmtc.group_norm(x, self.groups, p["stem.weight"], p["stem.bias"], rows_per_sample=rows_per_sample, act=fmtc.ACT_SILU, **more)
+
+    def forward(self, h, rows_per_sample=0):
         """The stream behind the last block and its normalised rows, without anything kept for gradients: the norm writes
-        the codes of the next product itself.  h: bf16 [rows, channels]."""
+        the codes of the next product itself.  h: bf16 [rows, channels], or with a stem [rows, inputs], rows_per_sample rows
+        (0: all) a map."""
         p, rows = self.params, len(h)
+        if self.inputs:
+            n, _ = fmtc.f8_quantize(self._stem(h, rows_per_sample)[0], scales=self.scales)
+            h = fmtc.f8_matmul(n, self.codes["ws"][0], bias=p["bs"])
         codes = lambda: fmtc.f8_empty(rows, self.channels, scales=self.scales, device=h.device)  # noqa: E731
         _, n, _ = fmtc.block_norm(None, h, None, p["w_pre.0"], eps=EPS, h_out=False, n_out=codes())
         for i in range(self.blocks):
@@ -60,9 +82,28 @@ class Blocks:
                                       n_out=codes() if i + 1 < self.blocks else None)
         return h, n
 
-    def forward_backward(self, h, target):
+    def forward_integers(self, h, rows_per_sample=0):
+        """As forward, with the weights of quantize_integers: rows are quantized on the way into each product, and the stem's
+        norm writes the codes of its product itself."""
+        p, q = self.params, self.integers
+        if self.inputs:
+            codes = fmtc.i8_empty(len(h), self.inputs, device=h.device)
+            h = fmtc.i8_matmul(self._stem(h, rows_per_sample, out=codes)[0], q["ws"], bias=p["bs"])
+        _, n, _ = fmtc.block_norm(None, h, None, p["w_pre.0"], eps=EPS, h_out=False)
+        for i in range(self.blocks):
+            a = fmtc.i8_linear(n, q[f"w1.{i}"], bias=p[f"b1.{i}"])
+            y = fmtc.i8_linear(a.relu_(), q[f"w2.{i}"])
+            h, n, _ = fmtc.block_norm(y, h, p[f"w_post.{i}"], p[f"w_pre.{i + 1}"], gate=p[f"gate.{i}"], eps=EPS)
+        return h, n
+
+    def forward_backward(self, h, target, rows_per_sample=0):
         """-> loss (half the mean square of n - target), gradients of the parameters by name."""
         p, kept = self.params, []
+        if self.inputs:
+            x = h
+            n, stem_stats = self._stem(x, rows_per_sample, stats=True)
+            n_q, stem_t = fmtc.f8_quantize(n, by_cols=True, scales=self.scales)
+            h = fmtc.f8_matmul(n_q, self.codes["ws"][0], bias=p["bs"])
         _, n, stats = fmtc.block_norm(None, h, None, p["w_pre.0"], eps=EPS, h_out=False, stats=True)
         first = (h, stats)
         for i in range(self.blocks):
@@ -82,25 +123,35 @@ class Blocks:
             dr, grads[f"w2.{i}"], _ = fmtc.f8_matmul_backward(dy, self.codes[f"w2.{i}"][1], r_t, scales=self.scales)
             da = torch.where(r > 0, dr, 0)
             dn, grads[f"w1.{i}"], grads[f"b1.{i}"] = fmtc.f8_matmul_backward(da, self.codes[f"w1.{i}"][1], n_t, scales=self.scales, bias=True)
-        _, _, _, grads["w_pre.0"], _ = fmtc.block_norm_backward(dn, dh, None, first[0], first[1], None, p["w_pre.0"])
+        _, dh, _, grads["w_pre.0"], _ = fmtc.block_norm_backward(dn, dh, None, first[0], first[1], None, p["w_pre.0"])
+        if self.inputs:
+            dn, grads["ws"], grads["bs"] = fmtc.f8_matmul_backward(dh, self.codes["ws"][1], stem_t, scales=self.scales, bias=True)
+            _, grads["stem.weight"], grads["stem.bias"] = fmtc.group_norm_backward(
+                dn, x, stem_stats, self.groups, p["stem.weight"], p["stem.bias"], rows_per_sample=rows_per_sample, act=fmtc.ACT_SILU, dx=False)
         return loss, grads
 
-    def step(self, h, target, rate):
-        """One step of gradient descent on normalised gradients.  -> loss"""
-        loss, grads = self.forward_backward(h, target)
-        for name, g in grads.items():
-            self.params[name] -= rate * self.params[name].norm() * g / g.norm().clamp_min(1e-30)
+    def step(self, h, target, rate, rows_per_sample=0, max_norm=None):
+        """One step of gradient descent: on normalised gradients, or, with max_norm, on gradients whose norm all together is at
+        most that.  -> loss"""
+        loss, grads = self.forward_backward(h, target, rows_per_sample)
+        if max_norm is not None:
+            fmtc.Tensors(grads.values()).clip(max_norm)
+            for name, g in grads.items():
+                self.params[name] -= rate * g
+        else:
+            for name, g in grads.items():
+                self.params[name] -= rate * self.params[name].norm() * g / g.norm().clamp_min(1e-30)
         self.quantize_weights()
         return loss
 
 
-def _map(pixels, channels, seed):
+def _map(pixels, channels, seed, outputs=None):
     """A synthetic stream and a smooth function of it to learn."""
     g = torch.Generator(device="cuda").manual_seed(seed)
     rank = max(1, channels // 8)
     z = torch.randn((pixels, rank), generator=g, device="cuda")
     h = z @ (torch.randn((rank, channels), generator=g, device="cuda") / rank ** 0.5)
-    target = torch.sin(z @ (torch.randn((rank, channels), generator=g, device="cuda") / rank ** 0.5))
+    target = torch.sin(z @ (torch.randn((rank, outputs or channels), generator=g, device="cuda") / rank ** 0.5))
     return h.to(torch.bfloat16), target
 
 
@@ -112,22 +163,27 @@ def main(argv=None):
     ap.add_argument("--steps", type=int, default=20)
     ap.add_argument("--side", type=int, default=56)
     ap.add_argument("--bits", type=int, default=6)
+    ap.add_argument("--inputs", type=int, default=0, help="channels of the maps before a stem (0: no stem)")
+    ap.add_argument("--groups", type=int, default=8, help="groups of the stem's norm")
+    ap.add_argument("--max-norm", type=float, default=0.0, help="clip all gradients together to this norm (0: normalise each)")
     a = ap.parse_args(argv)
-    net = Blocks(a.channels, a.hidden, a.blocks)
-    h, target = _map(a.side * a.side, a.channels, 1)
+    net = Blocks(a.channels, a.hidden, a.blocks, inputs=a.inputs, groups=a.groups)
+    h, target = _map(a.side * a.side, a.inputs or a.channels, 1, a.channels)
     losses = []
     for k in range(a.steps):
-        losses.append(float(net.step(h, target, 0.02)))
+        losses.append(float(net.step(h, target, 0.02, max_norm=a.max_norm or None)))
         print(f"step {k:3d}  loss {losses[-1]:.5f}", flush=True)
-    for rows in (1, len(h)):
-        x = h[:rows].contiguous()
-        net.forward(x)
-        torch.cuda.synchronize()
-        began = time.perf_counter()
-        for _ in range(20):
-            net.forward(x)
-        torch.cuda.synchronize()
-        print(f"forward, {rows} rows: {(time.perf_counter() - began) / 20 * 1e6:.0f} us", flush=True)
+    net.quantize_integers()
+    for name, forward in (("forward", net.forward), ("forward in integers", net.forward_integers)):
+        for rows in (1, len(h)):
+            x = h[:rows].contiguous()
+            forward(x)
+            torch.cuda.synchronize()
+            began = time.perf_counter()
+            for _ in range(20):
+                forward(x)
+            torch.cuda.synchronize()
+            print(f"{name}, {rows} rows: {(time.perf_counter() - began) / 20 * 1e6:.0f} us", flush=True)
     stream = net.forward(h)[0].float().view(1, a.side, a.side, a.channels)
     basis = fmtc.fit_basis(stream)
     stored, nbytes = fmtc.encode(basis, stream, a.bits)
