@@ -561,13 +561,25 @@ __global__ __launch_bounds__(1024) void k_group_norm_gradient_sums(Maps p, const
     sums_by_channel(p, at, stats, me.live, s, q, red_f, [&](int which, int c, float sum) { to[which * p.C + c] = sum; });
 }
 
+// The sum of from[first], from[first + step].. below n, `apart` from each other, 16 loads on their way together (a loop with a
+// remainder would wait for each load of that: 0.7 us each)
+__device__ __forceinline__ float strided_sum(const float* from, int64_t first, int64_t step, int64_t n, int64_t apart) {
+    float sum = 0.f;
+    for (int64_t k = first; k < n; k += 16 * step) {
+        float v[16];
+#pragma unroll
+        for (int j = 0; j < 16; j++) v[j] = from[(k + j * step < n ? k + j * step : n - 1) * apart];
+#pragma unroll
+        for (int j = 0; j < 16; j++) sum += k + j * step < n ? v[j] : 0.f;
+    }
+    return sum;
+}
+
 // dbias and dweight: sums over n rows of part, 32 columns a workgroup, slices of the rows, added up in order
 __device__ __forceinline__ void param_sums(const float* part, int64_t n, int C, float* dweight, float* dbias, float* slice) {
     const int col = threadIdx.x & 31, k = threadIdx.x >> 5, slices = blockDim.x >> 5, c = blockIdx.x * 32 + col;
     float sum = 0.f;
-    if (c < 2 * C)
-#pragma unroll 4
-        for (int64_t i = k; i < n; i += slices) sum += part[i * 2 * C + c];
+    if (c < 2 * C) sum = strided_sum(part + c, k, slices, n, 2 * C);
     slice[k * 33 + col] = sum;
     __syncthreads();
     if (k == 0 && c < 2 * C) {
@@ -595,9 +607,7 @@ __global__ __launch_bounds__(1024) void k_group_norm_dx(Maps p, const float* __r
     // sums over the chunks: neighbouring threads on neighbouring channels, several slices of the chunks where threads are left
     for (int i = t; i < (slices > 1 ? slices : 1) * wide; i += blockDim.x) {
         const int slice = i / wide, j = i - slice * wide, which = j >= at.width, c = at.c0 + j - which * at.width;
-        float sum = 0.f;
-#pragma unroll 4
-        for (int64_t k = slice; k < p.chunks; k += slices > 1 ? slices : 1) sum += part[(at.n * p.chunks + k) * 2 * p.C + which * p.C + c];
+        const float sum = strided_sum(part + at.n * p.chunks * 2 * p.C + which * p.C + c, slice, slices > 1 ? slices : 1, p.chunks, 2 * p.C);
         red_f[i] = sum * weight_at<T>(p, c);
     }
     __syncthreads();
@@ -646,6 +656,9 @@ struct Plan {
     int64_t chunks;           // two passes: parts of a sample's rows
 };
 constexpr double kCus = 256;
+// Every workgroup of the second pass reads the sums of all parts of its sample: 512 workgroups and 128 parts of 512 x 512 x 128
+// 39 us, 1024 and 256 47 us, 2048 and 256 53 us.
+constexpr int64_t kMostChunks = 128, kSecondPass = 512;
 
 int lanes_of(int W) { return (W + 7) / 8; }
 // registers of a thread for a slab: its rows go up in these steps
@@ -673,7 +686,7 @@ Plan make_plan(int64_t samples, int64_t S, int C, int groups, int size, int arra
     best.W = W;
     const int64_t rows = ceil_div(S, (int64_t)(kUnroll / arrays) * (best.threads / lanes_of(W)));
     best.chunks = want(W) < rows ? want(W) : rows;
-    best.chunks = ceil_div(S, ceil_div(S, best.chunks < 256 ? best.chunks : 256));
+    best.chunks = ceil_div(S, ceil_div(S, best.chunks < kMostChunks ? best.chunks : kMostChunks));
     if (!may_be_once) return best;
     double least = 8.0 + (bytes + values * size * arrays * (values * size * arrays > 2e8 ? 1.0 : 0.6)) / 5e6;
     for (int gs = 1;; gs = gs * 2 < groups ? gs * 2 : groups) {
@@ -780,7 +793,7 @@ hipError_t launch_group_norm(const fmtc_gnorm& a, void* d_y, int64_t ld_y, const
                 if (p.C <= 2048) return with(Int<256>{}, Int<1>{});
                 return with(Int<1024>{}, Int<1>{});
             }
-            const int64_t parts = d_y ? parts_of(p, p.LY, kUnroll, 1024 * 512 / plan.threads) : 1, rows = ceil_div(p.S, parts);
+            const int64_t parts = d_y ? parts_of(p, p.LY, kUnroll, kSecondPass) : 1, rows = ceil_div(p.S, parts);
             return go(K_GROUP_NORM, k_group_norm_apply<T, R>, p.samples * p.slabs * parts, plan.threads, lds_stats, s, p, part, parts, rows, a.eps,
                       a.act, static_cast<T*>(d_y), ld_y, d_stats);
         });
@@ -816,7 +829,7 @@ hipError_t launch_group_norm_backward(const fmtc_gnorm& a, const float* d_stats,
                                         d_stats, dy, ld_dy, part);
                 if (e != hipSuccess) return e;
                 if (!d_dx) return sum_params(p.samples * p.chunks);
-                const int64_t parts = parts_of(p, p.LY, kUnroll / 2, 1024 * 512 / plan.threads), rows = ceil_div(p.S, parts);
+                const int64_t parts = parts_of(p, p.LY, kUnroll / 2, kSecondPass), rows = ceil_div(p.S, parts);
                 size_t lds_dx = sizeof(float) * (2 * p.W > plan.threads ? 2 * p.W : plan.threads) + lds_ab;
                 if (lds_dx < sizeof(float) * 33 * (plan.threads / 32)) lds_dx = sizeof(float) * 33 * (plan.threads / 32);
                 return go(K_GROUP_NORM_BACKWARD, k_group_norm_dx<T, R, A>, param_groups + p.samples * p.slabs * parts, plan.threads, lds_dx, s, p, d_stats, part,
