@@ -326,7 +326,8 @@ __global__ __launch_bounds__(1024) void k_group_norm_apply(Maps p, const double2
     }
 }
 
-// To codes with a scale for each row: TPR lanes hold a row, VPT groups of 8 consecutive channels each.
+// To codes with a scale for each row: TPR lanes hold a row, VPT groups of 8 consecutive channels each.  The statistics come from
+// the sums of parts, or (part NULL) are there already.
 constexpr int codes_threads(int TPR) { return TPR < 256 ? 256 : TPR; }
 template <class T, bool RAGGED, int TPR, int VPT>
 __global__ __launch_bounds__(codes_threads(TPR)) void k_group_norm_codes(Maps p, const double2* __restrict__ part, int64_t parts, int64_t rows,
@@ -349,7 +350,15 @@ __global__ __launch_bounds__(codes_threads(TPR)) void k_group_norm_codes(Maps p,
     Scale scale[VPT];
 #pragma unroll
     for (int j = 0; j < VPT; j++) scale[j].template load<T, RAGGED>(p, at, 8 * (j * TPR + lane));
-    finish_parts(p, at, part, eps, mean_r, stats);
+    if (part) {
+        finish_parts(p, at, part, eps, mean_r, stats);
+    } else {
+        for (int g = threadIdx.x; g < p.G; g += blockDim.x) {
+            mean_r[g] = stats[at.n * p.G + g];
+            mean_r[p.G + g] = stats[(p.samples + at.n) * p.G + g];
+        }
+        __syncthreads();
+    }
 #pragma unroll
     for (int j = 0; j < VPT; j++) scale[j].settle(p, at, 8 * (j * TPR + lane), mean_r);
     int turn = 0;
@@ -673,7 +682,7 @@ int row_step(int64_t rows, int size) {
 }
 
 // The least of the times that are expected, in us.  arrays: read (1 forward, 2 backward)
-Plan make_plan(int64_t samples, int64_t S, int C, int groups, int size, int arrays, bool may_be_once) {
+Plan make_plan(int64_t samples, int64_t S, int C, int groups, int size, int arrays) {
     const int D = C / groups;
     const double values = (double)samples * S * C, bytes = values * size * (arrays + 1);
     Plan best{};
@@ -687,8 +696,7 @@ Plan make_plan(int64_t samples, int64_t S, int C, int groups, int size, int arra
     const int64_t rows = ceil_div(S, (int64_t)(kUnroll / arrays) * (best.threads / lanes_of(W)));
     best.chunks = want(W) < rows ? want(W) : rows;
     best.chunks = ceil_div(S, ceil_div(S, best.chunks < kMostChunks ? best.chunks : kMostChunks));
-    if (!may_be_once) return best;
-    double least = 8.0 + (bytes + values * size * arrays * (values * size * arrays > 2e8 ? 1.0 : 0.6)) / 5e6;
+    double least = 10.0 + (bytes + values * size * arrays * (values * size * arrays > 2e8 ? 1.0 : 0.6)) / 5e6;
     for (int gs = 1;; gs = gs * 2 < groups ? gs * 2 : groups) {
         const int W = gs * D, LX = lanes_of(W);
         for (int threads = 256; threads <= (arrays == 1 ? 1024 : 512); threads *= 2) {
@@ -749,20 +757,22 @@ int type_size(int type) { return type == FMTC_F32 ? 4 : 2; }
 }  // namespace
 
 size_t group_norm_workspace(int64_t samples, int64_t S, int C, int groups, int type, bool to_codes) {
-    const Plan plan = make_plan(samples, S, C, groups, type_size(type), 1, !to_codes);
-    return plan.rows ? 0 : align_up(sizeof(double2) * (size_t)(samples * plan.chunks) * groups, 256);
+    const Plan plan = make_plan(samples, S, C, groups, type_size(type), 1);
+    if (!plan.rows) return align_up(sizeof(double2) * (size_t)(samples * plan.chunks) * groups, 256);
+    return to_codes ? align_up(sizeof(float) * 2 * (size_t)samples * groups, 256) : 0;  // (statistics that the caller does not want)
 }
 size_t group_norm_backward_workspace(int64_t samples, int64_t S, int C, int groups) {
     size_t most = 0;
-    for (int size = 2; size <= 4; size += 2) {  // (in one pass there is one part of a sample, no more)
-        const size_t bytes = sizeof(float) * (size_t)(samples * make_plan(samples, S, C, groups, size, 2, false).chunks) * 2 * C;
+    for (int size = 2; size <= 4; size += 2) {  // (in one pass there is one part of a sample)
+        const Plan plan = make_plan(samples, S, C, groups, size, 2);
+        const size_t bytes = sizeof(float) * (size_t)(samples * (plan.rows ? 1 : plan.chunks)) * 2 * C;
         most = bytes > most ? bytes : most;
     }
     return align_up(most, 256);
 }
 
 hipError_t launch_group_norm(const fmtc_gnorm& a, void* d_y, int64_t ld_y, const fmtc_i8* codes, float* d_stats, void* d_ws, hipStream_t s) {
-    const Plan plan = make_plan(a.samples, a.rows_per_sample, a.C, a.groups, type_size(a.type), 1, !codes);
+    const Plan plan = make_plan(a.samples, a.rows_per_sample, a.C, a.groups, type_size(a.type), 1);
     Maps p = maps_of(a, plan);
     double2* const part = static_cast<double2*>(d_ws);
     return with_type(a.type, [&](auto ty) {
@@ -770,28 +780,33 @@ hipError_t launch_group_norm(const fmtc_gnorm& a, void* d_y, int64_t ld_y, const
         return with_bit(p.C % 8 != 0 || p.W % 8 != 0, [&](auto rg) {
             constexpr bool R = decltype(rg)::value;
             const size_t lds = sizeof(double) * (2 << p.pre) * plan.threads, lds_stats = sizeof(float) * 2 * p.groups;
+            float* const stats = codes && plan.rows && !d_stats ? static_cast<float*>(d_ws) : d_stats;
+            hipError_t e;
             if (plan.rows)
-                return with_rows<T>(plan.rows, [&](auto rows) {
+                e = with_rows<T>(plan.rows, [&](auto rows) {
                     return go(K_GROUP_NORM, k_group_norm_once<T, R, decltype(rows)::value>, p.samples * p.slabs, plan.threads, lds + lds_stats, s,
-                              p, a.eps, a.act, static_cast<T*>(d_y), ld_y, d_stats);
+                              p, a.eps, a.act, codes ? nullptr : static_cast<T*>(d_y), ld_y, stats);
                 });
-            const hipError_t e = go(K_GROUP_NORM, k_group_norm_sums<T, R>, p.samples * p.slabs * p.chunks, plan.threads, lds, s, p, part);
-            if (e != hipSuccess) return e;
+            else
+                e = go(K_GROUP_NORM, k_group_norm_sums<T, R>, p.samples * p.slabs * p.chunks, plan.threads, lds, s, p, part);
+            if (e != hipSuccess || (plan.rows && !codes)) return e;
             if (codes) {
                 p.W = p.C;  // (rows as a whole)
                 p.groups = p.G;
                 p.slabs = 1;
-                auto with = [&](auto tpr, auto vpt) {
-                    constexpr int TPR = decltype(tpr)::value, VPT = decltype(vpt)::value;
-                    const int64_t parts = parts_of(p, codes_threads(TPR) / TPR, 1, 2048), rows = ceil_div(p.S, parts);
-                    return go(K_GROUP_NORM, k_group_norm_codes<T, R, TPR, VPT>, p.samples * parts, codes_threads(TPR), sizeof(float) * 2 * p.G, s,
-                              p, part, parts, rows, a.eps, a.act, *codes, static_cast<T*>(d_y), ld_y, d_stats);
-                };
-                if (p.C <= 128) return with(Int<16>{}, Int<1>{});
-                if (p.C <= 512) return with(Int<64>{}, Int<1>{});
-                if (p.C <= 1024) return with(Int<64>{}, Int<2>{});
-                if (p.C <= 2048) return with(Int<256>{}, Int<1>{});
-                return with(Int<1024>{}, Int<1>{});
+                return with_bit(p.C % 8 != 0, [&](auto rg) {
+                    auto with = [&](auto tpr, auto vpt) {
+                        constexpr int TPR = decltype(tpr)::value, VPT = decltype(vpt)::value;
+                        const int64_t parts = parts_of(p, codes_threads(TPR) / TPR, 1, 2048), rows = ceil_div(p.S, parts);
+                        return go(K_GROUP_NORM, k_group_norm_codes<T, decltype(rg)::value, TPR, VPT>, p.samples * parts, codes_threads(TPR),
+                                  sizeof(float) * 2 * p.G, s, p, plan.rows ? nullptr : part, parts, rows, a.eps, a.act, *codes, static_cast<T*>(d_y), ld_y, stats);
+                    };
+                    if (p.C <= 128) return with(Int<16>{}, Int<1>{});
+                    if (p.C <= 512) return with(Int<64>{}, Int<1>{});
+                    if (p.C <= 1024) return with(Int<64>{}, Int<2>{});
+                    if (p.C <= 2048) return with(Int<256>{}, Int<1>{});
+                    return with(Int<1024>{}, Int<1>{});
+                });
             }
             const int64_t parts = d_y ? parts_of(p, p.LY, kUnroll, kSecondPass) : 1, rows = ceil_div(p.S, parts);
             return go(K_GROUP_NORM, k_group_norm_apply<T, R>, p.samples * p.slabs * parts, plan.threads, lds_stats, s, p, part, parts, rows, a.eps,
@@ -802,7 +817,7 @@ hipError_t launch_group_norm(const fmtc_gnorm& a, void* d_y, int64_t ld_y, const
 
 hipError_t launch_group_norm_backward(const fmtc_gnorm& a, const float* d_stats, const void* d_dy, int64_t ld_dy, void* d_dx, int64_t ld_dx,
                                       float* d_dweight, float* d_dbias, void* d_ws, hipStream_t s) {
-    const Plan plan = make_plan(a.samples, a.rows_per_sample, a.C, a.groups, type_size(a.type), 2, true);
+    const Plan plan = make_plan(a.samples, a.rows_per_sample, a.C, a.groups, type_size(a.type), 2);
     const Maps p = maps_of(a, plan);
     float* const part = static_cast<float*>(d_ws);
     return with_type(a.type, [&](auto ty) {

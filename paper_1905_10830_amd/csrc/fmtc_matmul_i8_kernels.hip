@@ -576,6 +576,7 @@ hipError_t launch_i8_quantize(const void* d_x, int type, int64_t rows, int64_t c
             // (the zeros behind a row are written by its lanes: they have to reach a multiple of 128)
             if (cols <= 128) return go(Int<16>{}, Int<1>{});
             if (cols <= 512) return go(Int<64>{}, Int<1>{});
+            if (cols <= 1024) return go(Int<64>{}, Int<2>{});
             if (cols <= 2048) return go(Int<256>{}, Int<1>{});
             if (cols <= 4096) return go(Int<256>{}, Int<2>{});
             if (cols <= 8192) return go(Int<1024>{}, Int<1>{});
