@@ -12,7 +12,7 @@ namespace {
 
 constexpr int kMost = 128;       // arrays of a launch (kernel arguments are 4096 bytes at most)
 constexpr int kThreads = 256;
-constexpr int64_t kStep = 8 * kThreads;      // values that a workgroup takes at a time
+constexpr int64_t kStep = 8 * kThreads;      // pieces are multiples of it: what a workgroup takes at a time, or twice that
 constexpr int64_t kPieces = 2048;            // about as many pieces as run at a time
 
 struct List {
@@ -49,49 +49,51 @@ template <class T>
 __device__ __forceinline__ int64_t values_before_line(const void* p) {
     return (int64_t)((0 - (uintptr_t)p) % 128 / sizeof(T));
 }
-// The values of a piece: f(index, values) for 8 at a time from `lead` on, U loads on their way together, and one(index) for
-// each of the few before the first line and behind the last 8.
-template <class T, int U, class F, class G>
+// The values of a piece: f(index, values) for V at a time from `lead` on, U loads on their way together, and one(index) for
+// each of the few before the first line and behind the last V.
+template <class T, int V, int U, class F, class G>
 __device__ __forceinline__ void walk(const T* in, int64_t index, int64_t piece, int64_t n, int64_t lead, F&& f, G&& one) {
+    constexpr int64_t kEach = V * kThreads;
     const int64_t c1 = lead + (index + 1) * piece < n ? lead + (index + 1) * piece : n;
     int64_t c = lead + index * piece;
     if (index == 0)
         for (int64_t i = threadIdx.x; i < (lead < n ? lead : n); i += kThreads) one(i);
-    const int64_t whole = c < c1 ? c + (c1 - c) / 8 * 8 : c;
+    const int64_t whole = c < c1 ? c + (c1 - c) / V * V : c;
     for (int64_t i = whole + threadIdx.x; i < c1; i += kThreads) one(i);
-    c += 8 * threadIdx.x;
-    for (; c + (U - 1) * kStep < whole; c += U * kStep) {
-        Raw<T> raw[U];
+    c += V * threadIdx.x;
+    for (; c + (U - 1) * kEach < whole; c += U * kEach) {
+        T raw[U][V];
 #pragma unroll
-        for (int u = 0; u < U; u++) raw[u].template load<false>(in, c + u * kStep, n);
+        for (int u = 0; u < U; u++) __builtin_memcpy(raw[u], in + c + u * kEach, sizeof raw[u]);
 #pragma unroll
         for (int u = 0; u < U; u++) {
-            float v[8];
+            float v[V];
 #pragma unroll
-            for (int i = 0; i < 8; i++) v[i] = raw[u][i];
-            f(c + u * kStep, v);
+            for (int i = 0; i < V; i++) v[i] = to_f32(raw[u][i]);
+            f(c + u * kEach, v);
         }
     }
-    for (; c < whole; c += kStep) {
-        float v[8];
-        load8<false>(in, c, n, v);
+    for (; c < whole; c += kEach) {
+        T raw[V];
+        __builtin_memcpy(raw, in + c, sizeof raw);
+        float v[V];
+#pragma unroll
+        for (int i = 0; i < V; i++) v[i] = to_f32(raw[i]);
         f(c, v);
     }
 }
 
-// 8 values, at a multiple of 16 bytes, past the caches, which keep what the first pass read
-template <class O>
-__device__ __forceinline__ void stream8(O* p, const float (&v)[8]) {
+// 16 bytes of results, at a multiple of 16 bytes, past the caches, which keep what the first pass read
+template <class O, int V>
+__device__ __forceinline__ void stream_out(O* p, const float (&v)[V]) {
     typedef uint32_t words __attribute__((ext_vector_type(4)));
-    O t[8];
+    static_assert(V * sizeof(O) == 16);
+    O t[V];
 #pragma unroll
-    for (int i = 0; i < 8; i++) t[i] = from_f32<O>(v[i]);
-#pragma unroll
-    for (int i = 0; i < (int)sizeof t / 16; i++) {
-        words w;
-        __builtin_memcpy(&w, reinterpret_cast<const char*>(t) + 16 * i, 16);
-        __builtin_nontemporal_store(w, reinterpret_cast<words*>(reinterpret_cast<char*>(p) + 16 * i));
-    }
+    for (int i = 0; i < V; i++) t[i] = from_f32<O>(v[i]);
+    words w;
+    __builtin_memcpy(&w, t, 16);
+    __builtin_nontemporal_store(w, reinterpret_cast<words*>(p));
 }
 
 template <class F>
@@ -109,10 +111,11 @@ __global__ __launch_bounds__(kThreads) void k_clip_squares(List a, double* __res
     with_kind(a.type[k], [&](auto ty) {
         using T = typename decltype(ty)::type;
         const T* const in = static_cast<const T*>(a.in[k]);
-        walk<T, 4>(in, piece - a.first[k], a.piece, a.n[k], values_before_line<T>(in),
-                   [&](int64_t, const float (&v)[8]) {
+        constexpr int V = 16 / sizeof(T);
+        walk<T, V, 4>(in, piece - a.first[k], a.piece, a.n[k], values_before_line<T>(in),
+                   [&](int64_t, const float (&v)[V]) {
 #pragma unroll
-                       for (int i = 0; i < 8; i += 2) {
+                       for (int i = 0; i < V; i += 2) {
                            s0 = fma((double)v[i], (double)v[i], s0);
                            s1 = fma((double)v[i + 1], (double)v[i + 1], s1);
                        }
@@ -146,12 +149,13 @@ __global__ __launch_bounds__(kThreads) void k_clip_scale(List a, const double* _
             using O = typename decltype(to)::type;
             O* const out = static_cast<O*>(a.out[k]);
             const T* const in = static_cast<const T*>(a.in[k]);
-            walk<T, 4>(in, piece - a.first[k], a.piece, a.n[k], values_before_line<O>(out),
-                       [&](int64_t c, const float (&v)[8]) {
-                           float w[8];
+            constexpr int V = 16 / sizeof(O);  // (a wavefront writes whole lines: 200e6 values of 2 bytes to f32 298 -> 225 us)
+            walk<T, V, 4>(in, piece - a.first[k], a.piece, a.n[k], values_before_line<O>(out),
+                       [&](int64_t c, const float (&v)[V]) {
+                           float w[V];
 #pragma unroll
-                           for (int i = 0; i < 8; i++) w[i] = v[i] * f;
-                           stream8(out + c, w);
+                           for (int i = 0; i < V; i++) w[i] = v[i] * f;
+                           stream_out(out + c, w);
                        },
                        [&](int64_t c) { out[c] = from_f32<O>(to_f32(in[c]) * f); });
         });
@@ -166,28 +170,22 @@ int64_t piece_values(const fmtc_tensor* list, int64_t count) {
 }
 int64_t pieces_of(int64_t n, int64_t piece) { return (n + piece - 1) / piece; }
 
-// The arrays of launch `which`, kMost of those that have values; base: the pieces of the launches before it
-List take(const fmtc_tensor* list, int64_t count, int64_t piece, int64_t which) {
+// The arrays from *at on that fit a launch, and where the next one begins; base: the pieces of the launches before it
+List take(const fmtc_tensor* list, int64_t count, int64_t piece, int64_t* at, uint32_t base) {
     List a{};
     a.piece = piece;
-    int64_t before = which * kMost;
+    a.base = base;
     int k = 0;
-    for (int64_t i = 0; i < count && k < kMost; i++) {
-        const fmtc_tensor& t = list[i];
+    for (; *at < count && k < kMost; ++*at) {
+        const fmtc_tensor& t = list[*at];
         if (t.n == 0) continue;
-        const uint32_t pieces = (uint32_t)pieces_of(t.n, piece);
-        if (before > 0) {
-            before--;
-            a.base += pieces;
-            continue;
-        }
         a.in[k] = t.d_in;
         a.out[k] = t.d_out;
         a.n[k] = t.n;
         a.first[k] = a.pieces;
         a.type[k] = (uint8_t)t.type;
         a.out_type[k] = (uint8_t)t.out_type;
-        a.pieces += pieces;
+        a.pieces += (uint32_t)pieces_of(t.n, piece);
         k++;
     }
     for (; k < kMost; k++) a.first[k] = ~0u;
@@ -206,28 +204,27 @@ size_t clip_workspace(const fmtc_tensor* list, int64_t count) {
 hipError_t launch_clip(const fmtc_tensor* list, int64_t count, double max_norm, double scale, double eps, float* d_norm, void* d_ws, hipStream_t s) {
     const int64_t piece = piece_values(list, count);
     double* const sums = static_cast<double*>(d_ws);
-    int64_t full = 0;
     uint32_t n_sums = 0;
     bool write = false;
-    for (int64_t i = 0; i < count; i++)
-        if (list[i].n) {
-            full++;
-            n_sums += (uint32_t)pieces_of(list[i].n, piece);
-            write = write || list[i].d_out;
-        }
-    const int64_t launches = (full + kMost - 1) / kMost;
     hipError_t e = hipSuccess;
-    List a{};
-    for (int64_t k = 0; k < launches && e == hipSuccess; k++) {
-        a = take(list, count, piece, k);
-        e = launch(K_CLIP, k_clip_squares, dim3(a.pieces), dim3(kThreads), 0, s, a, sums);
+    for (int64_t at = 0; at < count && e == hipSuccess;) {
+        const List a = take(list, count, piece, &at, n_sums);
+        if (a.pieces) e = launch(K_CLIP, k_clip_squares, dim3(a.pieces), dim3(kThreads), 0, s, a, sums);
+        n_sums += a.pieces;
+        write = write || a.out[0];
     }
     if (e == hipSuccess && d_norm && !write) {
         const List none{};
         return launch(K_CLIP, k_clip_scale, dim3(1), dim3(kThreads), 0, s, none, sums, n_sums, max_norm, scale, eps, d_norm);
     }
-    for (int64_t k = launches - 1; k >= 0 && write && e == hipSuccess; k--) {
-        if (k < launches - 1) a = take(list, count, piece, k);
+    // the last arrays first, whose values were read last
+    for (int64_t end = count; end > 0 && write && e == hipSuccess;) {
+        int64_t from = end;
+        for (int k = 0; from > 0 && k < kMost;) k += list[--from].n != 0;
+        int64_t at = from;
+        const List a = take(list, end, piece, &at, 0);
+        end = from;
+        if (!a.pieces) continue;
         e = launch(K_CLIP, k_clip_scale, dim3(a.pieces), dim3(kThreads), 0, s, a, sums, n_sums, max_norm, scale, eps, d_norm);
         d_norm = nullptr;
     }
