@@ -1,5 +1,8 @@
 """Group norm, products in 8-bit integers, gradients and clipping as they are used together: in one HIP graph replayed between
 eager work, on another stream, with workspaces of the caller's, and where a call may not be made."""
+import os
+import re
+
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -136,3 +139,19 @@ def test_inputs_of_another_stream_are_in_order():
     side.synchronize()
     want = ref.group_norm(x, 1, 1, None, None, "none", 1e-5, torch.float32)
     assert bool(((y.double() - want[0]).abs() <= want[1]).all())
+
+
+def test_the_program_of_the_readme():
+    text = open(os.path.join(os.path.dirname(os.path.dirname(__file__)), "README.md")).read()
+    code = [c for c in re.findall(r"```python\n(.*?)```", text, re.S) if "i8_linear" in c]
+    assert len(code) == 1
+    names = {"torch": torch, "fmtc": fmtc}
+    exec(code[0], names)
+    # two operands off by 0.8 % each (1 / sqrt(12) of 1 / 127 of a row's largest, 3 to 4 times its size)
+    want = names["x"].double() @ names["w"].double().t()
+    assert float((names["rows"].double() - want).norm() / want.norm()) < 0.02
+    want = names["y"].double() @ names["w"].double().t()
+    assert float((names["out"].double() - want).norm() / want.norm()) < 0.02
+    squares = sum(float(names[k].double().square().sum()) for k in ("dweight", "dshift"))
+    assert abs(squares ** 0.5 - min(1.0, float(names["total"]))) < 1e-5
+    assert names["dx"].shape == names["x"].shape
