@@ -399,30 +399,32 @@ __global__ __launch_bounds__(codes_threads(TPR)) void k_group_norm_codes(Maps p,
 }
 
 // ---- gradients ----
-// What a thread needs of its 8 channels: d = x - m, z = d a + b; x^ = d r only enters sums, to which r is a factor
+// What a thread needs of its 8 channels: x^ = (x - m) r, z = (x - m) a + b with a = w r.  (r stays with its x - m: apart from it,
+// as a factor of the sums, values of 1e19 and more or 1e-19 and less leave f32.)
 struct Channels {
-    float m[8], a[8], b[8];
+    float m[8], r[8], a[8], b[8];
     template <class T, bool RAGGED>
     __device__ __forceinline__ void load(const Maps& p, const Place& at, const float* stats, int c) {
         load_param<T, RAGGED>(p.w, p.weight_type, at.c0 + c, p.C, 1.f, a);
         load_param<T, RAGGED>(p.b, p.weight_type, at.c0 + c, p.C, 0.f, b);
-        const float *const mean = stats + at.n * p.G + at.g0, *const r = mean + p.samples * p.G;
+        const float *const mean = stats + at.n * p.G + at.g0, *const rs = mean + p.samples * p.G;
         each_group(c, at.width, p.D, [&](int i, int g) {
             m[i] = mean[g];
-            a[i] *= r[g];
+            r[i] = rs[g];
+            a[i] *= rs[g];
         });
     }
+    __device__ __forceinline__ float xh(int i, float x) const { return (x - m[i]) * r[i]; }
     template <int ACT>
     __device__ __forceinline__ float dz(int i, float x, float dy) const {
         return ACT == FMTC_ACT_NONE ? dy : dy * act_gradient<ACT>(fmaf(x - m[i], a[i], b[i]));
     }
 };
 
-// The sums of dz (s) and of dz d (q) of all threads, by channel of the slab, those of dz d times r: f(0 or 1, channel, sum) on
-// one thread each.  red: 16 floats a thread.
+// The sums of dz (s) and of dz x^ (q) of all threads, by channel of the slab: f(0 or 1, channel, sum) on one thread each.  red:
+// 16 floats a thread.
 template <class F>
-__device__ __forceinline__ void sums_by_channel(const Maps& p, const Place& at, const float* stats, bool live, const float (&s)[8],
-                                                const float (&q)[8], float* red, F&& f) {
+__device__ __forceinline__ void sums_by_channel(const Maps& p, const Place& at, bool live, const float (&s)[8], const float (&q)[8], float* red, F&& f) {
     const int T = blockDim.x;
 #pragma unroll
     for (int i = 0; i < 8; i++) {
@@ -436,7 +438,7 @@ __device__ __forceinline__ void sums_by_channel(const Maps& p, const Place& at, 
         float sum = 0.f;
         for (int y = l; y < p.LY; y += lanes) sum += from[y * p.LX];
         sum = lanes_sum(sum, lanes);
-        if (l == 0) f(which, c, which ? sum * stats[(p.samples + at.n) * p.G + at.g0 + quotient(c, 1.f / (float)p.D)] : sum);
+        if (l == 0) f(which, c, sum);
     });
 }
 
@@ -456,19 +458,17 @@ __device__ __forceinline__ void group_terms(const Maps& p, const Place& at, cons
     });
     __syncthreads();
 }
-// dx = r (w dz - A - x^ B) = a dz + (d D + E):  D = -r r B, E = -r A
+// dx = r (w dz - A - x^ B) = a dz + (x^ D + E):  D = -r B, E = -r A
 struct Terms {
     float D[8], E[8];
-    __device__ __forceinline__ void load(const Maps& p, const Place& at, const float* stats, int c, const float* ab) {
-        const float* const rs = stats + (p.samples + at.n) * p.G + at.g0;
+    __device__ __forceinline__ void load(const Maps& p, const Place& at, const Channels& ch, int c, const float* ab) {
         each_group(c, at.width, p.D, [&](int i, int g) {
-            const float r = rs[g];
-            E[i] = -r * ab[g];
-            D[i] = -r * (r * ab[at.groups + g]);
+            E[i] = -ch.r[i] * ab[g];
+            D[i] = -ch.r[i] * ab[at.groups + g];
         });
     }
     __device__ __forceinline__ float dx(const Channels& ch, int i, float x, float dz) const {
-        return fmaf(dz, ch.a[i], fmaf(x - ch.m[i], D[i], E[i]));
+        return fmaf(dz, ch.a[i], fmaf(ch.xh(i, x), D[i], E[i]));
     }
 };
 
@@ -505,13 +505,13 @@ __global__ __launch_bounds__(512) void k_group_norm_backward_once(Maps p, const 
             for (int i = 0; i < 8; i++) {
                 dz[u][i] = ch.dz<ACT>(i, raw[u][i], raw_g[u][i]);
                 s[i] += dz[u][i];
-                q[i] = fmaf(dz[u][i], raw[u][i] - ch.m[i], q[i]);
+                q[i] = fmaf(dz[u][i], ch.xh(i, raw[u][i]), q[i]);
             }
             __builtin_amdgcn_sched_barrier(0);  // (row by row: all rows widened at a time are more than the registers hold)
         }
     }
     float* const to = part + at.n * 2 * p.C + at.c0;
-    sums_by_channel(p, at, stats, me.live, s, q, red_f, [&](int which, int c, float sum) {
+    sums_by_channel(p, at, me.live, s, q, red_f, [&](int which, int c, float sum) {
         to[which * p.C + c] = sum;
         by_channel[which * at.width + c] = sum * weight_at<T>(p, at.c0 + c);
     });
@@ -524,7 +524,7 @@ __global__ __launch_bounds__(512) void k_group_norm_backward_once(Maps p, const 
 #pragma unroll
         for (int i = 0; i < Raw<T>::kWords; i++) asm volatile("" : "+v"(raw[u].w[i]));
     Terms terms;
-    terms.load(p, at, stats, me.c, ab);
+    terms.load(p, at, ch, me.c, ab);
     T* const out = slab_of<T>(dx, ld_dx, p, at);
 #pragma unroll
     for (int u = 0; u < R; u++) {
@@ -567,13 +567,13 @@ __global__ __launch_bounds__(1024) void k_group_norm_gradient_sums(Maps p, const
                 for (int i = 0; i < 8; i++) {
                     const float dz = ch.dz<ACT>(i, raw[u][i], raw_g[u][i]);
                     s[i] += dz;
-                    q[i] = fmaf(dz, raw[u][i] - ch.m[i], q[i]);
+                    q[i] = fmaf(dz, ch.xh(i, raw[u][i]), q[i]);
                 }
             }
         }
     }
     float* const to = part + (at.n * p.chunks + at.k) * 2 * p.C + at.c0;
-    sums_by_channel(p, at, stats, me.live, s, q, red_f, [&](int which, int c, float sum) { to[which * p.C + c] = sum; });
+    sums_by_channel(p, at, me.live, s, q, red_f, [&](int which, int c, float sum) { to[which * p.C + c] = sum; });
 }
 
 // The sum of from[first], from[first + step].. below n, `apart` from each other, 16 loads on their way together (a loop with a
@@ -638,7 +638,7 @@ __global__ __launch_bounds__(1024) void k_group_norm_dx(Maps p, const float* __r
     Channels ch;
     ch.load<T, RAGGED>(p, at, stats, me.c);
     Terms terms;
-    terms.load(p, at, stats, me.c, ab);
+    terms.load(p, at, ch, me.c, ab);
     const int64_t r0 = at.k * rows, r1 = r0 + rows < p.S ? r0 + rows : p.S;
     const T *const x = slab_of<T>(p.x, p.ld, p, at), *const g = slab_of<T>(dy, ld_dy, p, at);
     T* const out = slab_of<T>(dx, ld_dx, p, at);

@@ -126,6 +126,27 @@ def test_gradients_are_those_of_the_forward_pass(act):
             assert abs(diff - float(grad.view(-1)[i])) <= 1e-6 * (1 + abs(diff))
 
 
+@pytest.mark.parametrize("samples, rows", [(2, 500), (1, 40000)])
+@pytest.mark.parametrize("size", [1e-25, 1e25])
+def test_values_whose_squares_leave_f32(size, samples, rows):
+    """eps 0: the result is that of the same map at size 1, dx as much smaller as the values are larger"""
+    x = _values(samples, rows, 64, torch.float32)
+    dy = _values(samples, rows, 64, torch.float32, 2)
+    w, b = _params(64, torch.float32)
+    kw = dict(rows_per_sample=rows, act=fmtc.ACT_SILU)
+    big = x * size
+    y, stats = fmtc.group_norm(big, 8, w, b, stats=True, eps=0.0, **kw)
+    _close(y, *ref.group_norm(big, samples, 8, w, b, "silu", 0.0, torch.float32)[:2])
+    (want, want_w, want_b), (terms, terms_w, terms_b) = ref.group_norm_backward(dy, big, samples, 8, w, b, "silu", 0.0, stats)
+    dx, dw, db = fmtc.group_norm_backward(dy, big, stats, 8, w, b, **kw)
+    # as many roundings as there are additions, and 48 of the values' own (the difference to the mean, x^, z and the activation)
+    share = ref.U * (rows + 8 + samples + 48)
+    far = 1 + ((stats[0].abs() * stats[1]).max().double())  # the mean, in deviations: what its rounding is worth
+    _close(dx, want, 4 * share * far * terms)
+    _close(dw, want_w, 4 * share * far * terms_w)
+    _close(db, want_b, 4 * share * far * terms_b)
+
+
 def test_mean_far_from_zero():
     """A mean of 1000 deviations: the variance is as good as without it, and what is left is the rounding of the mean."""
     x = 1000.0 + _values(2, 500, 64, torch.float32, offset=0.0)
