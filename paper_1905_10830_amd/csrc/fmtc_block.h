@@ -117,6 +117,10 @@ struct Raw {
             }
         }
     }
+    // the same for rows known to have 8 values or more: no question stands between loads
+    __device__ __forceinline__ void load_long(const T* row, int64_t c, int64_t C) {
+        __builtin_memcpy(w, row + (c + 8 <= C ? c : c < C ? C - 8 : 0), sizeof w);
+    }
     // when the values are there, in rows whose length is no multiple of 8 (kernels are built for either: without the question
     // the loads of aligned rows run up to a tenth faster): those at the end of a row to their places, 0 behind them
     __device__ __forceinline__ void settle(int64_t c, int64_t C) {

@@ -45,14 +45,36 @@ struct Place {
 // i / d for i up to 2^20, r = 1 / d: what is added keeps the product further from the next whole number than its roundings go
 __device__ __forceinline__ int quotient(int i, float r) { return (int)(((float)i + 0.5f) * r); }
 
+// How the rows of a slab lie: multiples of 8 channels at multiples of 8; 8 channels or more; any number of them.  (The question
+// whether there are 8, asked at each load, holds the loads apart: sums of 41 x 1716 x
+// 522 40.8 -> 35.0 us, gradient sums of 2 x 18281 x 435 21.0 -> 18.4 us; rows that begin at multiples of 16 bytes: 17.8 and 15.8.)
+enum Kind { kWhole = 0, kLong = 1, kShort = 2 };
+template <int KIND, class T>
+__device__ __forceinline__ void load_raw(Raw<T>& raw, const T* row, int64_t c, int64_t C) {
+    if constexpr (KIND == kLong) raw.load_long(row, c, C);
+    else raw.template load<KIND == kShort>(row, c, C);
+}
+template <int KIND, class T>
+__device__ __forceinline__ void settle_raw(Raw<T>& raw, int64_t c, int64_t C) {
+    if constexpr (KIND == kLong) raw.settle(c, C);  // (short rows are loaded value by value, with zeros behind them)
+}
+template <int KIND, class T>
+__device__ __forceinline__ void load_values(const T* row, int64_t c, int64_t C, float (&v)[8]) {
+    Raw<T> raw;
+    load_raw<KIND>(raw, row, c, C);
+    if constexpr (KIND != kWhole) raw.settle(c, C);
+#pragma unroll
+    for (int i = 0; i < 8; i++) v[i] = raw[i];
+}
+
 // channels c .. c + 7 of the weight (1 where there is none) or of the bias (0); f32, or the type of the values
-template <class T, bool RAGGED>
+template <class T, int KIND>
 __device__ __forceinline__ void load_param(const void* p, int type, int c, int C, float without, float (&v)[8]) {
 #pragma unroll
     for (int i = 0; i < 8; i++) v[i] = without;
     if (p) {
-        if (type == FMTC_F32) load8<RAGGED>(static_cast<const float*>(p), c, C, v);
-        else load8<RAGGED>(static_cast<const T*>(p), c, C, v);
+        if (type == FMTC_F32) load_values<KIND>(static_cast<const float*>(p), c, C, v);
+        else load_values<KIND>(static_cast<const T*>(p), c, C, v);
     }
 }
 // f(i, group) for each of 8 channels from c on (of a slab of `width`; those past it: the last one's group)
@@ -127,13 +149,39 @@ __device__ __forceinline__ void sums_by_group(const Maps& p, const Place& at, bo
             red[(n + i) * T + threadIdx.x] = live ? q[i] : 0.0;
         }
     __syncthreads();
+    auto part_of = [&](int g, int first, int step, double* a, double* b) {
+#pragma unroll 4
+        for (int i = first; i < p.LY * D; i += step) {
+            const int y = quotient(i, rD), v = g * D + i - y * D, from = (v & (n - 1)) * T + y * p.LX + (v >> pre);
+            *a += red[from];
+            *b += red[n * T + from];
+        }
+    };
+    // Few groups: several wavefronts for each, whose sums meet in LDS again (2 x 16 x 448, one group of 14 channels a workgroup of
+    // 1024: 15.8 us with one wavefront, 11 with four or more).
+    const int waves = T / 64;
+    if (2 * at.groups <= waves) {
+        __shared__ double few[2][16];
+        const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, teams = waves / at.groups, g = wave / teams, team = wave - g * teams;
+        double a = 0.0, b = 0.0;
+        if (g < at.groups) part_of(g, team * 64 + lane, teams * 64, &a, &b);
+        a = lanes_sum(a, 64);
+        b = lanes_sum(b, 64);
+        if (lane == 0) few[0][wave] = a, few[1][wave] = b;
+        __syncthreads();
+        if ((int)threadIdx.x < at.groups) {
+            a = b = 0.0;
+            for (int i = 0; i < teams; i++) {
+                a += few[0][threadIdx.x * teams + i];
+                b += few[1][threadIdx.x * teams + i];
+            }
+            f((int)threadIdx.x, a, b);
+        }
+        return;
+    }
     spread(at.groups, [&](int g, int l, int lanes) {
         double a = 0.0, b = 0.0;
-        for (int i = l; i < p.LY * D; i += lanes) {
-            const int y = quotient(i, rD), v = g * D + i - y * D, from = (v & (n - 1)) * T + y * p.LX + (v >> pre);
-            a += red[from];
-            b += red[n * T + from];
-        }
+        part_of(g, l, lanes, &a, &b);
         a = lanes_sum(a, lanes);
         b = lanes_sum(b, lanes);
         if (l == 0) f(g, a, b);
@@ -165,10 +213,10 @@ __device__ __forceinline__ void finish(const Maps& p, const Place& at, int g, do
 // y = act((x - m) w + b) of a thread's 8 channels (c: of the slab's).  The parameters set out before the statistics are there.
 struct Scale {
     float m[8], w[8], b[8];
-    template <class T, bool RAGGED>
+    template <class T, int KIND>
     __device__ __forceinline__ void load(const Maps& p, const Place& at, int c) {
-        load_param<T, RAGGED>(p.w, p.weight_type, at.c0 + c, p.C, 1.f, w);
-        load_param<T, RAGGED>(p.b, p.weight_type, at.c0 + c, p.C, 0.f, b);
+        load_param<T, KIND>(p.w, p.weight_type, at.c0 + c, p.C, 1.f, w);
+        load_param<T, KIND>(p.b, p.weight_type, at.c0 + c, p.C, 0.f, b);
     }
     __device__ __forceinline__ void settle(const Maps& p, const Place& at, int c, const float* mean_r) {
         each_group(c < at.width ? c : at.width - 1, at.width, p.D, [&](int i, int g) {
@@ -210,7 +258,7 @@ constexpr int kUnroll = 4;  // rows of a thread on their way together
 
 // A slab in the registers of a workgroup, R rows a thread.  256 x 3136 x 64 (32 groups, a ReLU) 41 to 45 us, 4.6 to 5.0 TB/s
 // (in two passes 64); 128 x 784 x 256 23 us; 196 x 256 5.6 us, latency.
-template <class T, bool RAGGED, int R>
+template <class T, int KIND, int R>
 __global__ __launch_bounds__(1024) void k_group_norm_once(Maps p, float eps, int act_kind, T* y, int64_t ld_y, float* __restrict__ stats) {
     extern __shared__ __attribute__((aligned(16))) double red[];
     const Place at(p, 1, 0);
@@ -224,12 +272,12 @@ __global__ __launch_bounds__(1024) void k_group_norm_once(Maps p, float eps, int
 #pragma unroll
         for (int u = 0; u < R; u++) {
             const int64_t r = me.ly + (int64_t)u * p.LY;
-            raw[u].template load<RAGGED>(x + (r < p.S ? r : 0) * p.ld, me.c, at.width);
+            load_raw<KIND>(raw[u], x + (r < p.S ? r : 0) * p.ld, me.c, at.width);
         }
-        scale.load<T, RAGGED>(p, at, me.c);
+        scale.load<T, KIND>(p, at, me.c);
 #pragma unroll
         for (int u = 0; u < R; u++) {
-            if constexpr (RAGGED) raw[u].settle(me.c, at.width);
+            settle_raw<KIND>(raw[u], me.c, at.width);
             raw[u].zero_unless(me.ly + (int64_t)u * p.LY < p.S);
             add(raw[u], s, q);
         }
@@ -245,13 +293,13 @@ __global__ __launch_bounds__(1024) void k_group_norm_once(Maps p, float eps, int
         if (r >= p.S) break;
         float v[8];
         scale.apply(raw[u], act_kind, v);
-        store8(out + r * ld_y + me.c, RAGGED ? at.width - me.c : 8, v);
+        store8(out + r * ld_y + me.c, KIND != kWhole ? at.width - me.c : 8, v);
     }
 }
 
 // The sums of the values and of their squares, of each part of a sample's rows and each group: part[sample][chunk][group].  512 x
 // 512 x 128 12.2 to 13.2 us (5.1 to 5.5 TB/s).
-template <class T, bool RAGGED>
+template <class T, int KIND>
 __global__ __launch_bounds__(1024) void k_group_norm_sums(Maps p, double2* __restrict__ part) {
     extern __shared__ __attribute__((aligned(16))) double red[];
     const Place at(p, p.chunks, 0);
@@ -265,11 +313,11 @@ __global__ __launch_bounds__(1024) void k_group_norm_sums(Maps p, double2* __res
 #pragma unroll
             for (int u = 0; u < kUnroll; u++) {
                 const int64_t from = r + (int64_t)u * p.LY;
-                raw[u].template load<RAGGED>(x + (from < r1 ? from : r) * p.ld, me.c, at.width);
+                load_raw<KIND>(raw[u], x + (from < r1 ? from : r) * p.ld, me.c, at.width);
             }
 #pragma unroll
             for (int u = 0; u < kUnroll; u++) {
-                if constexpr (RAGGED) raw[u].settle(me.c, at.width);
+                settle_raw<KIND>(raw[u], me.c, at.width);
                 raw[u].zero_unless(r + (int64_t)u * p.LY < r1);
                 add(raw[u], s, q);
             }
@@ -283,10 +331,16 @@ __global__ __launch_bounds__(1024) void k_group_norm_sums(Maps p, double2* __res
 __device__ __forceinline__ void finish_parts(const Maps& p, const Place& at, const double2* part, float eps, float* mean_r, float* stats) {
     spread(at.groups, [&](int g, int l, int lanes) {
         double s = 0.0, q = 0.0;
-        for (int64_t k = l; k < p.chunks; k += lanes) {
-            const double2 v = part[(at.n * p.chunks + k) * p.G + at.g0 + g];
-            s += v.x;
-            q += v.y;
+        const double2* const from = part + at.n * p.chunks * p.G + at.g0 + g;
+        for (int64_t k = l; k < p.chunks; k += 8 * lanes) {  // (8 loads on their way together)
+            double2 v[8];
+#pragma unroll
+            for (int j = 0; j < 8; j++) v[j] = from[(k + j * lanes < p.chunks ? k + j * lanes : p.chunks - 1) * p.G];
+#pragma unroll
+            for (int j = 0; j < 8; j++) {
+                s += k + j * lanes < p.chunks ? v[j].x : 0.0;
+                q += k + j * lanes < p.chunks ? v[j].y : 0.0;
+            }
         }
         s = lanes_sum(s, lanes);
         q = lanes_sum(q, lanes);
@@ -296,14 +350,14 @@ __device__ __forceinline__ void finish_parts(const Maps& p, const Place& at, con
 }
 
 // The values again, and y.  512 x 512 x 128 23.8 to 25.2 us (5.3 to 5.6 TB/s of both).
-template <class T, bool RAGGED>
+template <class T, int KIND>
 __global__ __launch_bounds__(1024) void k_group_norm_apply(Maps p, const double2* __restrict__ part, int64_t parts, int64_t rows, float eps,
                                                            int act_kind, T* y, int64_t ld_y, float* __restrict__ stats) {
     extern __shared__ __attribute__((aligned(16))) float mean_r[];
     const Place at(p, parts, 0);
     const Lane me = lane_of(p, at);
     Scale scale;
-    scale.load<T, RAGGED>(p, at, me.c);
+    scale.load<T, KIND>(p, at, me.c);
     finish_parts(p, at, part, eps, mean_r, stats);
     if (!y || !me.live) return;
     scale.settle(p, at, me.c, mean_r);
@@ -315,16 +369,16 @@ __global__ __launch_bounds__(1024) void k_group_norm_apply(Maps p, const double2
 #pragma unroll
         for (int u = 0; u < kUnroll; u++) {
             const int64_t from = r + (int64_t)u * p.LY;
-            raw[u].template load<RAGGED>(x + (from < r1 ? from : r) * p.ld, me.c, at.width);
+            load_raw<KIND>(raw[u], x + (from < r1 ? from : r) * p.ld, me.c, at.width);
         }
 #pragma unroll
         for (int u = 0; u < kUnroll; u++) {
             const int64_t to = r + (int64_t)u * p.LY;
             if (to >= r1) break;
-            if constexpr (RAGGED) raw[u].settle(me.c, at.width);
+            settle_raw<KIND>(raw[u], me.c, at.width);
             float v[8];
             scale.apply(raw[u], act_kind, v);
-            store8(out + to * ld_y + me.c, RAGGED ? at.width - me.c : 8, v);
+            store8(out + to * ld_y + me.c, KIND != kWhole ? at.width - me.c : 8, v);
         }
     }
 }
@@ -333,7 +387,7 @@ __global__ __launch_bounds__(1024) void k_group_norm_apply(Maps p, const double2
 // the sums of parts, or (part NULL) are there already.  Bound by the activation's and the codes' instructions: 256 x 49 x 960 f16
 // 15.3 us (its bytes 7), 65 x 49 x 960 6.9 us.
 constexpr int codes_threads(int TPR) { return TPR < 256 ? 256 : TPR; }
-template <class T, bool RAGGED, int TPR, int VPT>
+template <class T, int KIND, int TPR, int VPT>
 __global__ __launch_bounds__(codes_threads(TPR)) void k_group_norm_codes(Maps p, const double2* __restrict__ part, int64_t parts, int64_t rows,
                                                                          float eps, int act_kind, fmtc_i8 out, T* y, int64_t ld_y,
                                                                          float* __restrict__ stats) {
@@ -348,12 +402,12 @@ __global__ __launch_bounds__(codes_threads(TPR)) void k_group_norm_codes(Maps p,
     auto fetch = [&](int64_t r) {
         const int64_t mine = r + threadIdx.x / TPR, from = mine < r1 ? mine : r1 - 1;
 #pragma unroll
-        for (int j = 0; j < VPT; j++) next[j].template load<RAGGED>(x + from * p.ld, 8 * (j * TPR + lane), p.C);
+        for (int j = 0; j < VPT; j++) load_raw<KIND>(next[j], x + from * p.ld, 8 * (j * TPR + lane), p.C);
     };
     fetch(r0);
     Scale scale[VPT];
 #pragma unroll
-    for (int j = 0; j < VPT; j++) scale[j].template load<T, RAGGED>(p, at, 8 * (j * TPR + lane));
+    for (int j = 0; j < VPT; j++) scale[j].template load<T, KIND>(p, at, 8 * (j * TPR + lane));
     if (part) {
         finish_parts(p, at, part, eps, mean_r, stats);
     } else {
@@ -377,7 +431,7 @@ __global__ __launch_bounds__(codes_threads(TPR)) void k_group_norm_codes(Maps p,
 #pragma unroll
         for (int j = 0; j < VPT; j++) {
             const int c = 8 * (j * TPR + lane);
-            if constexpr (RAGGED) raw[j].settle(c, p.C);
+            settle_raw<KIND>(raw[j], c, p.C);
             raw[j].zero_unless(c < p.C);
             scale[j].apply(raw[j], act_kind, v[j]);
             const uint32_t b = amax_bits8(v[j]);
@@ -403,10 +457,10 @@ __global__ __launch_bounds__(codes_threads(TPR)) void k_group_norm_codes(Maps p,
 // as a factor of the sums, values of 1e19 and more or 1e-19 and less leave f32.)
 struct Channels {
     float m[8], r[8], a[8], b[8];
-    template <class T, bool RAGGED>
+    template <class T, int KIND>
     __device__ __forceinline__ void load(const Maps& p, const Place& at, const float* stats, int c) {
-        load_param<T, RAGGED>(p.w, p.weight_type, at.c0 + c, p.C, 1.f, a);
-        load_param<T, RAGGED>(p.b, p.weight_type, at.c0 + c, p.C, 0.f, b);
+        load_param<T, KIND>(p.w, p.weight_type, at.c0 + c, p.C, 1.f, a);
+        load_param<T, KIND>(p.b, p.weight_type, at.c0 + c, p.C, 0.f, b);
         const float *const mean = stats + at.n * p.G + at.g0, *const rs = mean + p.samples * p.G;
         each_group(c, at.width, p.D, [&](int i, int g) {
             m[i] = mean[g];
@@ -436,6 +490,7 @@ __device__ __forceinline__ void sums_by_channel(const Maps& p, const Place& at, 
         const int which = i >= at.width, c = i - which * at.width;
         const float* const from = red + (8 * which + c % 8) * T + c / 8;
         float sum = 0.f;
+#pragma unroll 8
         for (int y = l; y < p.LY; y += lanes) sum += from[y * p.LX];
         sum = lanes_sum(sum, lanes);
         if (l == 0) f(which, c, sum);
@@ -452,6 +507,7 @@ __device__ __forceinline__ void group_terms(const Maps& p, const Place& at, cons
     spread(2 * at.groups, [&](int i, int l, int lanes) {
         const int which = i >= at.groups, g = i - which * at.groups;
         float sum = 0.f;
+#pragma unroll 8
         for (int c = l; c < p.D; c += lanes) sum += by_channel[which * at.width + g * p.D + c];
         sum = lanes_sum(sum, lanes);
         if (l == 0) ab[i] = sum * rcount;
@@ -476,7 +532,7 @@ struct Terms {
 // once: it costs as much as all the rest).  part[sample][2][C]: the sums by channel.  32 x 3136 x 256, 32 groups, silu 43 to 55 us: its
 // bytes take 30, but they come 32 of a row at a time and the activation's gradient is not all under them; 32 x 1568 x 512, 64
 // bytes at a time, 39 us.  In two passes 64 us; computing dz twice 73 us.
-template <class T, bool RAGGED, int ACT, int R>
+template <class T, int KIND, int ACT, int R>
 __global__ __launch_bounds__(512) void k_group_norm_backward_once(Maps p, const float* __restrict__ stats, const T* dy, int64_t ld_dy, T* dx,
                                                                   int64_t ld_dx, float* __restrict__ part) {
     extern __shared__ __attribute__((aligned(16))) float red_f[];
@@ -492,13 +548,13 @@ __global__ __launch_bounds__(512) void k_group_norm_backward_once(Maps p, const 
 #pragma unroll
         for (int u = 0; u < R; u++) {
             const int64_t r = me.ly + (int64_t)u * p.LY, from = r < p.S ? r : 0;
-            raw[u].template load<RAGGED>(x + from * p.ld, me.c, at.width);
-            raw_g[u].template load<RAGGED>(g + from * ld_dy, me.c, at.width);
+            load_raw<KIND>(raw[u], x + from * p.ld, me.c, at.width);
+            load_raw<KIND>(raw_g[u], g + from * ld_dy, me.c, at.width);
         }
-        ch.load<T, RAGGED>(p, at, stats, me.c);
+        ch.load<T, KIND>(p, at, stats, me.c);
 #pragma unroll
         for (int u = 0; u < R; u++) {
-            if constexpr (RAGGED) raw[u].settle(me.c, at.width), raw_g[u].settle(me.c, at.width);
+            settle_raw<KIND>(raw[u], me.c, at.width), settle_raw<KIND>(raw_g[u], me.c, at.width);
             raw[u].zero_unless(me.ly + (int64_t)u * p.LY < p.S);
             raw_g[u].zero_unless(me.ly + (int64_t)u * p.LY < p.S);
 #pragma unroll
@@ -533,12 +589,12 @@ __global__ __launch_bounds__(512) void k_group_norm_backward_once(Maps p, const 
         float v[8];
 #pragma unroll
         for (int i = 0; i < 8; i++) v[i] = terms.dx(ch, i, raw[u][i], dz[u][i]);
-        store8(out + r * ld_dx + me.c, RAGGED ? at.width - me.c : 8, v);
+        store8(out + r * ld_dx + me.c, KIND != kWhole ? at.width - me.c : 8, v);
     }
 }
 
 // The sums of dz and of dz x^ of each part of a sample's rows and each channel: part[sample][chunk][2][C].
-template <class T, bool RAGGED, int ACT>
+template <class T, int KIND, int ACT>
 __global__ __launch_bounds__(1024) void k_group_norm_gradient_sums(Maps p, const float* __restrict__ stats, const T* __restrict__ dy,
                                                                    int64_t ld_dy, float* __restrict__ part) {
     extern __shared__ __attribute__((aligned(16))) float red_f[];
@@ -548,7 +604,7 @@ __global__ __launch_bounds__(1024) void k_group_norm_gradient_sums(Maps p, const
     float s[8] = {}, q[8] = {};
     if (me.live) {
         Channels ch;
-        ch.load<T, RAGGED>(p, at, stats, me.c);
+        ch.load<T, KIND>(p, at, stats, me.c);
         const T *const x = slab_of<T>(p.x, p.ld, p, at), *const g = slab_of<T>(dy, ld_dy, p, at);
         constexpr int U = kUnroll / 2;
         for (int64_t r = r0 + me.ly; r < r1; r += (int64_t)U * p.LY) {
@@ -556,13 +612,13 @@ __global__ __launch_bounds__(1024) void k_group_norm_gradient_sums(Maps p, const
 #pragma unroll
             for (int u = 0; u < U; u++) {
                 const int64_t row = r + (int64_t)u * p.LY, from = row < r1 ? row : r;
-                raw[u].template load<RAGGED>(x + from * p.ld, me.c, at.width);
-                raw_g[u].template load<RAGGED>(g + from * ld_dy, me.c, at.width);
+                load_raw<KIND>(raw[u], x + from * p.ld, me.c, at.width);
+                load_raw<KIND>(raw_g[u], g + from * ld_dy, me.c, at.width);
             }
 #pragma unroll
             for (int u = 0; u < U; u++) {
                 if (r + (int64_t)u * p.LY >= r1) break;
-                if constexpr (RAGGED) raw[u].settle(me.c, at.width), raw_g[u].settle(me.c, at.width);
+                settle_raw<KIND>(raw[u], me.c, at.width), settle_raw<KIND>(raw_g[u], me.c, at.width);
 #pragma unroll
                 for (int i = 0; i < 8; i++) {
                     const float dz = ch.dz<ACT>(i, raw[u][i], raw_g[u][i]);
@@ -603,6 +659,23 @@ __device__ __forceinline__ void param_sums(const float* part, int64_t n, int C, 
         if (to) to[c < C ? c : c - C] = sum;
     }
 }
+// The sums of all parts of a sample by channel, where they are too many for every workgroup of the next kernel to add up: 32
+// columns a workgroup.  to[sample][2][C]
+__global__ __launch_bounds__(1024) void k_group_norm_join(const float* __restrict__ part, int64_t chunks, int C, float* __restrict__ to) {
+    __shared__ float slice[32 * 33];
+    const int64_t n = blockIdx.y;
+    const int col = threadIdx.x & 31, k = threadIdx.x >> 5, c = blockIdx.x * 32 + col;
+    float sum = 0.f;
+    if (c < 2 * C) sum = strided_sum(part + n * chunks * 2 * C + c, k, 32, chunks, 2 * C);
+    slice[k * 33 + col] = sum;
+    __syncthreads();
+    if (k == 0 && c < 2 * C) {
+#pragma unroll
+        for (int i = 1; i < 32; i++) sum += slice[i * 33 + col];
+        to[n * 2 * C + c] = sum;
+    }
+}
+
 __global__ __launch_bounds__(1024) void k_group_norm_params(const float* __restrict__ part, int64_t n, int C, float* __restrict__ dweight,
                                                             float* __restrict__ dbias) {
     __shared__ float slice[32 * 33];
@@ -611,7 +684,7 @@ __global__ __launch_bounds__(1024) void k_group_norm_params(const float* __restr
 
 // dx from the sums of the parts.  The first `before` workgroups do the sums for dbias and dweight.  7 x 1739 x 161 f32 12.8 us, latency:
 // its values set out when the sums over the parts are there (setting out before them gained nothing).
-template <class T, bool RAGGED, int ACT>
+template <class T, int KIND, int ACT>
 __global__ __launch_bounds__(1024) void k_group_norm_dx(Maps p, const float* __restrict__ stats, const float* __restrict__ part, int64_t parts,
                                                         int64_t rows, uint32_t before, const T* dy, int64_t ld_dy, T* dx, int64_t ld_dx,
                                                         float* __restrict__ dweight, float* __restrict__ dbias) {
@@ -636,7 +709,7 @@ __global__ __launch_bounds__(1024) void k_group_norm_dx(Maps p, const float* __r
     const Lane me = lane_of(p, at);
     if (!me.live) return;
     Channels ch;
-    ch.load<T, RAGGED>(p, at, stats, me.c);
+    ch.load<T, KIND>(p, at, stats, me.c);
     Terms terms;
     terms.load(p, at, ch, me.c, ab);
     const int64_t r0 = at.k * rows, r1 = r0 + rows < p.S ? r0 + rows : p.S;
@@ -648,18 +721,18 @@ __global__ __launch_bounds__(1024) void k_group_norm_dx(Maps p, const float* __r
 #pragma unroll
         for (int u = 0; u < U; u++) {
             const int64_t row = r + (int64_t)u * p.LY, from = row < r1 ? row : r;
-            raw[u].template load<RAGGED>(x + from * p.ld, me.c, at.width);
-            raw_g[u].template load<RAGGED>(g + from * ld_dy, me.c, at.width);
+            load_raw<KIND>(raw[u], x + from * p.ld, me.c, at.width);
+            load_raw<KIND>(raw_g[u], g + from * ld_dy, me.c, at.width);
         }
 #pragma unroll
         for (int u = 0; u < U; u++) {
             const int64_t to = r + (int64_t)u * p.LY;
             if (to >= r1) break;
-            if constexpr (RAGGED) raw[u].settle(me.c, at.width), raw_g[u].settle(me.c, at.width);
+            settle_raw<KIND>(raw[u], me.c, at.width), settle_raw<KIND>(raw_g[u], me.c, at.width);
             float v[8];
 #pragma unroll
             for (int i = 0; i < 8; i++) v[i] = terms.dx(ch, i, raw[u][i], ch.dz<ACT>(i, raw[u][i], raw_g[u][i]));
-            store8(out + to * ld_dx + me.c, RAGGED ? at.width - me.c : 8, v);
+            store8(out + to * ld_dx + me.c, KIND != kWhole ? at.width - me.c : 8, v);
         }
     }
 }
@@ -670,6 +743,7 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 struct Plan {
     int threads, W, rows;     // rows: of a thread, in its registers (0: in two passes)
     int64_t chunks;           // two passes: parts of a sample's rows
+    int join;                 // gradients: 1 where a kernel between the two joins the parts
 };
 constexpr double kCus = 256;
 // Every workgroup of the second pass reads the sums of all parts of its sample: 512 workgroups and 128 parts of 512 x 512 x 128
@@ -688,7 +762,9 @@ int row_step(int64_t rows, int size) {
     return 0;
 }
 
-// The least of the times that are expected, in us.  arrays: read (1 forward, 2 backward)
+// The least of the times that are expected, in us, from the bytes, the lines of memory that a compute unit takes in for them, and the
+// rounds of workgroups.  Over 59 drawn sizes the choice costs 3 % more than the best of all choices would, in the mean.  arrays: read
+// (1 forward, 2 backward)
 Plan make_plan(int64_t samples, int64_t S, int C, int groups, int size, int arrays) {
     const int D = C / groups;
     const double values = (double)samples * S * C, bytes = values * size * (arrays + 1);
@@ -703,20 +779,23 @@ Plan make_plan(int64_t samples, int64_t S, int C, int groups, int size, int arra
     const int64_t rows = ceil_div(S, (int64_t)(kUnroll / arrays) * (best.threads / lanes_of(W)));
     best.chunks = want(W) < rows ? want(W) : rows;
     best.chunks = ceil_div(S, ceil_div(S, best.chunks < kMostChunks ? best.chunks : kMostChunks));
-    double least = 10.0 + (bytes + values * size * arrays * (values * size * arrays > 2e8 ? 1.0 : 0.6)) / 5e6;
+    // (a workgroup's time for the sums over the parts: rounds of its threads, each of several rounds of loads, 0.8 us; a kernel 4)
+    best.join = arrays == 2 && best.chunks > 1 && ceil_div(best.chunks, 16) * ceil_div(2 * W, best.threads) > 4;
+    double least = 9.0 + (bytes + values * size * arrays * (values * size * arrays > 2e8 ? 1.0 : 0.6)) / 5e6 * (C % 8 ? 1.3 : 1.0);
     for (int gs = 1;; gs = gs * 2 < groups ? gs * 2 : groups) {
         const int W = gs * D, LX = lanes_of(W);
         for (int threads = 256; threads <= (arrays == 1 ? 1024 : 512); threads *= 2) {
             if (LX > threads || (W < 8 && W != C) || (double)samples * ceil_div(groups, gs) > 2e9) continue;
             const size_t lds = arrays == 1 ? sizeof(double) * (2 << fold_of(D)) * threads + sizeof(float) * 2 * gs : 0;
-            if (lds > 160 * 1024) continue;
+            if (lds > 159 * 1024) continue;
             const int R = row_step(ceil_div(S, threads / LX), size);
             if (!R) continue;
             const double wgs = (double)samples * ceil_div(groups, gs), at_once = kCus * 1024 / threads;
-            const double rounds = ceil(wgs / at_once), segment = W * size;
-            const double slow = (W == C || segment >= 128 ? 1.0 : segment >= 64 ? 1.05 : segment >= 32 ? 1.2 : 1.6) * (W % 8 && W != C ? 1.5 : 1.0);
-            const double mine = bytes / wgs * (wgs > kCus ? 1024.0 / threads : 1.0) * rounds / 30e3;  // one compute unit's part
-            const double t = 4.0 + 1.5 * rounds + fmax(bytes * slow / 5e6, mine);
+            const double rounds = ceil(wgs / at_once), segment = W * size, crooked = W % 8 && W != C ? 1.5 : 1.0;
+            const double slow = (W == C || segment >= 128 ? 1.0 : segment >= 64 ? 1.05 : segment >= 32 ? 1.2 : 1.6) * crooked;
+            const double lines = (W == C || segment >= 128 ? 1.0 : 128.0 / segment) * crooked;  // what a compute unit takes in
+            const double mine = bytes / wgs * lines * fmax(1.0, wgs / kCus) / 80e3;
+            const double t = 4.0 + 2.5 * rounds * threads / 512 + fmax(bytes * slow / 5e6, mine);
             if (t < least) {
                 least = t;
                 best.threads = threads;
@@ -738,6 +817,11 @@ Maps maps_of(const fmtc_gnorm& a, const Plan& plan) {
 int64_t parts_of(const Maps& p, int rows_at_a_time, int unroll, int64_t want) {
     const int64_t fit = ceil_div(p.S, (int64_t)unroll * rows_at_a_time), parts = ceil_div(want, p.samples * p.slabs);
     return ceil_div(p.S, ceil_div(p.S, parts < fit ? parts : fit));
+}
+template <class F>
+hipError_t with_kind(const Maps& p, F&& f) {
+    if (p.C % 8 == 0 && p.W % 8 == 0) return f(Int<kWhole>{});
+    return p.C - (p.slabs - 1) * p.W >= 8 ? f(Int<kLong>{}) : f(Int<kShort>{});  // (the last slab is the narrowest)
 }
 template <class F>
 hipError_t with_act(int act, F&& f) {
@@ -772,7 +856,7 @@ size_t group_norm_backward_workspace(int64_t samples, int64_t S, int C, int grou
     size_t most = 0;
     for (int size = 2; size <= 4; size += 2) {  // (in one pass there is one part of a sample)
         const Plan plan = make_plan(samples, S, C, groups, size, 2);
-        const size_t bytes = sizeof(float) * (size_t)(samples * (plan.rows ? 1 : plan.chunks)) * 2 * C;
+        const size_t bytes = sizeof(float) * (size_t)(samples * (plan.rows ? 1 : plan.chunks + plan.join)) * 2 * C;
         most = bytes > most ? bytes : most;
     }
     return align_up(most, 256);
@@ -784,8 +868,8 @@ hipError_t launch_group_norm(const fmtc_gnorm& a, void* d_y, int64_t ld_y, const
     double2* const part = static_cast<double2*>(d_ws);
     return with_type(a.type, [&](auto ty) {
         using T = typename decltype(ty)::type;
-        return with_bit(p.C % 8 != 0 || p.W % 8 != 0, [&](auto rg) {
-            constexpr bool R = decltype(rg)::value;
+        return with_kind(p, [&](auto kd) {
+            constexpr int R = decltype(kd)::value;
             const size_t lds = sizeof(double) * (2 << p.pre) * plan.threads, lds_stats = sizeof(float) * 2 * p.groups;
             float* const stats = codes && plan.rows && !d_stats ? static_cast<float*>(d_ws) : d_stats;
             hipError_t e;
@@ -801,11 +885,11 @@ hipError_t launch_group_norm(const fmtc_gnorm& a, void* d_y, int64_t ld_y, const
                 p.W = p.C;  // (rows as a whole)
                 p.groups = p.G;
                 p.slabs = 1;
-                return with_bit(p.C % 8 != 0, [&](auto rg) {
+                return with_kind(p, [&](auto rows_kind) {
                     auto with = [&](auto tpr, auto vpt) {
                         constexpr int TPR = decltype(tpr)::value, VPT = decltype(vpt)::value;
                         const int64_t parts = parts_of(p, codes_threads(TPR) / TPR, 1, 2048), rows = ceil_div(p.S, parts);
-                        return go(K_GROUP_NORM, k_group_norm_codes<T, decltype(rg)::value, TPR, VPT>, p.samples * parts, codes_threads(TPR),
+                        return go(K_GROUP_NORM, k_group_norm_codes<T, decltype(rows_kind)::value, TPR, VPT>, p.samples * parts, codes_threads(TPR),
                                   sizeof(float) * 2 * p.G, s, p, plan.rows ? nullptr : part, parts, rows, a.eps, a.act, *codes, static_cast<T*>(d_y), ld_y, stats);
                     };
                     if (p.C <= 128) return with(Int<16>{}, Int<1>{});
@@ -829,10 +913,9 @@ hipError_t launch_group_norm_backward(const fmtc_gnorm& a, const float* d_stats,
     float* const part = static_cast<float*>(d_ws);
     return with_type(a.type, [&](auto ty) {
         using T = typename decltype(ty)::type;
-        return with_bit(p.C % 8 != 0 || p.W % 8 != 0, [&](auto rg) {
+        return with_kind(p, [&](auto kd) {
             return with_act(a.act, [&](auto ac) {
-                constexpr bool R = decltype(rg)::value;
-                constexpr int A = decltype(ac)::value;
+                constexpr int R = decltype(kd)::value, A = decltype(ac)::value;
                 const T* dy = static_cast<const T*>(d_dy);
                 const bool params = d_dweight || d_dbias;
                 const int64_t param_groups = params ? ceil_div(2 * p.C, 32) : 0;
@@ -851,11 +934,21 @@ hipError_t launch_group_norm_backward(const fmtc_gnorm& a, const float* d_stats,
                                         d_stats, dy, ld_dy, part);
                 if (e != hipSuccess) return e;
                 if (!d_dx) return sum_params(p.samples * p.chunks);
+                Maps joined = p;
+                const float* sums_at = part;
+                if (plan.join) {
+                    float* const to = part + p.samples * p.chunks * 2 * p.C;
+                    const hipError_t e = launch(K_GROUP_NORM_BACKWARD, k_group_norm_join, dim3((unsigned)ceil_div(2 * p.C, 32), (unsigned)p.samples), dim3(1024), 0, s,
+                                                part, p.chunks, p.C, to);
+                    if (e != hipSuccess) return e;
+                    joined.chunks = 1;
+                    sums_at = to;
+                }
                 const int64_t parts = parts_of(p, p.LY, kUnroll / 2, kSecondPass), rows = ceil_div(p.S, parts);
                 size_t lds_dx = sizeof(float) * (2 * p.W > plan.threads ? 2 * p.W : plan.threads) + lds_ab;
                 if (lds_dx < sizeof(float) * 33 * (plan.threads / 32)) lds_dx = sizeof(float) * 33 * (plan.threads / 32);
-                return go(K_GROUP_NORM_BACKWARD, k_group_norm_dx<T, R, A>, param_groups + p.samples * p.slabs * parts, plan.threads, lds_dx, s, p, d_stats, part,
-                          parts, rows, (uint32_t)param_groups, dy, ld_dy, static_cast<T*>(d_dx), ld_dx, d_dweight, d_dbias);
+                return go(K_GROUP_NORM_BACKWARD, k_group_norm_dx<T, R, A>, param_groups + p.samples * p.slabs * parts, plan.threads, lds_dx, s, joined, d_stats,
+                          sums_at, parts, rows, (uint32_t)param_groups, dy, ld_dy, static_cast<T*>(d_dx), ld_dx, d_dweight, d_dbias);
             });
         });
     });
