@@ -158,7 +158,7 @@ __device__ __forceinline__ void sums_by_group(const Maps& p, const Place& at, bo
         }
     };
     // Few groups: several wavefronts for each, whose sums meet in LDS again (2 x 16 x 448, one group of 14 channels a workgroup of
-    // 1024: 15.8 us with one wavefront, 11 with four or more).
+    // 1024: 15.8 us with one wavefront, 9.4 with sixteen).
     const int waves = T / 64;
     if (2 * at.groups <= waves) {
         __shared__ double few[2][16];
