@@ -48,7 +48,7 @@ __device__ __forceinline__ int quotient(int i, float r) { return (int)(((float)i
 // How the rows of a slab lie: multiples of 8 channels at multiples of 8; 8 channels or more; any number of them.  (The question
 // whether there are 8, asked at each load, holds the loads apart: sums of 41 x 1716 x
 // 522 40.8 -> 35.0 us, gradient sums of 2 x 18281 x 435 21.0 -> 18.4 us; rows that begin at multiples of 16 bytes: 17.8 and 15.8.)
-enum Kind { kWhole = 0, kLong = 1, kShort = 2 };
+enum Kind { kWhole = 0, kLong = 1, kShort = 2 };  // (of the narrowest slab)
 template <int KIND, class T>
 __device__ __forceinline__ void load_raw(Raw<T>& raw, const T* row, int64_t c, int64_t C) {
     if constexpr (KIND == kLong) raw.load_long(row, c, C);
@@ -56,13 +56,13 @@ __device__ __forceinline__ void load_raw(Raw<T>& raw, const T* row, int64_t c, i
 }
 template <int KIND, class T>
 __device__ __forceinline__ void settle_raw(Raw<T>& raw, int64_t c, int64_t C) {
-    if constexpr (KIND == kLong) raw.settle(c, C);  // (short rows are loaded value by value, with zeros behind them)
+    if constexpr (KIND != kWhole) raw.settle(c, C);  // (rows of fewer than 8 are loaded value by value, with zeros behind them)
 }
 template <int KIND, class T>
 __device__ __forceinline__ void load_values(const T* row, int64_t c, int64_t C, float (&v)[8]) {
     Raw<T> raw;
     load_raw<KIND>(raw, row, c, C);
-    if constexpr (KIND != kWhole) raw.settle(c, C);
+    settle_raw<KIND>(raw, c, C);
 #pragma unroll
     for (int i = 0; i < 8; i++) v[i] = raw[i];
 }

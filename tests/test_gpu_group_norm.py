@@ -11,7 +11,10 @@ TYPES = [torch.bfloat16, torch.float16, torch.float32]
 # samples, rows, channels, groups
 SIZES = [(1, 1, 1, 1), (1, 1, 8, 1), (3, 1, 64, 2), (2, 5, 7, 7), (1, 196, 256, 32), (2, 49, 960, 32), (3, 17, 161, 7), (2, 3, 24, 3), (1, 700, 3, 1),
          (5, 64, 64, 32), (1, 3000, 128, 32), (2, 9, 2048, 32), (2, 4, 2049, 1), (1, 3, 8192, 8192), (1, 5, 8192, 1), (1, 2, 5001, 3), (70, 1, 96, 4),
-         (300, 2, 40, 5), (2, 1739, 161, 7), (1, 40000, 16, 4), (2, 333, 520, 1), (4, 784, 128, 128), (3, 1025, 64, 1), (1, 2100, 960, 30)]
+         (300, 2, 40, 5), (2, 1739, 161, 7), (1, 40000, 16, 4), (2, 333, 520, 1), (4, 784, 128, 128), (3, 1025, 64, 1), (1, 2100, 960, 30),
+         (1, 5, 15, 5), (3, 40, 27, 9), (2, 300, 33, 11), (1, 3400, 27, 9), (40, 600, 21, 7), (16, 4505, 40, 4), (10, 1364, 1416, 4), (2, 16, 448, 32),
+         # slabs of groups that are not multiples of 8, the last of them narrower than 8
+         (5, 158, 91, 13), (5, 556, 126, 21), (2, 654, 18, 6), (100, 2154, 25, 5), (1, 7, 245, 35), (20, 1191, 198, 33)]
 
 
 def _values(samples, rows, C, dtype, seed=0, offset=1.0):
