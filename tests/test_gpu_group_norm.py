@@ -34,8 +34,10 @@ def _close(got, want, bound):
 
 
 def _check_stats(stats, want):
-    for got, w in zip(stats.double(), want):
-        assert bool(((got - w).abs() <= ref.U * w.abs() * 1.01 + 1e-12 * want[0].abs().max()).all())
+    """Both are sums in f64, rounded once (U); r = (variance + eps)^-1/2 has eps as f32 holds it, off by U of it at most, which is
+    half that of r where there is no variance: 128 samples of two equal values have it all."""
+    for got, w, share in zip(stats.double(), want, (1.01, 1.51)):
+        assert bool(((got - w).abs() <= share * ref.U * w.abs() + 1e-12 * want[0].abs().max()).all())
 
 
 @pytest.mark.parametrize("act", ref.ACTS)
