@@ -485,7 +485,7 @@ fmtc_status fmtc_group_norm(const fmtc_gnorm *args, void *d_y, int64_t ld_y, con
  * read): d_dx (may be d_dy or d_x itself with the same row stride), d_dweight and d_dbias [C] in f32,
  * any may be NULL.  The gradient of max(z, 0) at 0 is 0.  Sums over rows are in a fixed
  * order; without rows d_dweight and d_dbias are 0. */
-size_t fmtc_group_norm_backward_workspace_size(int64_t samples, int64_t rows_per_sample, int C, int groups);
+size_t fmtc_group_norm_backward_workspace_size(int64_t samples, int64_t rows_per_sample, int C, int groups, fmtc_dtype type);
 fmtc_status fmtc_group_norm_backward(const fmtc_gnorm *args, const float *d_stats, const void *d_dy, int64_t ld_dy,
                                      void *d_dx, int64_t ld_dx, float *d_dweight, float *d_dbias, void *d_workspace,
                                      size_t ws_bytes, void *hip_stream);

@@ -164,7 +164,7 @@ def load_library():
     lib.fmtc_i8_linear.argtypes = [vp, i32, i64, i64, i8, vp, vp, i32, i64, vp, sz, vp]
     lib.fmtc_group_norm_workspace_size.argtypes = [i64, i64, i32, i32, i32, i32]
     lib.fmtc_group_norm_workspace_size.restype = sz
-    lib.fmtc_group_norm_backward_workspace_size.argtypes = [i64, i64, i32, i32]
+    lib.fmtc_group_norm_backward_workspace_size.argtypes = [i64, i64, i32, i32, i32]
     lib.fmtc_group_norm_backward_workspace_size.restype = sz
     lib.fmtc_group_norm.argtypes = [gnorm, vp, i64, i8, vp, vp, sz, vp]
     lib.fmtc_group_norm_backward.argtypes = [gnorm, vp, vp, i64, vp, i64, vp, vp, vp, sz, vp]
@@ -1119,7 +1119,7 @@ def group_norm(x, groups, weight=None, bias=None, rows_per_sample=0, act=ACT_NON
     else:
         y_ptr, _, y_ld = _rows(out, "out", C, P, x.dtype)
     if stats is True:
-        stats = torch.empty((2, a.samples, groups), dtype=torch.float32, device=x.device)
+        stats = torch.empty_strided((2, a.samples, groups), (a.samples * groups, groups, 1), dtype=torch.float32, device=x.device)
     elif stats is False:
         stats = None
     _on_current("group_norm", x, weight, bias, codes._codes if codes is not None else out, stats, workspace)
@@ -1130,9 +1130,12 @@ def group_norm(x, groups, weight=None, bias=None, rows_per_sample=0, act=ACT_NON
     return out, stats
 
 
-def group_norm_backward_workspace_size(P, C, groups, rows_per_sample=0):
+def group_norm_backward_workspace_size(P, C, groups, rows_per_sample=0, dtype=None):
+    """Bytes for group_norm_backward of values of `dtype` (bf16 unless given)."""
+    import torch
+
     rows = rows_per_sample or P
-    return load_library().fmtc_group_norm_backward_workspace_size(P // rows if rows else 0, rows, C, groups)
+    return load_library().fmtc_group_norm_backward_workspace_size(P // rows if rows else 0, rows, C, groups, _dtype(dtype or torch.bfloat16))
 
 
 def group_norm_backward(dy, x, stats, groups, weight=None, bias=None, rows_per_sample=0, act=ACT_NONE, dx=None, workspace=None):
@@ -1156,7 +1159,7 @@ def group_norm_backward(dy, x, stats, groups, weight=None, bias=None, rows_per_s
     _on_current("group_norm_backward", dy, x, stats, weight, bias, dx, workspace)
     s_ptr = _vector(stats, "stats", 2 * a.samples * groups, torch.float32)
     lib = load_library()
-    workspace, ws, size = _workspace(workspace, lib.fmtc_group_norm_backward_workspace_size(a.samples, a.rows_per_sample, C, groups), x.device)
+    workspace, ws, size = _workspace(workspace, lib.fmtc_group_norm_backward_workspace_size(a.samples, a.rows_per_sample, C, groups, a.type), x.device)
     _check(lib.fmtc_group_norm_backward(ctypes.byref(a), s_ptr, dy_ptr, dy_ld, dx_ptr, dx_ld,
                                         None if dweight is None else dweight.data_ptr(), None if dbias is None else dbias.data_ptr(),
                                         ws, size, _stream()))

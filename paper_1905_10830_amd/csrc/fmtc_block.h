@@ -47,7 +47,7 @@ hipError_t launch_i8_linear_one(const void* d_x, int type, int64_t rows, int64_t
 size_t group_norm_workspace(int64_t samples, int64_t rows, int C, int groups, int type, bool to_codes);
 hipError_t launch_group_norm(const fmtc_gnorm& a, void* d_y, int64_t ld_y, const fmtc_i8* codes, float* d_stats, void* d_ws,
                              hipStream_t s);
-size_t group_norm_backward_workspace(int64_t samples, int64_t rows, int C, int groups);
+size_t group_norm_backward_workspace(int64_t samples, int64_t rows, int C, int groups, int type);
 hipError_t launch_group_norm_backward(const fmtc_gnorm& a, const float* d_stats, const void* d_dy, int64_t ld_dy, void* d_dx,
                                       int64_t ld_dx, float* d_dweight, float* d_dbias, void* d_ws, hipStream_t s);
 

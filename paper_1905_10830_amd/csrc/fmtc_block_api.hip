@@ -423,8 +423,8 @@ fmtc_status fmtc_group_norm(const fmtc_gnorm* args, void* d_y, int64_t ld_y, con
     return hip_status(launch_group_norm(*args, d_y, ld_y, codes, d_stats, d_workspace, (hipStream_t)hip_stream), who);
 }
 
-size_t fmtc_group_norm_backward_workspace_size(int64_t samples, int64_t rows_per_sample, int C, int groups) {
-    return gnorm_size_ok(samples, rows_per_sample, C, groups) ? group_norm_backward_workspace(samples, rows_per_sample, C, groups) : 0;
+size_t fmtc_group_norm_backward_workspace_size(int64_t samples, int64_t rows_per_sample, int C, int groups, fmtc_dtype type) {
+    return gnorm_size_ok(samples, rows_per_sample, C, groups) && dtype_ok(type) ? group_norm_backward_workspace(samples, rows_per_sample, C, groups, type) : 0;
 }
 
 fmtc_status fmtc_group_norm_backward(const fmtc_gnorm* args, const float* d_stats, const void* d_dy, int64_t ld_dy, void* d_dx,
@@ -450,7 +450,7 @@ fmtc_status fmtc_group_norm_backward(const fmtc_gnorm* args, const float* d_stat
         CHECK(check_in_place(who, "dx", d_dx, ld_dx, "x", args->d_x, args->ld_x));
         CHECK(check_in_place(who, "dx", d_dx, ld_dx, "dy", d_dy, ld_dy));
     }
-    CHECK(check_workspace(who, d_workspace, ws_bytes, group_norm_backward_workspace(args->samples, args->rows_per_sample, args->C, args->groups)));
+    CHECK(check_workspace(who, d_workspace, ws_bytes, group_norm_backward_workspace(args->samples, args->rows_per_sample, args->C, args->groups, args->type)));
     return hip_status(launch_group_norm_backward(*args, d_stats, d_dy, ld_dy, d_dx, ld_dx, d_dweight, d_dbias, d_workspace, s), who);
 }
 

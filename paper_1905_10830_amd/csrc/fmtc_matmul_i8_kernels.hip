@@ -482,7 +482,7 @@ struct Plan { int kernel, splits; int64_t split_blocks; };
 enum { kRows = 0, kTiles128 = 1, kTiles256 = 2, kTiles128Deep = 3 };
 constexpr double kCus = 256;
 
-Plan make_plan(int64_t M, int64_t N, int64_t K) {
+Plan choose(int64_t M, int64_t N, int64_t K) {
     const int64_t blocks = (K + kBlock - 1) / kBlock;
     Plan best{kRows, 1, blocks};
     if (M <= 16) return best;
@@ -506,6 +506,14 @@ Plan make_plan(int64_t M, int64_t N, int64_t K) {
             }
         }
     return best;
+}
+
+// A call asks three times for the same sizes (for its workspace, for the check of it, for the launch).
+Plan make_plan(int64_t M, int64_t N, int64_t K) {
+    struct Last { int64_t M, N, K; Plan plan; };
+    static thread_local Last last{};
+    if (last.M != M || last.N != N || last.K != K) last = {M, N, K, choose(M, N, K)};
+    return last.plan;
 }
 
 int64_t split_ld(int64_t N) { return (N + 3) / 4 * 4; }

@@ -70,7 +70,7 @@ def test_workspaces(lib, kind):
                        (lib.fmtc_i8_linear_workspace_size(M, N, K), lambda ws, n: lib.fmtc_i8_linear(SOME, kind, M, K, b, None, SOME, kind, N, ws, n, None)),
                        (lib.fmtc_group_norm_workspace_size(1, 100000, 64, 8, kind, 0), lambda ws, n: lib.fmtc_group_norm(_norm(samples=1, rows_per_sample=100000, C=64, type=kind), SOME, 64, None, None, ws, n, None)),
                        (lib.fmtc_group_norm_workspace_size(2, 50, 64, 8, kind, 1), lambda ws, n: lib.fmtc_group_norm(_norm(samples=2, rows_per_sample=50, C=64, type=kind), None, 0, _i8(rows=100, depth=64, ld=128), None, ws, n, None)),
-                       (lib.fmtc_group_norm_backward_workspace_size(2, 50, 64, 8), lambda ws, n: lib.fmtc_group_norm_backward(_norm(samples=2, rows_per_sample=50, C=64, type=kind), SOME, SOME, 64, SOME + 4096, 64, None, None, ws, n, None))):
+                       (lib.fmtc_group_norm_backward_workspace_size(2, 50, 64, 8, kind), lambda ws, n: lib.fmtc_group_norm_backward(_norm(samples=2, rows_per_sample=50, C=64, type=kind), SOME, SOME, 64, SOME + 4096, 64, None, None, ws, n, None))):
         assert size > 0
         for ws, n, want in ((SOME, size - 1, fmtc.EBUFSIZE), (SOME, 0, fmtc.EBUFSIZE), (SOME + 1, size, fmtc.EINVAL), (SOME + 128, size, fmtc.EINVAL), (None, size, fmtc.EINVAL)):
             _refused(lib, call(ws, n), "workspace", want)
@@ -145,8 +145,8 @@ def test_norm_outputs(lib):
     _refused(lib, back(dw=SOME + 2), "dweight")
     _refused(lib, back(db=SOME + 2), "dbias")
     for sizes in ((0, 4, 8, 8), (4, 0, 8, 8), (4, 4, 0, 1), (4, 4, 8, 3), (4, 4, 8, 0), (1 << 20, 1 << 20, 8, 8), (4, 4, 8200, 8)):
-        assert lib.fmtc_group_norm_workspace_size(*sizes, fmtc.F32, 1) == 0 and lib.fmtc_group_norm_backward_workspace_size(*sizes) == 0
-    assert lib.fmtc_group_norm_workspace_size(4, 4, 8, 8, 7, 1) == 0
+        assert lib.fmtc_group_norm_workspace_size(*sizes, fmtc.F32, 1) == 0 and lib.fmtc_group_norm_backward_workspace_size(*sizes, fmtc.F32) == 0
+    assert lib.fmtc_group_norm_workspace_size(4, 4, 8, 8, 7, 1) == 0 and lib.fmtc_group_norm_backward_workspace_size(4, 4, 8, 8, 7) == 0
 
 
 def _list(*entries):
