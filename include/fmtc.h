@@ -497,8 +497,8 @@ fmtc_status fmtc_group_norm_backward(const fmtc_gnorm *args, const float *d_stat
  *     out  = in * f,  f = scale * min(1, max_norm / (norm + eps))              (f rounded to f32, then the product)
  * d_out may be d_in itself (with out_type = type); otherwise no array that is
  * written may overlap another one of the list.  d_out NULL in all entries: the norm only (max_norm and eps are not
- * read).  d_norm: f32 [1], may be NULL.  An infinite norm makes f 0, a norm that is not a
- * number makes all outputs not a number.  scale >= 0, max_norm >= 0, eps >= 0, finite (max_norm: or infinite).  Workspace:
+ * read).  d_norm: f32 [1], may be NULL.  An infinite norm makes f 0, whatever max_norm is; where
+ * norm + eps is 0, f is scale; a norm that is not a number makes all outputs not a number.  scale >= 0, max_norm >= 0, eps >= 0, finite (max_norm: or infinite).  Workspace:
  * 256-byte aligned.  Results do not depend on the run. */
 typedef struct fmtc_tensor {
     const void *d_in;

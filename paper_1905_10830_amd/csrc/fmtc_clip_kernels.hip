@@ -138,7 +138,8 @@ __global__ __launch_bounds__(kThreads) void k_clip_scale(List a, const double* _
     const double norm = scale * sqrt(block_sum(s, part));
     if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
     if (blockIdx.x >= a.pieces) return;
-    const double r = max_norm / (norm + eps);
+    // 0 for an infinite norm, whatever max_norm is; 1 where norm + eps is 0 (values of 0, or a scale of 0): not inf / inf and 0 / 0
+    const double most = norm + eps, r = most == 0.0 ? 1.0 : __builtin_isinf(norm) ? 0.0 : max_norm / most;
     const float f = (float)(scale * (r > 1.0 ? 1.0 : r));  // (not a number stays that)
     const uint32_t piece = a.pieces - 1 - blockIdx.x;
     const int k = find(a, piece);

@@ -84,6 +84,29 @@ def test_infinities_and_nan():
     assert math.isnan(float(handle.clip(1.0))) and bool(torch.isnan(torch.cat(outs)).all())
 
 
+@pytest.mark.parametrize("max_norm", [1.0, 0.0, 1e300, math.inf])
+def test_an_infinite_norm_makes_the_factor_0(max_norm):
+    """0 times what is finite, whatever the norm may be at most; only the infinite value itself is not a number then"""
+    t = torch.tensor([1.0, math.inf, -2.0] + [3.0] * 3000, device="cuda")
+    for tensors in ([t.clone()], [t.clone(), torch.ones(5, device="cuda").bfloat16()]):
+        assert float(fmtc.Tensors(tensors).clip(max_norm)) == math.inf
+        flat = torch.cat([v.float() for v in tensors])
+        assert bool(torch.isnan(flat[1])) and int(torch.isnan(flat).sum()) == 1 and not bool(flat.nan_to_num(0.0).any())
+
+
+@pytest.mark.parametrize("max_norm", [0.0, 1.0, math.inf])
+@pytest.mark.parametrize("scale", [1.0, 0.0, 0.5])
+def test_values_of_0_stay_0_without_eps(max_norm, scale):
+    tensors = [torch.zeros(3000, device="cuda"), torch.zeros(7, device="cuda").bfloat16()]
+    outs = [torch.full_like(t, 9.0) for t in tensors]
+    assert float(fmtc.Tensors(tensors, out=outs).clip(max_norm, scale=scale, eps=0.0)) == 0.0
+    assert not any(bool(o.any()) for o in outs)
+    if scale == 0.0:  # a norm of 0 of other values: the factor is the scale
+        tensors[0].fill_(2.0)
+        assert float(fmtc.Tensors(tensors, out=outs).clip(max_norm, scale=scale, eps=0.0)) == 0.0
+        assert not any(bool(o.any()) for o in outs)
+
+
 def test_nothing():
     for tensors in ([], [torch.empty(0, device="cuda")]):
         handle = fmtc.Tensors(tensors)
