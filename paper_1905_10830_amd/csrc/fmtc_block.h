@@ -238,7 +238,8 @@ __device__ __forceinline__ float i8_row_scale(uint32_t amax_bits, float* held) {
     return finite ? 1.f / s : 0.f;
 }
 // four codes, the first in the lowest byte.  The product is rounded before the sum rounds it to a whole number (of up to
-// 127, in the sum's lowest byte); a row that is not finite has factor 0, and its NaN become 0 here.
+// 127, in the sum's lowest byte).  A row that is not finite has factor 0, and codes 0 by the question for that: a NaN keeps its
+// payload through product and sum, whose lowest byte would be the code.
 __device__ __forceinline__ uint32_t i8_encode4(const float* v, float inv) {
 #pragma clang fp contract(off)
     uint32_t q[4];
@@ -248,7 +249,7 @@ __device__ __forceinline__ uint32_t i8_encode4(const float* v, float inv) {
         q[i] = __float_as_uint(t + 0x1.8p23f);
     }
     const uint32_t lo = __builtin_amdgcn_perm(q[1], q[0], 0x0c0c0400u), hi = __builtin_amdgcn_perm(q[3], q[2], 0x04000c0cu);
-    return lo | hi;
+    return inv == 0.f ? 0u : lo | hi;
 }
 __device__ __forceinline__ uint32_t amax_bits8(const float (&v)[8]) {
     uint32_t m = 0;

@@ -74,6 +74,35 @@ def test_codes_at_the_ends_of_the_range():
     assert torch.equal(torch.isnan(y).all(1), torch.isnan(q.scales)) and torch.equal(torch.isnan(y).any(1), torch.isnan(q.scales))
 
 
+@pytest.mark.parametrize("cols", [4, 130, 960, 2048, 4100, 17000])
+def test_codes_of_any_nan_are_0(cols):
+    """NaN of any sign and payload, quiet and not: a row's codes are 0 and its scale is not a number, the others as they are."""
+    x = _values(5, cols, torch.float32)
+    want, scales = ref.codes(x)
+    payloads = torch.tensor([0x7fc00001, 0x7f800001, 0x7f8000ff, 0x7fffffff, -1, -0x3fffff, -0x7fff81], dtype=torch.int64, device="cuda")
+    bits = x.view(torch.int32)
+    for row in (1, 3):
+        at = torch.arange(row % 2, cols, 2, device="cuda")
+        bits[row, at] = payloads[at % len(payloads)].to(torch.int32)
+    assert bool(torch.isnan(x[1]).any()) and bool(torch.isnan(x[3]).any())
+    q = fmtc.i8_quantize(x)
+    assert not bool(q.codes[1].any()) and not bool(q.codes[3].any())
+    assert bool(torch.isnan(q.scales[[1, 3]]).all())
+    for row in (0, 2, 4):
+        assert torch.equal(q.codes[row], ref.pad(want)[row]) and bool(q.scales[row] == scales[row])
+    y = fmtc.i8_linear(x, fmtc.i8_quantize(_values(40, cols, torch.float32, 1)))
+    assert torch.equal(torch.isnan(y).all(1), torch.isnan(q.scales)) and torch.equal(torch.isnan(y).any(1), torch.isnan(q.scales))
+
+
+@pytest.mark.parametrize("dtype, bad", [(torch.bfloat16, 0x7f81), (torch.bfloat16, -1), (torch.float16, 0x7c01), (torch.float16, 0x7fff)])
+def test_codes_of_any_nan_of_16_bits_are_0(dtype, bad):
+    x = _values(3, 300, dtype)
+    x.view(torch.int16)[1, ::3] = bad
+    assert bool(torch.isnan(x[1]).any())
+    q = fmtc.i8_quantize(x)
+    assert not bool(q.codes[1].any()) and torch.equal(torch.isnan(q.scales), torch.tensor([False, True, False], device="cuda"))
+
+
 SIZES = [(1, 1, 1), (1, 17, 130), (2, 33, 129), (7, 100, 1000), (16, 1000, 1111), (17, 1, 8), (17, 24, 1024), (31, 513, 65), (64, 64, 64), (65, 129, 257),
          (100, 4096, 300), (128, 128, 4096), (130, 77, 9000), (255, 257, 127), (257, 255, 1025), (513, 1000, 960), (1000, 2050, 384), (2049, 1027, 130),
          (20, 513, 4200), (300, 300, 12000), (1, 5000, 8192), (1100, 1300, 700), (2500, 2600, 259)]
