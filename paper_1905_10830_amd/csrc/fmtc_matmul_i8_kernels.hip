@@ -103,8 +103,10 @@ __device__ __forceinline__ v4f load_four(const float* p, int64_t n, int64_t N) {
     return v;
 }
 
-// The factors one after the other: their product alone could leave f32's range.
+// The factors one after the other: their product alone could leave f32's range.  Each step rounded, as fmtc.h defines it: left to
+// itself the compiler fuses the second factor with the bias, and kernels that fused differently would differ in last bits.
 __device__ __forceinline__ v4f scaled(v4i sum, float sa, v4f sb, v4f bias) {
+#pragma clang fp contract(off)
     v4f v;
 #pragma unroll
     for (int i = 0; i < 4; i++) v[i] = (float)sum[i] * sa * sb[i] + bias[i];

@@ -124,6 +124,24 @@ def test_products(dtype, M, N, K):
     assert torch.equal(torch.where(over, got.double(), 0.0), torch.where(over, torch.sign(want) * float("inf"), 0.0))
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("biased", [False, True])
+@pytest.mark.parametrize("M, N, K", [s for s in SIZES if s[0] * s[1] < 2000000])
+def test_products_bit_for_bit(dtype, biased, M, N, K):
+    """The sum to f32, times s_a, times s_b, plus the bias, each of them rounded, then to the type of the results."""
+    qa, sa = _operand(M, K, 11)
+    qb, sb = _operand(N, K, 12)
+    sa, sb = sa * 1e-3, sb * 1e-3
+    want = (qa.double() @ qb.double().t()).float()  # (whole numbers below 2^53: exact until here)
+    want = want * sa[:, None]
+    want = want * sb
+    bias = torch.randn(N, device="cuda") * float(want.abs().median()) if biased else None
+    if biased:
+        want = want + bias
+    got = fmtc.i8_matmul(fmtc.I8(ref.pad(qa), sa, K), fmtc.I8(ref.pad(qb), sb, K), bias=bias, dtype=dtype)
+    assert torch.equal(got, want.to(dtype))
+
+
 @pytest.mark.parametrize("M", [1, 40, 700])
 def test_longest_depth_does_not_overflow(M):
     """-128 x -128, 131071 times: 2^31 - 2^14"""
