@@ -473,7 +473,7 @@ typedef struct fmtc_gnorm {
     const void *d_weight, *d_bias;
 } fmtc_gnorm;
 /* d_y (may be d_x itself with the same row stride) and codes ([samples * rows_per_sample][C], the codes of
- * fmtc_i8_quantize for y before it is rounded): one of them, or neither and
+ * fmtc_i8_quantize for y before it is rounded): one of them (not both), or neither and
  * d_stats.  d_stats: f32 [2][samples][groups], the means and r, what the backward pass needs;
  * may be NULL.  Workspace: 256-byte aligned, fmtc_group_norm_workspace_size bytes (to_codes: with `codes`; may be
  * 0: then NULL is fine). */

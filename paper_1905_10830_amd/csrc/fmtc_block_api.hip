@@ -415,6 +415,7 @@ fmtc_status fmtc_group_norm(const fmtc_gnorm* args, void* d_y, int64_t ld_y, con
     if (!aligned(d_stats, 4)) return set_error(FMTC_EINVAL, "%s: stats is not aligned to its type", who);
     if (rows == 0) return FMTC_OK;
     if (!d_y && !codes && !d_stats) return set_error(FMTC_EINVAL, "%s: no output", who);
+    if (d_y && codes) return set_error(FMTC_EINVAL, "%s: y and codes, one of them at most", who);
     if (d_y) {
         CHECK(check_values(who, "y", d_y, args->type, rows, args->C, ld_y));
         CHECK(check_in_place(who, "y", d_y, ld_y, "x", args->d_x, args->ld_x));

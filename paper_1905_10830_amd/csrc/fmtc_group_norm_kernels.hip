@@ -389,8 +389,7 @@ __global__ __launch_bounds__(1024) void k_group_norm_apply(Maps p, const double2
 constexpr int codes_threads(int TPR) { return TPR < 256 ? 256 : TPR; }
 template <class T, int KIND, int TPR, int VPT>
 __global__ __launch_bounds__(codes_threads(TPR)) void k_group_norm_codes(Maps p, const double2* __restrict__ part, int64_t parts, int64_t rows,
-                                                                         float eps, int act_kind, fmtc_i8 out, T* y, int64_t ld_y,
-                                                                         float* __restrict__ stats) {
+                                                                         float eps, int act_kind, fmtc_i8 out, float* __restrict__ stats) {
     extern __shared__ __attribute__((aligned(16))) float mean_r[];
     __shared__ uint32_t turns[2][codes_threads(TPR) / 64];
     constexpr int kRows = codes_threads(TPR) / TPR;
@@ -446,7 +445,6 @@ __global__ __launch_bounds__(codes_threads(TPR)) void k_group_norm_codes(Maps p,
             const int c = 8 * (j * TPR + lane);
             if (c < width)
                 *reinterpret_cast<uint2*>(static_cast<uint8_t*>(out.d_codes) + row * out.ld + c) = make_uint2(i8_encode4(v[j], inv), i8_encode4(v[j] + 4, inv));
-            if (y && c < p.C) store8(y + row * ld_y + c, p.C - c, v[j]);
         }
         if (lane == 0) out.d_scales[row] = held;
     }
@@ -894,7 +892,7 @@ hipError_t launch_group_norm(const fmtc_gnorm& a, void* d_y, int64_t ld_y, const
                         constexpr int TPR = decltype(tpr)::value, VPT = decltype(vpt)::value;
                         const int64_t parts = parts_of(p, codes_threads(TPR) / TPR, 1, 2048), rows = ceil_div(p.S, parts);
                         return go(K_GROUP_NORM, k_group_norm_codes<T, decltype(rows_kind)::value, TPR, VPT>, p.samples * parts, codes_threads(TPR),
-                                  sizeof(float) * 2 * p.G, s, p, plan.rows ? nullptr : part, parts, rows, a.eps, a.act, *codes, static_cast<T*>(d_y), ld_y, stats);
+                                  sizeof(float) * 2 * p.G, s, p, plan.rows ? nullptr : part, parts, rows, a.eps, a.act, *codes, stats);
                     };
                     if (p.C <= 128) return with(Int<16>{}, Int<1>{});
                     if (p.C <= 512) return with(Int<64>{}, Int<1>{});

@@ -149,6 +149,12 @@ def test_norm_outputs(lib):
     assert lib.fmtc_group_norm_workspace_size(4, 4, 8, 8, 7, 1) == 0 and lib.fmtc_group_norm_backward_workspace_size(4, 4, 8, 8, 7) == 0
 
 
+def test_a_norm_writes_values_or_codes(lib):
+    codes = _i8(rows=20, depth=16, ld=128)
+    _refused(lib, lib.fmtc_group_norm(_norm(), SOME + 8192, 16, codes, None, SOME, 1 << 20, None), "y and codes")
+    _refused(lib, lib.fmtc_group_norm(_norm(), SOME + 8192, 16, codes, SOME + 4096, SOME, 1 << 20, None), "y and codes")
+
+
 def _list(*entries):
     return (fmtc._Tensor * len(entries))(*(fmtc._Tensor(**(dict(d_in=SOME, d_out=SOME + 8192, n=100, type=fmtc.F32, out_type=fmtc.BF16) | e)) for e in entries))
 
