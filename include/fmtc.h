@@ -462,7 +462,8 @@ fmtc_status fmtc_i8_linear(const void *d_x, fmtc_dtype type, int64_t rows, int64
  * sample's group: mean, variance (of all values, not one less), r = 1 / sqrt(variance + eps);
  *     z = weight * (x - mean) * r + bias       y = act(z)
  * act: z, max(z, 0) (NaN stays NaN), or z / (1 + e^-z).  x, y, dy and dx are `type`; weight and
- * bias (NULL: 1 and 0) f32 or `type`.  Statistics are summed in f64. */
+ * bias (NULL: 1 and 0) f32 or `type`.  Statistics are summed in f64, right however far the mean is from 0; mean and r are rounded
+ * to f32 before they are applied. */
 typedef enum fmtc_act { FMTC_ACT_NONE = 0, FMTC_ACT_RELU = 1, FMTC_ACT_SILU = 2 } fmtc_act;
 typedef struct fmtc_gnorm {
     int64_t samples, rows_per_sample;

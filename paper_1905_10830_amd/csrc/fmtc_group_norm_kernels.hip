@@ -187,19 +187,64 @@ __device__ __forceinline__ void sums_by_group(const Maps& p, const Place& at, bo
         if (l == 0) f(g, a, b);
     });
 }
+// The variance is right however far the mean is from 0, with sums in f64 (reading 100 MB takes the same time with them as with f32
+// ones, 5.1 TB/s):
+// * f32: what is summed is the values' distance from an origin, the first value of their sample's group (0 where that is not
+//   finite); in f64 that difference is exact unless the two are 2^29 apart.  The origin lies within sqrt(S D) deviations of the
+//   mean, so that the variance loses S D of 2^53 at most.  Sums of the values themselves lose (mean / deviation)^2, which was 7e-4
+//   of r at a mean of 3e6 deviations.  (The differences cost 0 to 5 % of a norm's time: 1 x 262144 x 64 36.7 -> 37.3 us, 128 x 784 x
+//   256 47.8 -> 48.6, 100 x 60 x 960 14.7 -> 15.4.)
+// * 16 bits: values of one sign whose magnitudes are within 4 of each other are multiples of 2^-13 of the largest: sums of up to 2^27
+//   of them and of their squares are exact, and finish() loses nothing of those either.  Where others are among them, the mean
+//   is within 3 sqrt(S D) deviations of 0.
 template <class T>
-__device__ __forceinline__ void add(const Raw<T>& raw, double (&s)[8], double (&q)[8]) {
-#pragma unroll
-    for (int i = 0; i < 8; i++) {
-        const double v = raw[i];
-        s[i] += v;
-        q[i] = fma(v, v, q[i]);
+constexpr bool kFromOrigin = sizeof(T) == 4;
+// The origins of a thread's 8 channels (ONE: they are of one group): loaded behind the first values, not before them (128 x 784 x 256
+// 48.6 us, else 54.5), and looked at when those are on their way.
+template <class T, bool ONE>
+struct Origins {
+    static constexpr int N = !kFromOrigin<T> ? 0 : ONE ? 1 : 8;
+    T raw[N ? N : 1];
+    double o[N ? N : 1];
+    __device__ __forceinline__ void load(const Maps& p, const Place& at, int c) {
+        const T* const first = static_cast<const T*>(p.x) + at.n * p.S * p.ld + at.c0;
+        if constexpr (N == 1) raw[0] = first[quotient(c, 1.f / (float)p.D) * p.D];
+        if constexpr (N == 8) each_group(c, at.width, p.D, [&](int i, int g) { raw[i] = first[g * p.D]; });
     }
-}
-// From sums in f64, so that the variance is right however far the mean is from 0 (reading 100 MB takes the same time with f64
-// sums as with f32 ones, 5.1 TB/s).  stats: the caller's, or NULL
-__device__ __forceinline__ void finish(const Maps& p, const Place& at, int g, double s, double q, float eps, float* mean_r, float* stats) {
-    const double count = (double)p.S * (double)p.D, mean = s / count, var = q / count - mean * mean;
+    __device__ __forceinline__ float finite(int i) const { return __builtin_isfinite(to_f32(raw[i])) ? to_f32(raw[i]) : 0.f; }
+    __device__ __forceinline__ void settle() {
+#pragma unroll
+        for (int i = 0; i < N; i++) {
+            asm volatile("" : "+v"(raw[i]));  // (here, and not before the loop that this stands in)
+            o[i] = finite(i);
+        }
+    }
+    // to where finish() looks for them
+    __device__ __forceinline__ void keep(const Maps& p, const Place& at, int c, float* to) const {
+        if constexpr (N == 1) to[quotient(c, 1.f / (float)p.D)] = finite(0);
+        if constexpr (N == 8) each_group(c, at.width, p.D, [&](int i, int g) { to[g] = finite(i); });
+    }
+    __device__ __forceinline__ void add(Raw<T>& values, bool live, double (&s)[8], double (&q)[8]) const {
+        if constexpr (N > 0) {
+            if (!live) return;
+        } else {
+            values.zero_unless(live);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            double v = values[i];
+            if constexpr (N > 0) v -= o[ONE ? 0 : i];
+            s[i] += v;
+            q[i] = fma(v, v, q[i]);
+        }
+    }
+};
+// s, q: sums of the distances from the origin and of their squares.  var = (n q - s^2) / n^2, both products with what their
+// rounding takes (and not fused with the difference by the compiler).  stats: the caller's, or NULL
+__device__ __forceinline__ void finish(const Maps& p, const Place& at, int g, double origin, double s, double q, float eps, float* mean_r, float* stats) {
+#pragma clang fp contract(off)
+    const double count = (double)p.S * (double)p.D, mean = origin + s / count, nq = count * q, ss = s * s;
+    const double var = ((nq - ss) + (fma(count, q, -nq) - fma(s, s, -ss))) / (count * count);
     // (a variance that is not a number stays that)
     const float m = (float)mean, r = (float)(1.0 / sqrt((var < 0.0 ? 0.0 : var) + (double)eps));
     mean_r[g] = m;
@@ -258,7 +303,7 @@ constexpr int kUnroll = 4;  // rows of a thread on their way together
 
 // A slab in the registers of a workgroup, R rows a thread.  256 x 3136 x 64 (32 groups, a ReLU) 41 to 45 us, 4.6 to 5.0 TB/s
 // (in two passes 64); 128 x 784 x 256 23 us; 196 x 256 5.6 us, latency.
-template <class T, int KIND, int R>
+template <class T, int KIND, bool ONE, int R>
 __global__ __launch_bounds__(1024) void k_group_norm_once(Maps p, float eps, int act_kind, T* y, int64_t ld_y, float* __restrict__ stats) {
     extern __shared__ __attribute__((aligned(16))) double red[];
     const Place at(p, 1, 0);
@@ -269,20 +314,27 @@ __global__ __launch_bounds__(1024) void k_group_norm_once(Maps p, float eps, int
     Scale scale;
     double s[8] = {}, q[8] = {};
     if (me.live) {
+        Origins<T, ONE> origins;
 #pragma unroll
         for (int u = 0; u < R; u++) {
             const int64_t r = me.ly + (int64_t)u * p.LY;
             load_raw<KIND>(raw[u], x + (r < p.S ? r : 0) * p.ld, me.c, at.width);
         }
-        scale.load<T, KIND>(p, at, me.c);
+        origins.load(p, at, me.c);
+        constexpr bool kLater = kFromOrigin<T> && !ONE;  // (there are no registers for it beside the origins)
+        if constexpr (!kLater) scale.load<T, KIND>(p, at, me.c);
+        origins.settle();
 #pragma unroll
         for (int u = 0; u < R; u++) {
             settle_raw<KIND>(raw[u], me.c, at.width);
-            raw[u].zero_unless(me.ly + (int64_t)u * p.LY < p.S);
-            add(raw[u], s, q);
+            origins.add(raw[u], me.ly + (int64_t)u * p.LY < p.S, s, q);
         }
+        if (me.ly == 0) origins.keep(p, at, me.c, mean_r);
+        if constexpr (kLater) scale.load<T, KIND>(p, at, me.c);
     }
-    sums_by_group(p, at, me.live, s, q, red, [&](int g, double a, double b) { finish(p, at, g, a, b, eps, mean_r, stats); });
+    sums_by_group(p, at, me.live, s, q, red, [&](int g, double a, double b) {
+        finish(p, at, g, kFromOrigin<T> ? mean_r[g] : 0.0, a, b, eps, mean_r, stats);
+    });
     __syncthreads();
     if (!me.live || !y) return;
     scale.settle(p, at, me.c, mean_r);
@@ -297,9 +349,10 @@ __global__ __launch_bounds__(1024) void k_group_norm_once(Maps p, float eps, int
     }
 }
 
-// The sums of the values and of their squares, of each part of a sample's rows and each group: part[sample][chunk][group].  512 x
+// The sums of the values (f32: of their distances from the origin) and of the squares, of each part of a sample's rows and each
+// group: part[sample][chunk][group], and behind them the origins [sample][group]: the next kernel may write over the values.  512 x
 // 512 x 128 12.2 to 13.2 us (5.1 to 5.5 TB/s).
-template <class T, int KIND>
+template <class T, int KIND, bool ONE>
 __global__ __launch_bounds__(1024) void k_group_norm_sums(Maps p, double2* __restrict__ part) {
     extern __shared__ __attribute__((aligned(16))) double red[];
     const Place at(p, p.chunks, 0);
@@ -308,6 +361,8 @@ __global__ __launch_bounds__(1024) void k_group_norm_sums(Maps p, double2* __res
     double s[8] = {}, q[8] = {};
     if (me.live) {
         const T* const x = slab_of<T>(p.x, p.ld, p, at);
+        Origins<T, ONE> origins;
+        origins.load(p, at, me.c);
         for (int64_t r = r0 + me.ly; r < r1; r += (int64_t)kUnroll * p.LY) {
             Raw<T> raw[kUnroll];
 #pragma unroll
@@ -315,20 +370,23 @@ __global__ __launch_bounds__(1024) void k_group_norm_sums(Maps p, double2* __res
                 const int64_t from = r + (int64_t)u * p.LY;
                 load_raw<KIND>(raw[u], x + (from < r1 ? from : r) * p.ld, me.c, at.width);
             }
+            origins.settle();
 #pragma unroll
             for (int u = 0; u < kUnroll; u++) {
                 settle_raw<KIND>(raw[u], me.c, at.width);
-                raw[u].zero_unless(r + (int64_t)u * p.LY < r1);
-                add(raw[u], s, q);
+                origins.add(raw[u], r + (int64_t)u * p.LY < r1, s, q);
             }
         }
+        if (at.k == 0 && me.ly == 0) origins.keep(p, at, me.c, reinterpret_cast<float*>(part + p.samples * p.chunks * p.G) + at.n * p.G + at.g0);
     }
     double2* const to = part + (at.n * p.chunks + at.k) * p.G + at.g0;
     sums_by_group(p, at, me.live, s, q, red, [&](int g, double a, double b) { to[g] = make_double2(a, b); });
 }
 
 // mean and r of each group of a slab into LDS, and, by the first workgroup of a slab, where the caller wants them
+template <class T>
 __device__ __forceinline__ void finish_parts(const Maps& p, const Place& at, const double2* part, float eps, float* mean_r, float* stats) {
+    const float* const origins = reinterpret_cast<const float*>(part + p.samples * p.chunks * p.G) + at.n * p.G + at.g0;
     spread(at.groups, [&](int g, int l, int lanes) {
         double s = 0.0, q = 0.0;
         const double2* const from = part + at.n * p.chunks * p.G + at.g0 + g;
@@ -344,7 +402,7 @@ __device__ __forceinline__ void finish_parts(const Maps& p, const Place& at, con
         }
         s = lanes_sum(s, lanes);
         q = lanes_sum(q, lanes);
-        if (l == 0) finish(p, at, g, s, q, eps, mean_r, at.k == 0 ? stats : nullptr);
+        if (l == 0) finish(p, at, g, kFromOrigin<T> ? origins[g] : 0.0, s, q, eps, mean_r, at.k == 0 ? stats : nullptr);
     });
     __syncthreads();
 }
@@ -358,7 +416,7 @@ __global__ __launch_bounds__(1024) void k_group_norm_apply(Maps p, const double2
     const Lane me = lane_of(p, at);
     Scale scale;
     scale.load<T, KIND>(p, at, me.c);
-    finish_parts(p, at, part, eps, mean_r, stats);
+    finish_parts<T>(p, at, part, eps, mean_r, stats);
     if (!y || !me.live) return;
     scale.settle(p, at, me.c, mean_r);
     const int64_t r0 = at.k * rows, r1 = r0 + rows < p.S ? r0 + rows : p.S;
@@ -408,7 +466,7 @@ __global__ __launch_bounds__(codes_threads(TPR)) void k_group_norm_codes(Maps p,
 #pragma unroll
     for (int j = 0; j < VPT; j++) scale[j].template load<T, KIND>(p, at, 8 * (j * TPR + lane));
     if (part) {
-        finish_parts(p, at, part, eps, mean_r, stats);
+        finish_parts<T>(p, at, part, eps, mean_r, stats);
     } else {
         for (int g = threadIdx.x; g < p.G; g += blockDim.x) {
             mean_r[g] = stats[at.n * p.G + g];
@@ -856,7 +914,8 @@ int type_size(int type) { return type == FMTC_F32 ? 4 : 2; }
 
 size_t group_norm_workspace(int64_t samples, int64_t S, int C, int groups, int type, bool to_codes) {
     const Plan plan = make_plan(samples, S, C, groups, type_size(type), 1);
-    if (!plan.rows) return align_up(sizeof(double2) * (size_t)(samples * plan.chunks) * groups, 256);
+    // (sums, and the groups' origins)
+    if (!plan.rows) return align_up((sizeof(double2) * (size_t)plan.chunks + (type == FMTC_F32 ? sizeof(float) : 0)) * (size_t)samples * groups, 256);
     return to_codes ? align_up(sizeof(float) * 2 * (size_t)samples * groups, 256) : 0;  // (statistics that the caller does not want)
 }
 size_t group_norm_backward_workspace(int64_t samples, int64_t S, int C, int groups, int type) {
@@ -874,14 +933,18 @@ hipError_t launch_group_norm(const fmtc_gnorm& a, void* d_y, int64_t ld_y, const
             constexpr int R = decltype(kd)::value;
             const size_t lds = sizeof(double) * (2 << p.pre) * plan.threads, lds_stats = sizeof(float) * 2 * p.groups;
             float* const stats = codes && plan.rows && !d_stats ? static_cast<float*>(d_ws) : d_stats;
+            auto first = [&](auto one) {
+                constexpr bool ONE = decltype(one)::value;
+                if (plan.rows)
+                    return with_rows<T>(plan.rows, [&](auto rows) {
+                        return go(K_GROUP_NORM, k_group_norm_once<T, R, ONE, decltype(rows)::value>, p.samples * p.slabs, plan.threads, lds + lds_stats, s,
+                                  p, a.eps, a.act, codes ? nullptr : static_cast<T*>(d_y), ld_y, stats);
+                    });
+                return go(K_GROUP_NORM, k_group_norm_sums<T, R, ONE>, p.samples * p.slabs * p.chunks, plan.threads, lds, s, p, part);
+            };
             hipError_t e;
-            if (plan.rows)
-                e = with_rows<T>(plan.rows, [&](auto rows) {
-                    return go(K_GROUP_NORM, k_group_norm_once<T, R, decltype(rows)::value>, p.samples * p.slabs, plan.threads, lds + lds_stats, s,
-                              p, a.eps, a.act, codes ? nullptr : static_cast<T*>(d_y), ld_y, stats);
-                });
-            else
-                e = go(K_GROUP_NORM, k_group_norm_sums<T, R>, p.samples * p.slabs * p.chunks, plan.threads, lds, s, p, part);
+            if constexpr (kFromOrigin<T> && R == kWhole) e = p.pre == 0 ? first(Int<1>{}) : first(Int<0>{});  // (a thread's channels are of one group)
+            else e = first(Int<0>{});
             if (e != hipSuccess || (plan.rows && !codes)) return e;
             if (codes) {
                 p.W = p.C;  // (rows as a whole)

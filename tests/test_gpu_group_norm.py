@@ -161,6 +161,89 @@ def test_mean_far_from_zero():
     _check_stats(stats, want_stats)
 
 
+# in one pass and in two, the last ones in parts; groups of 8, 3, 23 and all channels
+FAR = [(2, 196, 64, 8), (3, 50, 27, 9), (7, 1739, 161, 7), (1, 262144, 16, 4), (1, 40000, 40, 1), (2, 3000, 2048, 32)]
+
+
+@pytest.mark.parametrize("mean, deviation", [(1e4, 1 / 16), (1e5, 1 / 16), (1e6, 1.0), (-3e6, 1.0), (1e30, 1e25)])
+@pytest.mark.parametrize("samples, rows, C, groups", FAR)
+def test_statistics_wherever_the_mean_is(samples, rows, C, groups, mean, deviation):
+    """A mean of 1e5 to 3e6 deviations, without eps: r off by the roundings of f32, as near 0.  (The differences from a group's first
+    value are exact in 64 bits; that value is within 6 deviations here, which costs the variance 36 of 2^53.)"""
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x = mean + deviation * torch.randn((samples * rows, C), generator=g, device="cuda")
+    y, stats = fmtc.group_norm(x, groups, rows_per_sample=rows, stats=True, eps=0.0)
+    want, bound, want_stats = ref.group_norm(x, samples, groups, None, None, "none", 0.0, torch.float32)
+    _close(y, want, bound)
+    for got, w in zip(stats.double(), want_stats):  # (rounded once; r in f64 off by far less)
+        assert bool(((got - w).abs() <= 1.01 * ref.U * w.abs()).all())
+    q = fmtc.i8_empty(samples * rows, C)
+    assert torch.equal(fmtc.group_norm(x, groups, rows_per_sample=rows, out=q, stats=True, eps=0.0)[1], stats)
+    assert torch.equal(fmtc.group_norm(x, groups, rows_per_sample=rows, out=x, eps=0.0)[0], y)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("samples, rows, C, groups", FAR)
+def test_the_first_value_far_from_the_others(samples, rows, C, groups, dtype):
+    """What the sums are taken from lies as far from the mean as one of S D values can: that costs the variance S D of 2^53 at most, and
+    the mean half a step of f64 of that value for each addition that it passes.  Of a group that begins with an infinity or a NaN
+    all is not a number, but the mean, which is what the sum of its values is."""
+    x = _values(samples, rows, C, dtype)
+    D = C // groups
+    x.view(samples, rows, C)[:, 0, ::D] = 30000.0
+    w, b = _params(C, torch.float32)
+    y, stats = fmtc.group_norm(x, groups, w, b, rows_per_sample=rows, stats=True)
+    want, bound, want_stats = ref.group_norm(x, samples, groups, w, b, "none", 1e-5, dtype)
+    _close(y, want, bound)
+    added = 2.0 ** -53 * 30000 * (rows + D + 64)
+    assert bool(((stats[0].double() - want_stats[0]).abs() <= 1.01 * ref.U * want_stats[0].abs() + added).all())
+    assert bool(((stats[1].double() - want_stats[1]).abs() <= 1.51 * ref.U * want_stats[1]).all())
+    x.view(samples, rows, C)[-1, 0, 0] = float("inf")
+    x.view(samples, rows, C)[0, 0, C - D] = float("nan")
+    y, got = fmtc.group_norm(x, groups, w, b, rows_per_sample=rows, stats=True)
+    bad = torch.zeros((samples, groups), dtype=torch.bool, device="cuda")
+    bad[-1, 0] = bad[0, groups - 1] = True
+    assert torch.equal(torch.isnan(got[1]), bad) and torch.equal(got[:, ~bad], stats[:, ~bad])
+    if (samples, groups) != (1, 1):
+        assert float(got[0, -1, 0]) == float("inf")
+    assert torch.equal(torch.isnan(y).view(samples, rows, groups, D).any(3).any(1), bad)
+
+
+@pytest.mark.parametrize("value", [3.0, 1e5 + 1 / 128, -7e9, 3e4 + 16])
+@pytest.mark.parametrize("samples, rows, C, groups", FAR)
+def test_maps_of_one_value(samples, rows, C, groups, value):
+    """The variance of equal values is 0, not what f64 leaves of the difference of two squares: r is eps^-1/2, rounded (and eps in
+    f32: half a step of it, which is half of that of r), y the bias."""
+    w, b = _params(C, torch.float32)
+    for dtype in (torch.float32, torch.bfloat16):
+        x = torch.full((samples * rows, C), value, device="cuda").to(dtype)
+        y, stats = fmtc.group_norm(x, groups, w, b, rows_per_sample=rows, stats=True)
+        assert torch.equal(y, b.to(dtype).expand(x.shape))
+        assert bool((stats[0] == x[0, 0].float()).all())
+        assert float((stats[1].double() - 1e-5 ** -0.5).abs().max()) <= 1.51 * ref.U * 1e-5 ** -0.5
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("samples, rows, C, groups", FAR)
+def test_maps_of_almost_one_value(samples, rows, C, groups, dtype):
+    """One value of a group a step away from the others, without eps: a variance of 2^-44 of the mean's square and less.  The last value
+    of a group, and (second sample, or all groups but the first) its first one."""
+    base = torch.full((1,), 200.0, device="cuda").to(dtype)
+    step = torch.nextafter(base.cpu(), torch.full((1,), 1e4, dtype=dtype)).to("cuda")
+    x = base.expand(samples * rows, C).clone()
+    v = x.view(samples, rows, groups, C // groups)
+    v[0, -1, 0, -1] = step
+    v[0, 0, 1:, 0] = step
+    v[1:, 0, :, 0] = step
+    y, stats = fmtc.group_norm(x, groups, rows_per_sample=rows, stats=True, eps=0.0)
+    n, off = rows * C // groups, float(step) - float(base)
+    r = 1.0 / (off * (1.0 / n * (1.0 - 1.0 / n)) ** 0.5)  # n - 1 equal values and one: (n - 1) / n^2 off^2
+    assert bool(((stats[1].double() - r).abs() <= 1.01 * ref.U * r).all())
+    assert bool(((stats[0].double() - (float(base) + off / n)).abs() <= 1.01 * ref.U * float(step)).all())
+    want, bound, _ = ref.group_norm(x, samples, groups, None, None, "none", 0.0, dtype)
+    _close(y, want, bound)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_in_place_and_strides(dtype):
     samples, rows, C, groups = 3, 50, 96, 8
