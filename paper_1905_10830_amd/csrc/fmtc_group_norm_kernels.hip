@@ -689,52 +689,55 @@ __global__ __launch_bounds__(1024) void k_group_norm_gradient_sums(Maps p, const
 }
 
 // The sum of from[first], from[first + step].. below n, `apart` from each other, 16 loads on their way together (a loop with a
-// remainder would wait for each load of that: 0.7 us each)
-__device__ __forceinline__ float strided_sum(const float* from, int64_t first, int64_t step, int64_t n, int64_t apart) {
-    float sum = 0.f;
+// remainder would wait for each load of that: 0.7 us each).  V: double over samples, of which there are any number; float over the
+// parts of one (128 at most): 7 x 1739 x 161 f32 1 us less.
+template <class V>
+__device__ __forceinline__ V strided_sum(const float* from, int64_t first, int64_t step, int64_t n, int64_t apart) {
+    V sum = 0;
     for (int64_t k = first; k < n; k += 16 * step) {
         float v[16];
 #pragma unroll
         for (int j = 0; j < 16; j++) v[j] = from[(k + j * step < n ? k + j * step : n - 1) * apart];
 #pragma unroll
-        for (int j = 0; j < 16; j++) sum += k + j * step < n ? v[j] : 0.f;
+        for (int j = 0; j < 16; j++) sum += (V)(k + j * step < n ? v[j] : 0.f);
     }
     return sum;
 }
 
 // dbias and dweight: sums over n rows of part, 32 columns a workgroup, slices of the rows, added up in order
-__device__ __forceinline__ void param_sums(const float* part, int64_t n, int C, float* dweight, float* dbias, float* slice) {
+__device__ __forceinline__ void param_sums(const float* part, int64_t n, int C, float* dweight, float* dbias, double* slice) {
     const int col = threadIdx.x & 31, k = threadIdx.x >> 5, slices = blockDim.x >> 5, c = blockIdx.x * 32 + col;
-    float sum = 0.f;
-    if (c < 2 * C) sum = strided_sum(part + c, k, slices, n, 2 * C);
+    double sum = 0.0;
+    if (c < 2 * C) sum = strided_sum<double>(part + c, k, slices, n, 2 * C);
     slice[k * 33 + col] = sum;
     __syncthreads();
     if (k == 0 && c < 2 * C) {
         for (int i = 1; i < slices; i++) sum += slice[i * 33 + col];
         float* const to = c < C ? dbias : dweight;
-        if (to) to[c < C ? c : c - C] = sum;
+        if (to) to[c < C ? c : c - C] = (float)sum;
     }
 }
-// The sums of all parts of a sample by channel, where they are too many for every workgroup of the next kernel to add up: 32
-// columns a workgroup.  to[sample][2][C]
-__global__ __launch_bounds__(1024) void k_group_norm_join(const float* __restrict__ part, int64_t chunks, int C, float* __restrict__ to) {
-    __shared__ float slice[32 * 33];
-    const int64_t n = blockIdx.y;
+// The sums of every `each` parts by channel: those of a sample, where they are too many for every workgroup of the next kernel to
+// add up, or of kEach samples, where there are too many for the few workgroups that the channels make.  32 columns a workgroup.
+// to[parts / each][2][C]
+__global__ __launch_bounds__(1024) void k_group_norm_join(const float* __restrict__ part, int64_t each, int64_t parts, int C, float* __restrict__ to) {
+    __shared__ double slice[32 * 33];
+    const int64_t n = blockIdx.y, mine = parts - n * each < each ? parts - n * each : each;
     const int col = threadIdx.x & 31, k = threadIdx.x >> 5, c = blockIdx.x * 32 + col;
-    float sum = 0.f;
-    if (c < 2 * C) sum = strided_sum(part + n * chunks * 2 * C + c, k, 32, chunks, 2 * C);
+    double sum = 0.0;
+    if (c < 2 * C) sum = strided_sum<double>(part + n * each * 2 * C + c, k, 32, mine, 2 * C);
     slice[k * 33 + col] = sum;
     __syncthreads();
     if (k == 0 && c < 2 * C) {
 #pragma unroll
         for (int i = 1; i < 32; i++) sum += slice[i * 33 + col];
-        to[n * 2 * C + c] = sum;
+        to[n * 2 * C + c] = (float)sum;
     }
 }
 
 __global__ __launch_bounds__(1024) void k_group_norm_params(const float* __restrict__ part, int64_t n, int C, float* __restrict__ dweight,
                                                             float* __restrict__ dbias) {
-    __shared__ float slice[32 * 33];
+    __shared__ double slice[32 * 33];
     param_sums(part, n, C, dweight, dbias, slice);
 }
 
@@ -745,14 +748,14 @@ __global__ __launch_bounds__(1024) void k_group_norm_dx(Maps p, const float* __r
                                                         int64_t rows, uint32_t before, const T* dy, int64_t ld_dy, T* dx, int64_t ld_dx,
                                                         float* __restrict__ dweight, float* __restrict__ dbias) {
     extern __shared__ __attribute__((aligned(16))) float red_f[];  // [slices][2][width] (or the other sums' slices), then [2][groups]: A and B
-    if (blockIdx.x < before) return param_sums(part, p.samples * p.chunks, p.C, dweight, dbias, red_f);
+    if (blockIdx.x < before) return param_sums(part, p.samples * p.chunks, p.C, dweight, dbias, reinterpret_cast<double*>(red_f));
     const Place at(p, parts, before);
     const int wide = 2 * at.width, t = threadIdx.x, slices = (int)blockDim.x / wide < p.chunks ? (int)blockDim.x / wide : (int)p.chunks;
     float* const ab = red_f + (slices > 1 ? slices : 1) * wide;
     // sums over the chunks: neighbouring threads on neighbouring channels, several slices of the chunks where threads are left
     for (int i = t; i < (slices > 1 ? slices : 1) * wide; i += blockDim.x) {
         const int slice = i / wide, j = i - slice * wide, which = j >= at.width, c = at.c0 + j - which * at.width;
-        const float sum = strided_sum(part + at.n * p.chunks * 2 * p.C + which * p.C + c, slice, slices > 1 ? slices : 1, p.chunks, 2 * p.C);
+        const float sum = strided_sum<float>(part + at.n * p.chunks * 2 * p.C + which * p.C + c, slice, slices > 1 ? slices : 1, p.chunks, 2 * p.C);
         red_f[i] = sum * weight_at<T>(p, c);
     }
     __syncthreads();
@@ -918,9 +921,14 @@ size_t group_norm_workspace(int64_t samples, int64_t S, int C, int groups, int t
     if (!plan.rows) return align_up((sizeof(double2) * (size_t)plan.chunks + (type == FMTC_F32 ? sizeof(float) : 0)) * (size_t)samples * groups, 256);
     return to_codes ? align_up(sizeof(float) * 2 * (size_t)samples * groups, 256) : 0;  // (statistics that the caller does not want)
 }
+// More than kMostParts parts are joined by kEach at a time before the few workgroups that the channels make add them up: 32768 x 64 x
+// 128 bf16 440 -> 342 us, 16384 x 49 x 256 328 -> 283.
+constexpr int64_t kMostParts = 2048, kEach = 256;
+int64_t joined_parts(int64_t parts) { return parts > kMostParts ? ceil_div(parts, kEach) : 0; }
 size_t group_norm_backward_workspace(int64_t samples, int64_t S, int C, int groups, int type) {
     const Plan plan = make_plan(samples, S, C, groups, type_size(type), 2);  // (in one pass there is one part of a sample)
-    return align_up(sizeof(float) * (size_t)(samples * (plan.rows ? 1 : plan.chunks + plan.join)) * 2 * C, 256);
+    const int64_t parts = samples * (plan.rows ? 1 : plan.chunks), joined = plan.join && !plan.rows ? samples : 0;
+    return align_up(sizeof(float) * (size_t)(parts + (joined > joined_parts(parts) ? joined : joined_parts(parts))) * 2 * C, 256);
 }
 
 hipError_t launch_group_norm(const fmtc_gnorm& a, void* d_y, int64_t ld_y, const fmtc_i8* codes, float* d_stats, void* d_ws, hipStream_t s) {
@@ -985,8 +993,21 @@ hipError_t launch_group_norm_backward(const fmtc_gnorm& a, const float* d_stats,
                 const bool params = d_dweight || d_dbias;
                 const int64_t param_groups = params ? ceil_div(2 * p.C, 32) : 0;
                 const size_t lds = sizeof(float) * 16 * plan.threads, lds_ab = sizeof(float) * 2 * p.groups;
+                auto join = [&](int64_t each, int64_t parts, float* to) {
+                    return launch(K_GROUP_NORM_BACKWARD, k_group_norm_join, dim3((unsigned)ceil_div(2 * p.C, 32), (unsigned)ceil_div(parts, each)), dim3(1024), 0, s,
+                                  part, each, parts, p.C, to);
+                };
                 auto sum_params = [&](int64_t n) {
-                    return params ? go(K_GROUP_NORM_BACKWARD, k_group_norm_params, param_groups, 1024, 0, s, part, n, p.C, d_dweight, d_dbias) : hipSuccess;
+                    if (!params) return hipSuccess;
+                    const float* from = part;
+                    if (const int64_t joined = joined_parts(n)) {
+                        float* const to = part + n * 2 * p.C;
+                        const hipError_t e = join(kEach, n, to);
+                        if (e != hipSuccess) return e;
+                        from = to;
+                        n = joined;
+                    }
+                    return go(K_GROUP_NORM_BACKWARD, k_group_norm_params, param_groups, 1024, 0, s, from, n, p.C, d_dweight, d_dbias);
                 };
                 if (plan.rows) {
                     const hipError_t e = with_rows<T>(plan.rows, [&](auto rows) {
@@ -998,22 +1019,26 @@ hipError_t launch_group_norm_backward(const fmtc_gnorm& a, const float* d_stats,
                 const hipError_t e = go(K_GROUP_NORM_BACKWARD, k_group_norm_gradient_sums<T, R, A>, p.samples * p.slabs * p.chunks, plan.threads, lds, s, p,
                                         d_stats, dy, ld_dy, part);
                 if (e != hipSuccess) return e;
-                if (!d_dx) return sum_params(p.samples * p.chunks);
+                const bool before = d_dx && !joined_parts(p.samples * p.chunks);  // (the parameters' sums by workgroups of the last kernel)
+                if (!before) {
+                    const hipError_t e = sum_params(p.samples * p.chunks);
+                    if (e != hipSuccess || !d_dx) return e;
+                }
                 Maps joined = p;
                 const float* sums_at = part;
                 if (plan.join) {
                     float* const to = part + p.samples * p.chunks * 2 * p.C;
-                    const hipError_t e = launch(K_GROUP_NORM_BACKWARD, k_group_norm_join, dim3((unsigned)ceil_div(2 * p.C, 32), (unsigned)p.samples), dim3(1024), 0, s,
-                                                part, p.chunks, p.C, to);
+                    const hipError_t e = join(p.chunks, p.samples * p.chunks, to);
                     if (e != hipSuccess) return e;
                     joined.chunks = 1;
                     sums_at = to;
                 }
                 const int64_t parts = parts_of(p, p.LY, kUnroll / 2, kSecondPass), rows = ceil_div(p.S, parts);
                 size_t lds_dx = sizeof(float) * (2 * p.W > plan.threads ? 2 * p.W : plan.threads) + lds_ab;
-                if (lds_dx < sizeof(float) * 33 * (plan.threads / 32)) lds_dx = sizeof(float) * 33 * (plan.threads / 32);
-                return go(K_GROUP_NORM_BACKWARD, k_group_norm_dx<T, R, A>, param_groups + p.samples * p.slabs * parts, plan.threads, lds_dx, s, joined, d_stats,
-                          sums_at, parts, rows, (uint32_t)param_groups, dy, ld_dy, static_cast<T*>(d_dx), ld_dx, d_dweight, d_dbias);
+                if (lds_dx < sizeof(double) * 33 * (plan.threads / 32)) lds_dx = sizeof(double) * 33 * (plan.threads / 32);
+                const int64_t of_params = before ? param_groups : 0;
+                return go(K_GROUP_NORM_BACKWARD, k_group_norm_dx<T, R, A>, of_params + p.samples * p.slabs * parts, plan.threads, lds_dx, s, joined, d_stats,
+                          sums_at, parts, rows, (uint32_t)of_params, dy, ld_dy, static_cast<T*>(d_dx), ld_dx, d_dweight, d_dbias);
             });
         });
     });

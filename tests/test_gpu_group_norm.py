@@ -291,6 +291,26 @@ def test_one_of_weight_and_bias(weight, bias):
     assert only[0] is None and all((a is None) == (c is None) and (a is None or torch.equal(a, c)) for a, c in zip(only[1:], (dw, db)))
 
 
+# in one pass and in two, with sums of parts in every number
+MANY = [(1000, 1, 64, 8), (2049, 3, 64, 8), (5000, 1, 40, 5), (70000, 1, 16, 2), (3000, 1, 264, 33), (9, 30000, 8, 1), (2100, 1, 4104, 1), (2300, 400, 64, 1)]
+
+
+@pytest.mark.parametrize("dx", [None, False])
+@pytest.mark.parametrize("samples, rows, C, groups", MANY)
+def test_parameter_gradients_of_many_samples(samples, rows, C, groups, dx):
+    """Gradients of 4 / 3 everywhere: f32 sums one after the other lose the same part of a step each time.  Within a sample's part there
+    are no more additions than rows, the parts are added up in f64; two roundings to f32 at the end."""
+    x = _values(samples, rows, C, torch.float32)
+    dy = torch.full_like(x, 4 / 3)
+    w, b = _params(C, torch.float32)
+    _, stats = fmtc.group_norm(x, groups, w, b, rows_per_sample=rows, out=False, stats=True)
+    _, dw, db = fmtc.group_norm_backward(dy, x, stats, groups, w, b, rows_per_sample=rows, dx=dx)
+    (_, want_w, want_b), (_, size_w, size_b) = ref.group_norm_backward(dy, x, samples, groups, w, b, "none", 1e-5, stats)
+    added = min(rows, 1500)  # (a sample of more rows is cut in parts, each of its threads' sums is a part of that)
+    _close(db, want_b, ref.U * (added + 1.02) * size_b)
+    _close(dw, want_w, ref.U * (added + 1.02 + 3) * size_w)  # (and each dz x^: the difference, the product with r, and with dz)
+
+
 def test_no_rows():
     x = torch.empty((0, 48), dtype=torch.bfloat16, device="cuda")
     w, b = _params(48, torch.float32)
