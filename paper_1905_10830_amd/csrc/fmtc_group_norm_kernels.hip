@@ -8,6 +8,8 @@
 // there.  Where a slab fits the registers of one workgroup, all is done with one read of the values (k_group_norm_once,
 // k_group_norm_backward_once); else the rows are cut in chunks, whose sums one kernel leaves in the workspace and the next one
 // adds up before it reads the values again.
+#include <type_traits>
+
 #include "fmtc_block.h"
 
 namespace fmtc {
@@ -15,7 +17,7 @@ namespace fmtc {
 namespace {
 
 struct Maps {
-    int64_t samples, S, ld;
+    int64_t samples, all, S, ld;  // samples of this launch, and those that the statistics are of (from one to the next of their arrays)
     int C, G, D;          // D channels a group
     int W, groups, slabs, LX, LY; // channels and groups of a slab (the last one may have fewer), slabs of a row; lanes of a row, rows at a time
     int pre;                      // sums by group: a thread's 8 channels leave 1 << pre values (see fold)
@@ -251,7 +253,7 @@ __device__ __forceinline__ void finish(const Maps& p, const Place& at, int g, do
     mean_r[at.groups + g] = r;
     if (stats) {
         stats[at.n * p.G + at.g0 + g] = m;
-        stats[(p.samples + at.n) * p.G + at.g0 + g] = r;
+        stats[(p.all + at.n) * p.G + at.g0 + g] = r;
     }
 }
 
@@ -470,7 +472,7 @@ __global__ __launch_bounds__(codes_threads(TPR)) void k_group_norm_codes(Maps p,
     } else {
         for (int g = threadIdx.x; g < p.G; g += blockDim.x) {
             mean_r[g] = stats[at.n * p.G + g];
-            mean_r[p.G + g] = stats[(p.samples + at.n) * p.G + g];
+            mean_r[p.G + g] = stats[(p.all + at.n) * p.G + g];
         }
         __syncthreads();
     }
@@ -517,7 +519,7 @@ struct Channels {
     __device__ __forceinline__ void load(const Maps& p, const Place& at, const float* stats, int c) {
         load_param<T, KIND>(p.w, p.weight_type, at.c0 + c, p.C, 1.f, a);
         load_param<T, KIND>(p.b, p.weight_type, at.c0 + c, p.C, 0.f, b);
-        const float *const mean = stats + at.n * p.G + at.g0, *const rs = mean + p.samples * p.G;
+        const float *const mean = stats + at.n * p.G + at.g0, *const rs = mean + p.all * p.G;
         each_group(c, at.width, p.D, [&](int i, int g) {
             m[i] = mean[g];
             r[i] = rs[g];
@@ -704,8 +706,10 @@ __device__ __forceinline__ V strided_sum(const float* from, int64_t first, int64
     return sum;
 }
 
-// dbias and dweight: sums over n rows of part, 32 columns a workgroup, slices of the rows, added up in order
-__device__ __forceinline__ void param_sums(const float* part, int64_t n, int C, float* dweight, float* dbias, double* slice) {
+// dbias and dweight: sums over n rows of part, 32 columns a workgroup, slices of the rows, added up in order; with those of the
+// launches before this one in sums [2][C], where there are several (first: of the first one)
+struct Carry { double* sums; int first; };
+__device__ __forceinline__ void param_sums(const float* part, int64_t n, int C, float* dweight, float* dbias, Carry carry, double* slice) {
     const int col = threadIdx.x & 31, k = threadIdx.x >> 5, slices = blockDim.x >> 5, c = blockIdx.x * 32 + col;
     double sum = 0.0;
     if (c < 2 * C) sum = strided_sum<double>(part + c, k, slices, n, 2 * C);
@@ -713,6 +717,10 @@ __device__ __forceinline__ void param_sums(const float* part, int64_t n, int C, 
     __syncthreads();
     if (k == 0 && c < 2 * C) {
         for (int i = 1; i < slices; i++) sum += slice[i * 33 + col];
+        if (carry.sums) {
+            if (!carry.first) sum += carry.sums[c];
+            carry.sums[c] = sum;
+        }
         float* const to = c < C ? dbias : dweight;
         if (to) to[c < C ? c : c - C] = (float)sum;
     }
@@ -736,9 +744,9 @@ __global__ __launch_bounds__(1024) void k_group_norm_join(const float* __restric
 }
 
 __global__ __launch_bounds__(1024) void k_group_norm_params(const float* __restrict__ part, int64_t n, int C, float* __restrict__ dweight,
-                                                            float* __restrict__ dbias) {
+                                                            float* __restrict__ dbias, Carry carry) {
     __shared__ double slice[32 * 33];
-    param_sums(part, n, C, dweight, dbias, slice);
+    param_sums(part, n, C, dweight, dbias, carry, slice);
 }
 
 // dx from the sums of the parts.  The first `before` workgroups do the sums for dbias and dweight.  7 x 1739 x 161 f32 12.8 us, latency:
@@ -746,9 +754,9 @@ __global__ __launch_bounds__(1024) void k_group_norm_params(const float* __restr
 template <class T, int KIND, int ACT>
 __global__ __launch_bounds__(1024) void k_group_norm_dx(Maps p, const float* __restrict__ stats, const float* __restrict__ part, int64_t parts,
                                                         int64_t rows, uint32_t before, const T* dy, int64_t ld_dy, T* dx, int64_t ld_dx,
-                                                        float* __restrict__ dweight, float* __restrict__ dbias) {
+                                                        float* __restrict__ dweight, float* __restrict__ dbias, Carry carry) {
     extern __shared__ __attribute__((aligned(16))) float red_f[];  // [slices][2][width] (or the other sums' slices), then [2][groups]: A and B
-    if (blockIdx.x < before) return param_sums(part, p.samples * p.chunks, p.C, dweight, dbias, reinterpret_cast<double*>(red_f));
+    if (blockIdx.x < before) return param_sums(part, p.samples * p.chunks, p.C, dweight, dbias, carry, reinterpret_cast<double*>(red_f));
     const Place at(p, parts, before);
     const int wide = 2 * at.width, t = threadIdx.x, slices = (int)blockDim.x / wide < p.chunks ? (int)blockDim.x / wide : (int)p.chunks;
     float* const ab = red_f + (slices > 1 ? slices : 1) * wide;
@@ -876,9 +884,15 @@ Plan make_plan(int64_t samples, int64_t S, int C, int groups, int size, int arra
     return last.plan;
 }
 
-Maps maps_of(const fmtc_gnorm& a, const Plan& plan) {
+// Samples of a launch: workgroups have a sample each, a grid has less than 2^32 threads, and what lies in the workspace for each
+// sample shall not grow without end: sums by group (up to 160 MB), the gradients' sums by channel (64 MB).
+constexpr int64_t kMostThreads = ((int64_t)1 << 32) - 1;
+int64_t least_of(int64_t a, int64_t b) { return a < b ? a : b; }
+int64_t samples_forward(int64_t samples, int groups) { return least_of(samples, least_of((int64_t)1 << 20, ((int64_t)1 << 23) / groups)); }
+int64_t samples_backward(int64_t samples, int C) { return least_of(samples, ((int64_t)1 << 23) / (C < 8 ? 8 : C)); }
+Maps maps_of(const fmtc_gnorm& a, int64_t all, const Plan& plan) {
     const int LX = lanes_of(plan.W), D = a.C / a.groups;
-    return {a.samples, a.rows_per_sample, a.ld_x, a.C, a.groups, D, plan.W, plan.W / D, (int)ceil_div(a.C, plan.W), LX, plan.threads / LX, fold_of(D),
+    return {a.samples, all, a.rows_per_sample, a.ld_x, a.C, a.groups, D, plan.W, plan.W / D, (int)ceil_div(a.C, plan.W), LX, plan.threads / LX, fold_of(D),
             a.d_x, a.d_weight, a.d_bias, a.weight_type, plan.chunks, plan.chunks ? ceil_div(a.rows_per_sample, plan.chunks) : 0};
 }
 // parts of a sample's rows for the second pass: some rows for every thread, about `want` workgroups in all
@@ -916,6 +930,7 @@ int type_size(int type) { return type == FMTC_F32 ? 4 : 2; }
 }  // namespace
 
 size_t group_norm_workspace(int64_t samples, int64_t S, int C, int groups, int type, bool to_codes) {
+    samples = samples_forward(samples, groups);
     const Plan plan = make_plan(samples, S, C, groups, type_size(type), 1);
     // (sums, and the groups' origins)
     if (!plan.rows) return align_up((sizeof(double2) * (size_t)plan.chunks + (type == FMTC_F32 ? sizeof(float) : 0)) * (size_t)samples * groups, 256);
@@ -925,22 +940,27 @@ size_t group_norm_workspace(int64_t samples, int64_t S, int C, int groups, int t
 // 128 bf16 440 -> 342 us, 16384 x 49 x 256 328 -> 283.
 constexpr int64_t kMostParts = 2048, kEach = 256;
 int64_t joined_parts(int64_t parts) { return parts > kMostParts ? ceil_div(parts, kEach) : 0; }
-size_t group_norm_backward_workspace(int64_t samples, int64_t S, int C, int groups, int type) {
+static size_t sums_workspace(int64_t samples, int64_t S, int C, int groups, int type) {  // of a launch
     const Plan plan = make_plan(samples, S, C, groups, type_size(type), 2);  // (in one pass there is one part of a sample)
     const int64_t parts = samples * (plan.rows ? 1 : plan.chunks), joined = plan.join && !plan.rows ? samples : 0;
     return align_up(sizeof(float) * (size_t)(parts + (joined > joined_parts(parts) ? joined : joined_parts(parts))) * 2 * C, 256);
 }
+size_t group_norm_backward_workspace(int64_t samples, int64_t S, int C, int groups, int type) {
+    const int64_t some = samples_backward(samples, C);
+    return sums_workspace(some, S, C, groups, type) + (some < samples ? align_up(sizeof(double) * 2 * C, 256) : 0);
+}
 
-hipError_t launch_group_norm(const fmtc_gnorm& a, void* d_y, int64_t ld_y, const fmtc_i8* codes, float* d_stats, void* d_ws, hipStream_t s) {
-    const Plan plan = make_plan(a.samples, a.rows_per_sample, a.C, a.groups, type_size(a.type), 1);
-    Maps p = maps_of(a, plan);
+static hipError_t norm_some(const fmtc_gnorm& a, int64_t all, const Plan& plan, void* d_y, int64_t ld_y, const fmtc_i8* codes, float* d_stats,
+                            void* d_ws, hipStream_t s) {
+    const bool own_stats = codes && plan.rows && !d_stats;  // (in the workspace)
+    Maps p = maps_of(a, own_stats ? a.samples : all, plan);
     double2* const part = static_cast<double2*>(d_ws);
     return with_type(a.type, [&](auto ty) {
         using T = typename decltype(ty)::type;
         return with_kind(p, [&](auto kd) {
             constexpr int R = decltype(kd)::value;
             const size_t lds = sizeof(double) * (2 << p.pre) * plan.threads, lds_stats = sizeof(float) * 2 * p.groups;
-            float* const stats = codes && plan.rows && !d_stats ? static_cast<float*>(d_ws) : d_stats;
+            float* const stats = own_stats ? static_cast<float*>(d_ws) : d_stats;
             auto first = [&](auto one) {
                 constexpr bool ONE = decltype(one)::value;
                 if (plan.rows)
@@ -979,10 +999,36 @@ hipError_t launch_group_norm(const fmtc_gnorm& a, void* d_y, int64_t ld_y, const
     });
 }
 
-hipError_t launch_group_norm_backward(const fmtc_gnorm& a, const float* d_stats, const void* d_dy, int64_t ld_dy, void* d_dx, int64_t ld_dx,
-                                      float* d_dweight, float* d_dbias, void* d_ws, hipStream_t s) {
-    const Plan plan = make_plan(a.samples, a.rows_per_sample, a.C, a.groups, type_size(a.type), 2);
-    const Maps p = maps_of(a, plan);
+template <class P>
+static P* from_row(P* values, int type, int64_t row, int64_t ld) {
+    using Byte = typename std::conditional<std::is_const<P>::value, const char, char>::type;
+    return values ? static_cast<Byte*>(values) + row * ld * type_size(type) : nullptr;
+}
+// the samples from n on, `most` at most
+static fmtc_gnorm samples_from(const fmtc_gnorm& a, int64_t n, int64_t most) {
+    fmtc_gnorm b = a;
+    b.samples = a.samples - n < most ? a.samples - n : most;
+    b.d_x = from_row(a.d_x, a.type, n * a.rows_per_sample, a.ld_x);
+    return b;
+}
+hipError_t launch_group_norm(const fmtc_gnorm& a, void* d_y, int64_t ld_y, const fmtc_i8* codes, float* d_stats, void* d_ws, hipStream_t s) {
+    int64_t most = samples_forward(a.samples, a.groups);
+    const Plan plan = make_plan(most, a.rows_per_sample, a.C, a.groups, type_size(a.type), 1);
+    most = least_of(most, kMostThreads / (plan.threads * ceil_div(a.C, plan.W) * (plan.rows ? 1 : plan.chunks)));
+    hipError_t e = hipSuccess;
+    for (int64_t n = 0; n < a.samples && e == hipSuccess; n += most) {
+        const int64_t row = n * a.rows_per_sample;
+        fmtc_i8 q{};
+        if (codes) q = {static_cast<uint8_t*>(codes->d_codes) + row * codes->ld, codes->d_scales + row, codes->rows, codes->depth, codes->ld};
+        e = norm_some(samples_from(a, n, most), a.samples, plan, from_row(d_y, a.type, row, ld_y), ld_y, codes ? &q : nullptr,
+                      d_stats ? d_stats + n * a.groups : nullptr, d_ws, s);
+    }
+    return e;
+}
+
+static hipError_t backward_some(const fmtc_gnorm& a, int64_t all, const Plan& plan, const float* d_stats, const void* d_dy, int64_t ld_dy, void* d_dx,
+                                int64_t ld_dx, float* d_dweight, float* d_dbias, void* d_ws, Carry carry, hipStream_t s) {
+    const Maps p = maps_of(a, all, plan);
     float* const part = static_cast<float*>(d_ws);
     return with_type(a.type, [&](auto ty) {
         using T = typename decltype(ty)::type;
@@ -1007,7 +1053,7 @@ hipError_t launch_group_norm_backward(const fmtc_gnorm& a, const float* d_stats,
                         from = to;
                         n = joined;
                     }
-                    return go(K_GROUP_NORM_BACKWARD, k_group_norm_params, param_groups, 1024, 0, s, from, n, p.C, d_dweight, d_dbias);
+                    return go(K_GROUP_NORM_BACKWARD, k_group_norm_params, param_groups, 1024, 0, s, from, n, p.C, d_dweight, d_dbias, carry);
                 };
                 if (plan.rows) {
                     const hipError_t e = with_rows<T>(plan.rows, [&](auto rows) {
@@ -1038,10 +1084,25 @@ hipError_t launch_group_norm_backward(const fmtc_gnorm& a, const float* d_stats,
                 if (lds_dx < sizeof(double) * 33 * (plan.threads / 32)) lds_dx = sizeof(double) * 33 * (plan.threads / 32);
                 const int64_t of_params = before ? param_groups : 0;
                 return go(K_GROUP_NORM_BACKWARD, k_group_norm_dx<T, R, A>, of_params + p.samples * p.slabs * parts, plan.threads, lds_dx, s, joined, d_stats,
-                          sums_at, parts, rows, (uint32_t)of_params, dy, ld_dy, static_cast<T*>(d_dx), ld_dx, d_dweight, d_dbias);
+                          sums_at, parts, rows, (uint32_t)of_params, dy, ld_dy, static_cast<T*>(d_dx), ld_dx, d_dweight, d_dbias, carry);
             });
         });
     });
+}
+
+hipError_t launch_group_norm_backward(const fmtc_gnorm& a, const float* d_stats, const void* d_dy, int64_t ld_dy, void* d_dx, int64_t ld_dx,
+                                      float* d_dweight, float* d_dbias, void* d_ws, hipStream_t s) {
+    const int64_t most = samples_backward(a.samples, a.C);  // (times C / 8 slabs of 512 threads: 2^29)
+    const Plan plan = make_plan(most, a.rows_per_sample, a.C, a.groups, type_size(a.type), 2);
+    const size_t sums = sums_workspace(most, a.rows_per_sample, a.C, a.groups, a.type);
+    double* const carry = most < a.samples ? reinterpret_cast<double*>(static_cast<char*>(d_ws) + sums) : nullptr;
+    hipError_t e = hipSuccess;
+    for (int64_t n = 0; n < a.samples && e == hipSuccess; n += most) {
+        const int64_t row = n * a.rows_per_sample;
+        e = backward_some(samples_from(a, n, most), a.samples, plan, d_stats + n * a.groups, from_row(d_dy, a.type, row, ld_dy), ld_dy,
+                          from_row(d_dx, a.type, row, ld_dx), ld_dx, d_dweight, d_dbias, d_ws, {carry, n == 0}, s);
+    }
+    return e;
 }
 
 }  // namespace fmtc

@@ -311,6 +311,36 @@ def test_parameter_gradients_of_many_samples(samples, rows, C, groups, dx):
     _close(dw, want_w, ref.U * (added + 1.02 + 3) * size_w)  # (and each dz x^: the difference, the product with r, and with dz)
 
 
+# more samples than a launch takes, by a few; more than HIP's 2^32 threads would take with a workgroup each
+SEVERAL = [(2 * 131072 + 3, 1, 64, 8), (2048 + 5, 2, 8184, 8184), (2043 + 3, 2, 4104, 3), (1024 + 1, 3, 8192, 1), ((1 << 24) + 5, 1, 8, 2)]
+
+
+@pytest.mark.parametrize("samples, rows, C, groups", SEVERAL)
+def test_samples_of_several_launches(samples, rows, C, groups):
+    x = _values(samples, rows, C, torch.float32)
+    w, b = _params(C, torch.float32)
+    kw = dict(rows_per_sample=rows)
+    y, stats = fmtc.group_norm(x, groups, w, b, stats=True, **kw)
+    want, bound, want_stats = ref.group_norm(x, samples, groups, w, b, "none", 1e-5, torch.float32)
+    _close(y, want, bound)
+    _check_stats(stats, want_stats)
+    q = fmtc.i8_empty(samples * rows, C)
+    fmtc.group_norm(x, groups, w, b, out=q, **kw)
+    off = bound + q.scales.double()[:, None] * (0.5 + 127 * 3 * ref.U)
+    _close(q.codes[:, :C].double() * q.scales.double()[:, None], want, off)
+    del want, bound, off, q
+    dy = torch.full_like(x, 4 / 3)
+    dy[::2] = -0.3
+    (want, want_w, want_b), (terms, size_w, size_b) = ref.group_norm_backward(dy, x, samples, groups, w, b, "none", 1e-5, stats)
+    far = 1 + ((stats[0].abs() * stats[1]).max().double())  # the mean, in deviations: what its rounding is worth
+    for dx in (None, False):
+        got, dw, db = fmtc.group_norm_backward(dy, x, stats, groups, w, b, dx=dx, **kw)
+        if dx is None:
+            _close(got, want, 4 * ref.U * (rows + C // groups + 64) * far * terms)
+        _close(db, want_b, ref.U * (rows + 1.02) * size_b)
+        _close(dw, want_w, ref.U * (rows + 1.02 + 3) * size_w)
+
+
 def test_no_rows():
     x = torch.empty((0, 48), dtype=torch.bfloat16, device="cuda")
     w, b = _params(48, torch.float32)

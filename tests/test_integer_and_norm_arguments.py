@@ -149,6 +149,20 @@ def test_norm_outputs(lib):
     assert lib.fmtc_group_norm_workspace_size(4, 4, 8, 8, 7, 1) == 0 and lib.fmtc_group_norm_backward_workspace_size(4, 4, 8, 8, 7) == 0
 
 
+@pytest.mark.parametrize("kind", [fmtc.F32, fmtc.BF16])
+@pytest.mark.parametrize("C, groups", [(1, 1), (8, 2), (64, 8), (960, 32), (4104, 3), (8192, 1), (8192, 8192)])
+def test_workspaces_of_many_samples(lib, C, groups, kind):
+    """What a sample leaves in the workspace is there for as many samples as a launch takes, not for all: up to 2^30 of them."""
+    for rows in (1, 2, 50):
+        sizes = []
+        for samples in (1000, 1 << 14, 1 << 21, (1 << 24) + 5, 1 << 30):
+            if samples * rows < 1 << 31:
+                sizes.append([lib.fmtc_group_norm_workspace_size(samples, rows, C, groups, kind, to) for to in (0, 1)] +
+                             [lib.fmtc_group_norm_backward_workspace_size(samples, rows, C, groups, kind)])
+                assert all(n <= 1 << 28 for n in sizes[-1]), (samples, rows, sizes[-1])
+        assert sizes[-1] == sizes[-2]
+
+
 def test_a_norm_writes_values_or_codes(lib):
     codes = _i8(rows=20, depth=16, ld=128)
     _refused(lib, lib.fmtc_group_norm(_norm(), SOME + 8192, 16, codes, None, SOME, 1 << 20, None), "y and codes")
