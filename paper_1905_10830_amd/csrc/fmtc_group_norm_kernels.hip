@@ -849,9 +849,17 @@ Plan choose(int64_t samples, int64_t S, int C, int groups, int size, int arrays)
     // (a workgroup's time for the sums over the parts: rounds of its threads, each of several rounds of loads, 0.8 us; a kernel 4)
     best.join = arrays == 2 && best.chunks > 1 && ceil_div(best.chunks, 16) * ceil_div(2 * W, best.threads) > 4;
     double least = 9.0 + (bytes + values * size * arrays * (values * size * arrays > 2e8 ? 1.0 : 0.6)) / 5e6 * (C % 8 ? 1.3 : 1.0);
+    // (and the rounds of workgroups past the two or three that the parts make, where there are many samples: 16384 x 16 x 64 215 us,
+    // gradients 277, in one pass 31 and 48)
+    const double two_rounds = ceil((double)samples * ceil_div(C, W) * best.chunks / (kCus * 1024 / best.threads));
+    if (two_rounds > 3) least += (arrays == 1 ? 5.5 : 8.0) * (two_rounds - 2);
     for (int gs = 1;; gs = gs * 2 < groups ? gs * 2 : groups) {
         const int W = gs * D, LX = lanes_of(W);
-        for (int threads = 256; threads <= (arrays == 1 ? 1024 : 512); threads *= 2) {
+        // (small workgroups only for whole samples of few rows, and more of them than run at a time: 2^20 x 1 x 64 0.82 ms with 64
+        // threads, 3.1 with 256, gradients 1.3 and 3.9; 2048 x 1 x 64 in 8 slabs 16.5 us, whole with 256 threads 9.6)
+        const bool tiny = W == C && samples > 4096;
+        for (int threads = tiny ? 64 : 256; threads <= (arrays == 1 ? 1024 : 512); threads *= 2) {
+            if (threads < 256 && S * LX > threads) continue;
             if (LX > threads || (W < 8 && W != C) || (double)samples * ceil_div(groups, gs) > 2e9) continue;
             const size_t lds = arrays == 1 ? sizeof(double) * (2 << fold_of(D)) * threads + sizeof(float) * 2 * gs : 0;
             if (lds > 159 * 1024) continue;

@@ -311,6 +311,20 @@ def test_parameter_gradients_of_many_samples(samples, rows, C, groups, dx):
     _close(dw, want_w, ref.U * (added + 1.02 + 3) * size_w)  # (and each dz x^: the difference, the product with r, and with dz)
 
 
+# workgroups of every size: 64, 128 and 256 threads for samples of few rows
+SMALL = [(9000, 1, 64, 8), (9000, 7, 64, 8), (9001, 16, 64, 8), (8200, 3, 27, 9), (8193, 1, 520, 5), (8200, 1, 1000, 125), (9000, 2, 7, 7), (20000, 1, 2, 1),
+         (8200, 60, 15, 5), (8200, 1, 1032, 1), (2100, 1, 520, 65), (9000, 1, 91, 13)]
+
+
+@pytest.mark.parametrize("act", ["none", "silu"])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("samples, rows, C, groups", SMALL)
+def test_many_small_samples(samples, rows, C, groups, dtype, act):
+    test_forward(samples, rows, C, groups, dtype, act)
+    test_codes(samples, rows, C, groups, dtype, act)
+    test_backward(samples, rows, C, groups, dtype, act)
+
+
 # more samples than a launch takes, by a few; more than HIP's 2^32 threads would take with a workgroup each
 SEVERAL = [(2 * 131072 + 3, 1, 64, 8), (2048 + 5, 2, 8184, 8184), (2043 + 3, 2, 4104, 3), (1024 + 1, 3, 8192, 1), ((1 << 24) + 5, 1, 8, 2)]
 
