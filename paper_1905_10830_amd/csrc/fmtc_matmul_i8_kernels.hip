@@ -520,6 +520,26 @@ Plan make_plan(int64_t M, int64_t N, int64_t K) {
 
 int64_t split_ld(int64_t N) { return (N + 3) / 4 * 4; }
 
+// A grid has less than 2^32 threads: f(first, how many) for ranges of n things that take `threads` each
+template <class F>
+hipError_t in_launches(int64_t n, int64_t threads, F&& f) {
+    const int64_t most = (((int64_t)1 << 32) - 1) / threads;
+    if (most == 0) return hipErrorInvalidConfiguration;
+    hipError_t e = hipSuccess;
+    for (int64_t at = 0; at < n && e == hipSuccess; at += most) e = f(at, n - at < most ? n - at : most);
+    return e;
+}
+// the product with 16 `tiles` columns from the tile `at` on
+Product columns_of(Product p, int64_t at, int64_t tiles) {
+    const int64_t n = 16 * at;
+    p.b += n * p.ld_b;
+    p.sb += n;
+    if (p.bias) p.bias += n;
+    p.out = static_cast<char*>(p.out) + n * (p.out_type == FMTC_F32 ? 4 : 2);
+    p.N = p.N - n < 16 * tiles ? p.N - n : 16 * tiles;
+    return p;
+}
+
 }  // namespace
 
 size_t matmul_i8_workspace(int64_t M, int64_t N, int64_t K) {
@@ -548,9 +568,11 @@ hipError_t launch_i8_matmul(const fmtc_i8& a, const fmtc_i8& b, const float* d_b
     };
     auto rows = [&](auto mt) {
         constexpr int MT = decltype(mt)::value;
-        const int64_t n_tiles = (p.N + 15) / 16;
-        return launch(K_I8_MATMUL, k_i8_matmul_rows<MT, 1>, dim3((unsigned)(n_tiles * ((p.M + 16 * MT - 1) / (16 * MT)))),
-                      dim3(64 * kRowsWaves), 0, s, p, (uint32_t)n_tiles);
+        const int64_t row_tiles = (p.M + 16 * MT - 1) / (16 * MT);
+        return in_launches((p.N + 15) / 16, row_tiles * 64 * kRowsWaves, [&](int64_t at, int64_t n_tiles) {
+            return launch(K_I8_MATMUL, k_i8_matmul_rows<MT, 1>, dim3((unsigned)(n_tiles * row_tiles)), dim3(64 * kRowsWaves), 0, s,
+                          columns_of(p, at, n_tiles), (uint32_t)n_tiles);
+        });
     };
     hipError_t e;
     if (plan.kernel == kTiles256) e = tiles(Tile<2, 4, 8, 4, 2>{});
@@ -572,13 +594,15 @@ hipError_t launch_i8_linear_one(const void* d_x, int type, int64_t rows, int64_t
     return with_type(type, [&](auto ty) {
         using T = typename decltype(ty)::type;
         return with_bit(w.depth % 8 != 0, [&](auto rg) {
-            return launch(K_I8_MATMUL, k_i8_linear_rows<T, decltype(rg)::value>, dim3((unsigned)((p.N + 15) / 16)), dim3(kLinearThreads), 0, s, p,
-                          static_cast<const T*>(d_x), w.depth, ld_x, tpr);
+            return in_launches((p.N + 15) / 16, kLinearThreads, [&](int64_t at, int64_t n_tiles) {
+                return launch(K_I8_MATMUL, k_i8_linear_rows<T, decltype(rg)::value>, dim3((unsigned)n_tiles), dim3(kLinearThreads), 0, s,
+                              columns_of(p, at, n_tiles), static_cast<const T*>(d_x), w.depth, ld_x, tpr);
+            });
         });
     });
 }
 
-hipError_t launch_i8_quantize(const void* d_x, int type, int64_t rows, int64_t cols, int64_t ld_x, const fmtc_i8& out, hipStream_t s) {
+static hipError_t quantize_rows(const void* d_x, int type, int64_t rows, int64_t cols, int64_t ld_x, const fmtc_i8& out, hipStream_t s) {
     return with_type(type, [&](auto ty) {
         using T = typename decltype(ty)::type;
         const T* x = static_cast<const T*>(d_x);
@@ -599,6 +623,15 @@ hipError_t launch_i8_quantize(const void* d_x, int type, int64_t rows, int64_t c
             if (cols <= 8192) return go(Int<1024>{}, Int<1>{});
             return go(Int<1024>{}, Int<2>{});
         });
+    });
+}
+
+hipError_t launch_i8_quantize(const void* d_x, int type, int64_t rows, int64_t cols, int64_t ld_x, const fmtc_i8& out, hipStream_t s) {
+    return in_launches(rows, 1024, [&](int64_t at, int64_t n) {
+        fmtc_i8 some = out;
+        some.d_codes = static_cast<uint8_t*>(out.d_codes) + at * out.ld;
+        some.d_scales = out.d_scales + at;
+        return quantize_rows(static_cast<const char*>(d_x) + at * ld_x * (type == FMTC_F32 ? 4 : 2), type, n, cols, ld_x, some, s);
     });
 }
 

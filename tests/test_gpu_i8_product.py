@@ -196,6 +196,34 @@ def test_layer_of_a_row_that_is_not_finite(M):
     assert bool(torch.isnan(y[M - 1]).all()) and not bool(torch.isnan(y[:M - 1]).any())
 
 
+def test_more_rows_than_a_launch_takes():
+    """A grid has less than 2^32 threads: from 2^22 rows on there are several."""
+    for rows in (1 << 22, 2 * (1 << 22) + 3):
+        x = _values(rows, 8, torch.bfloat16)
+        q = fmtc.i8_quantize(x)
+        codes, scales = ref.codes(x)
+        assert torch.equal(q.codes[:, :8], codes) and not bool(q.codes[:, 8:].any()) and torch.equal(q.scales, scales)
+
+
+@pytest.mark.parametrize("M", [1, 3, 12])
+def test_more_columns_than_a_launch_takes(M):
+    """2^27 and some rows of weights (16 a workgroup of 512 threads)"""
+    N, K = (1 << 27) + 37, 6
+    store = torch.zeros((N, 128), dtype=torch.int8, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(1)
+    for c in range(K):
+        store[:, c] = torch.randint(-127, 128, (N,), generator=g, device="cuda", dtype=torch.int8)
+    scales = torch.rand(N, generator=g, device="cuda")
+    w, bias, x = fmtc.I8(store, scales, K), torch.randn(N, generator=g, device="cuda"), _values(M, K, torch.float32)
+    qa, sa = ref.codes(x)
+    want = sum(qa[:, c].float()[:, None] * store[:, c].float() for c in range(K))  # (whole numbers below 2^24: exact)
+    want = want * sa[:, None]
+    want = want * scales
+    want = want + bias
+    assert torch.equal(fmtc.i8_linear(x, w, bias=bias), want)
+    assert torch.equal(fmtc.i8_matmul(fmtc.i8_quantize(x), w, bias=bias, dtype=torch.float32), want)
+
+
 def test_no_rows():
     w = fmtc.i8_quantize(_values(40, 300, torch.float32))
     x = torch.empty((0, 300), dtype=torch.bfloat16, device="cuda")
