@@ -8,6 +8,8 @@
 // there.  Where a slab fits the registers of one workgroup, all is done with one read of the values (k_group_norm_once,
 // k_group_norm_backward_once); else the rows are cut in chunks, whose sums one kernel leaves in the workspace and the next one
 // adds up before it reads the values again.
+// Times are the kernels' own, on inputs and results that stay where they are (the memory-side cache serves a part), where not said
+// otherwise.
 #include <type_traits>
 
 #include "fmtc_block.h"
@@ -303,8 +305,8 @@ __device__ __forceinline__ const T* slab_of(const void* base, int64_t ld, const 
 
 constexpr int kUnroll = 4;  // rows of a thread on their way together
 
-// A slab in the registers of a workgroup, R rows a thread.  256 x 3136 x 64 (32 groups, a ReLU) 41 to 45 us, 4.6 to 5.0 TB/s
-// (in two passes 64); 128 x 784 x 256 23 us; 196 x 256 5.6 us, latency.
+// A slab in the registers of a workgroup, R rows a thread.  256 x 3136 x 64 (32 groups, a ReLU) 42 us (in two passes 64), with inputs
+// and results in other memory each time 52.8 us, 3.9 TB/s; 128 x 784 x 256 23 us; 196 x 256 5.2 us, latency.
 template <class T, int KIND, bool ONE, int R>
 __global__ __launch_bounds__(1024) void k_group_norm_once(Maps p, float eps, int act_kind, T* y, int64_t ld_y, float* __restrict__ stats) {
     extern __shared__ __attribute__((aligned(16))) double red[];
@@ -587,8 +589,8 @@ struct Terms {
 };
 
 // A slab in the registers of a workgroup, R rows a thread: x as it is and dz in f32 (an activation's gradient is computed
-// once: it costs as much as all the rest).  part[sample][2][C]: the sums by channel.  32 x 3136 x 256, 32 groups, silu 43 to 55 us: its
-// bytes take 30, but they come 32 of a row at a time and the activation's gradient is not all under them; 32 x 1568 x 512, 64
+// once: it costs as much as all the rest).  part[sample][2][C]: the sums by channel.  32 x 3136 x 256, 32 groups, silu 44 us (as
+// called 47, with other inputs and results each time 60): its bytes take 30, but they come 32 of a row at a time and the activation's gradient is not all under them; 32 x 1568 x 512, 64
 // bytes at a time, 39 us.  In two passes 64 us; computing dz twice 73 us.
 template <class T, int KIND, int ACT, int R>
 __global__ __launch_bounds__(512) void k_group_norm_backward_once(Maps p, const float* __restrict__ stats, const T* dy, int64_t ld_dy, T* dx,

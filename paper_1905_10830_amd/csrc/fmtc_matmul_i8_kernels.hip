@@ -3,6 +3,7 @@
 // The sum is exact in 32 bits, whatever its order, so that the depth can be taken by several wavefronts or workgroups
 // without a result depending on it.  b's rows are the matrix instruction's first operand and a's its second: a lane then
 // holds four consecutive columns n of one row m of the result, and the results leave in vectors.
+// Times are the kernels' own, on operands and results that stay where they are.
 #include <type_traits>
 
 #include "fmtc_block.h"
@@ -287,7 +288,7 @@ __global__ __launch_bounds__(kLinearThreads) void k_i8_linear_rows(Product p, co
 // Rows of 128 bytes in LDS, the 16-byte pieces of a row exchanged by a key of the row, so that 16 lanes that read the same
 // piece of 16 rows touch every bank once.
 //
-// bf16 results: 4096^3 56 to 58 us (2400 TOPS), 8192^3 445 to 468 us (2350 to 2470), 3137 x 960 x 1000 11.6 us.  The clock falls to 1.95 GHz
+// bf16 results: 4096^3 56 to 58 us (2400 TOPS), 8192^3 445 to 468 us (2350 to 2470), 3137 x 960 x 1000 12.6 us.  The clock falls to 1.95 GHz
 // under this load, and the matrix pipes are busy 59 % of it; without the loop's loads 8192^3 takes 340 us, without its LDS reads
 // too 318 us.  32 x 32 x 32 instructions with the same tiles: 515 us; one wavefront a SIMD with 128 x 128 results each: 521 us.
 template <int WM_, int WN_, int MT_, int NT_, int STAGES_>
