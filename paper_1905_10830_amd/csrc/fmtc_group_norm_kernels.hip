@@ -862,7 +862,7 @@ Plan choose(int64_t samples, int64_t S, int C, int groups, int size, int arrays)
         const bool tiny = W == C && samples > 4096;
         for (int threads = tiny ? 64 : 256; threads <= (arrays == 1 ? 1024 : 512); threads *= 2) {
             if (threads < 256 && S * LX > threads) continue;
-            if (LX > threads || (W < 8 && W != C) || (double)samples * ceil_div(groups, gs) > 2e9) continue;
+            if (LX > threads || (W < 8 && W != C)) continue;
             const size_t lds = arrays == 1 ? sizeof(double) * (2 << fold_of(D)) * threads + sizeof(float) * 2 * gs : 0;
             if (lds > 159 * 1024) continue;
             const int R = row_step(ceil_div(S, threads / LX), size);
